@@ -322,6 +322,108 @@ int qalora_forward_static(const qalora_desc* desc, int64_t m, const void* x, con
                           const float* qparams, const void* A, const void* B, void* y,
                           void* cuda_stream);
 
+/* ---- Key/value cache of a served model -------------------------------------
+ * A merged model (rank 0 layers, Section 3.2's efficient deployment) generates text with
+ * attention between its q/k/v projections and its output projection.  These calls keep the
+ * keys and values of earlier tokens in 8 bits, attend over them, and shorten a sequence by the
+ * attention its tokens gathered.  (The paper has no counterpart; the codes are symmetric
+ * 8-bit ones, one scale per block of tokens and head.)
+ *
+ * The cache is a pool of blocks of `block_tokens` tokens, caller-owned like every buffer:
+ *   codes  int8    [num_blocks][2][kv_heads][block_tokens][head_dim]   keys (0), values (1)
+ *   scales float32 [num_blocks][2][kv_heads]      an element is code * scale, scale >= 0
+ *   score  float32 [num_blocks][kv_heads][block_tokens]   attention weight gathered so far
+ *                                                         (only where a caller evicts)
+ * A sequence of a batch is described by DEVICE arrays, so that a captured graph can be
+ * replayed while sequences grow:
+ *   table  int32 [batch][max_blocks]   block b*max_blocks + j holds tokens j*block_tokens ...
+ *   lens   int32 [batch]               tokens of the sequence, this call's new ones included
+ *   starts int32 [batch + 1]           rows starts[b] .. starts[b+1]-1 of q, k, v, out belong
+ *                                      to sequence b: its n newest tokens, at positions
+ *                                      lens[b] - n ... lens[b] - 1
+ * and by three HOST bounds: `m` rows in all (<= QALORA_MAX_ROWS), `max_new` rows of one
+ * sequence, `max_len` tokens of one sequence.  A row whose position is negative (fewer tokens
+ * than rows) is not there: it is not stored, it attends to nothing, its output is 0 and its
+ * lse -infinity.  Entries that break a bound (a length above max_len or max_blocks *
+ * block_tokens, starts that fall or leave 0 .. m, a block outside the pool) never cause an
+ * access outside the buffers; the rows concerned are then unspecified.
+ * The heads of a group read one key head: query head h reads kv head h / (heads / kv_heads).
+ * Supported: heads a multiple of kv_heads, heads <= 1024; head_dim 64 or 128; block_tokens 16,
+ * 32, 64 or 128; num_blocks * 2 * kv_heads * block_tokens < 2^31 (QALORA_ERR_UNSUPPORTED_SHAPE
+ * beyond); batch <= 65535.  q, k and v are bf16 rows [m][heads or kv_heads][head_dim] whose
+ * rows lie `..._stride` elements apart (a multiple of 8, at least the row: the parts of a
+ * fused projection can be passed as they are); table, lens and starts need 4-byte alignment,
+ * everything else 16. */
+typedef struct qalora_kv_desc {
+  int32_t heads;         /* query heads                 */
+  int32_t kv_heads;      /* key/value heads             */
+  int32_t head_dim;
+  int32_t block_tokens;  /* tokens that share a scale   */
+  int32_t num_blocks;    /* blocks of the pool          */
+} qalora_kv_desc;
+
+/* Sizes in bytes of codes, scales and score (HOST pointers out). */
+int qalora_kv_cache_bytes(const qalora_kv_desc* desc, size_t* code_bytes, size_t* scale_bytes, size_t* score_bytes);
+
+/* Stores the new tokens' keys and values.  Per block, head and keys/values, in IEEE float32,
+ * one correctly rounded operation at a time, x the new elements that fall into the block:
+ *   need = max |x| / 127;  scale' = max(need, scale) if the block held earlier tokens of the
+ *   sequence, else need;  earlier codes c' = rint(c * (scale / scale'));
+ *   new codes c = clamp(rint(x / scale'), -127, 127), 0 where scale' is 0.
+ * (The scale of a block only grows while it fills; a code is re-rounded only when it does.)
+ *   score      : the new tokens' entries are set to 0; or NULL
+ *   dev_status : as in qalora_quantize, bit 0 is OR-ed in when x is not finite: infinities
+ *                become +-127, NaNs 0, and neither enters a scale.  May be NULL.
+ * A sequence of the batch may have no new rows.  No block may appear twice among those that
+ * the new tokens enter. */
+int qalora_kv_append(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t max_new,
+                     const int32_t* starts, const int32_t* lens, const int32_t* table, int32_t max_blocks,
+                     const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                     void* codes, float* scales, float* score, int32_t* dev_status, void* cuda_stream);
+
+/* Reads tokens back: row i of sequence b is its token first[b] + i, code * scale, in float32
+ * (out_bf16 == 0) or rounded to bf16: k, v out [m][kv_heads][head_dim] dense; either may be
+ * NULL to skip it.  Rows outside the table are left unwritten. */
+int qalora_kv_read(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t max_new,
+                   const int32_t* starts, const int32_t* first, const int32_t* table, int32_t max_blocks,
+                   const void* codes, const float* scales, void* k, void* v, int out_bf16, void* cuda_stream);
+
+/* Attention of the new tokens over their sequences (they must have been appended): with
+ * S[i, t] = softmax_scale * q_i . k_t for the tokens t at or before token i's position,
+ *   out_i = sum_t softmax(S[i, :])_t * v_t  (bf16 [m][heads][head_dim], dense)
+ *   lse_i = ln sum_t exp(S[i, t])           (float32 [m][heads], or NULL)
+ * and, when score_out is not NULL, for every token t of a sequence that has new rows,
+ *   score_out[t] = score_in[t] + sum over the sequence's new rows i and the heads of the group
+ *                  of softmax(S[i, :])_t
+ * in the layout of `score`; score_in may be NULL (zeros) and may be score_out.  Sums and
+ * softmax statistics are float32, products are exact (8-bit codes and bf16 in fp16 operands);
+ * a row's weights are rounded to fp16, relative to its largest, before they meet the values.
+ * softmax_scale must be positive and finite.  No atomics: results are reproducible bit for bit
+ * for given bounds and device.  `workspace`: qalora_kv_attention_workspace_bytes() bytes for
+ * the same batch, m, max_new and max_len, content undefined; its first int32 becomes the
+ * status word described at qalora_workspace_bytes. */
+int qalora_kv_attention_workspace_bytes(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t max_new,
+                                        int32_t max_len, int with_score, size_t* bytes);
+int qalora_kv_attention(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t max_new, int32_t max_len,
+                        const int32_t* starts, const int32_t* lens, const int32_t* table, int32_t max_blocks,
+                        const void* q, int64_t q_stride, const void* codes, const float* scales, float softmax_scale,
+                        void* out, float* lse, const float* score_in, float* score_out,
+                        void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Shortens sequences to at most `budget` tokens each: for every sequence and kv head the last
+ * `recent` tokens (0 <= recent <= budget) and, of the others, the budget - recent with the
+ * largest score (ties go to the earlier token; NaN counts as the largest), in their order, are
+ * copied to the blocks that dst_table names, with their scores.  Sequences of at most `budget`
+ * tokens are copied whole.  Scales are made anew from the copied values as by qalora_kv_append
+ * into empty blocks.  The destination blocks must not be among the sources; the caller frees
+ * the sources afterwards.
+ *   dst_lens out int32 [batch];  kept out int32 [batch][kv_heads][budget]: the source position
+ *   of each copied token, -1 beyond dst_lens. */
+int qalora_kv_evict(const qalora_kv_desc* desc, int32_t batch, int32_t max_len, int32_t budget, int32_t recent,
+                    const int32_t* lens, const int32_t* table, int32_t max_blocks,
+                    void* codes, float* scales, float* score, const int32_t* dst_table, int32_t dst_max_blocks,
+                    int32_t* dst_lens, int32_t* kept, void* cuda_stream);
+
 /* ---- Instrumentation (no counterpart in the paper) ------------------------ */
 
 /* Number of CUDA kernels this library has launched in this process so far

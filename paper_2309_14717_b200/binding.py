@@ -30,6 +30,8 @@ EXPORTS = (
     "qalora_forward_group_workspace_bytes", "qalora_forward_group",
     "qalora_forward_train", "qalora_backward_train",
     "qalora_debug_checks", "qalora_debug_report",
+    "qalora_kv_cache_bytes", "qalora_kv_append", "qalora_kv_read",
+    "qalora_kv_attention_workspace_bytes", "qalora_kv_attention", "qalora_kv_evict",
 )
 
 STATIC_SCRATCH_BYTES = 1 << 20
@@ -48,6 +50,11 @@ class GroupLayer(Structure):
 class AdamwHyper(Structure):
     _fields_ = [("lr", c_float), ("beta1", c_float), ("beta2", c_float), ("eps", c_float),
                 ("weight_decay", c_float), ("max_grad_norm", c_float), ("step", c_int64)]
+
+
+class KvDesc(Structure):
+    _fields_ = [("heads", c_int32), ("kv_heads", c_int32), ("head_dim", c_int32), ("block_tokens", c_int32),
+                ("num_blocks", c_int32)]
 
 
 class QaloraError(RuntimeError):
@@ -113,6 +120,21 @@ def load() -> ctypes.CDLL:
     lib.qalora_forward_group_workspace_bytes.argtypes = [POINTER(GroupLayer), c_int, c_int64, POINTER(c_size_t)]
     lib.qalora_forward_group.restype = c_int
     lib.qalora_forward_group.argtypes = [POINTER(GroupLayer), c_int, c_int64, c_void_p, c_size_t, c_void_p]
+    KV = POINTER(KvDesc)
+    lib.qalora_kv_cache_bytes.restype = c_int
+    lib.qalora_kv_cache_bytes.argtypes = [KV] + [POINTER(c_size_t)] * 3
+    lib.qalora_kv_append.restype = c_int
+    lib.qalora_kv_append.argtypes = ([KV, c_int32, c_int64, c_int32] + [c_void_p] * 3 + [c_int32, c_void_p, c_int64, c_void_p, c_int64]
+                                     + [c_void_p] * 5)
+    lib.qalora_kv_read.restype = c_int
+    lib.qalora_kv_read.argtypes = [KV, c_int32, c_int64, c_int32] + [c_void_p] * 3 + [c_int32] + [c_void_p] * 4 + [c_int, c_void_p]
+    lib.qalora_kv_attention_workspace_bytes.restype = c_int
+    lib.qalora_kv_attention_workspace_bytes.argtypes = [KV, c_int32, c_int64, c_int32, c_int32, c_int, POINTER(c_size_t)]
+    lib.qalora_kv_attention.restype = c_int
+    lib.qalora_kv_attention.argtypes = ([KV, c_int32, c_int64, c_int32, c_int32] + [c_void_p] * 3 + [c_int32, c_void_p, c_int64]
+                                        + [c_void_p] * 2 + [c_float] + [c_void_p] * 5 + [c_size_t, c_void_p])
+    lib.qalora_kv_evict.restype = c_int
+    lib.qalora_kv_evict.argtypes = ([KV] + [c_int32] * 4 + [c_void_p] * 2 + [c_int32] + [c_void_p] * 4 + [c_int32] + [c_void_p] * 3)
     lib.qalora_kernel_launches.restype = ctypes.c_uint64
     lib.qalora_kernel_launches.argtypes = []
     lib.qalora_profile_next_main_kernel.restype = c_int
@@ -322,6 +344,143 @@ def qalora_adamw_step(hyper: AdamwHyper, n: int, grad, param, exp_avg, exp_avg_s
                                                          _ptr(workspace),
                                                          workspace.numel() * workspace.element_size()
                                                          if workspace is not None else 0, _stream(stream)))
+
+
+# ---- key/value cache in 8 bits -----------------------------------------------------------------
+def kv_desc(heads: int, kv_heads: int, head_dim: int, block_tokens: int, num_blocks: int) -> KvDesc:
+    return KvDesc(heads, kv_heads, head_dim, block_tokens, num_blocks)
+
+
+def qalora_kv_cache_bytes(d: KvDesc):
+    """(bytes of codes, of scales, of score)."""
+    c, s, w = c_size_t(), c_size_t(), c_size_t()
+    _check("qalora_kv_cache_bytes", load().qalora_kv_cache_bytes(byref(d), byref(c), byref(s), byref(w)))
+    return c.value, s.value, w.value
+
+
+def alloc_kv_cache(d: KvDesc, device="cuda"):
+    """Zeroed (codes int8 [num_blocks, 2, kv_heads, block_tokens, head_dim], scales float32 [num_blocks, 2, kv_heads],
+    score float32 [num_blocks, kv_heads, block_tokens])."""
+    qalora_kv_cache_bytes(d)                       # (the descriptor's checks)
+    codes = torch.zeros((d.num_blocks, 2, d.kv_heads, d.block_tokens, d.head_dim), dtype=torch.int8, device=device)
+    scales = torch.zeros((d.num_blocks, 2, d.kv_heads), dtype=torch.float32, device=device)
+    score = torch.zeros((d.num_blocks, d.kv_heads, d.block_tokens), dtype=torch.float32, device=device)
+    return codes, scales, score
+
+
+def _kv_want(name, t, dtype, shape):
+    """Checks a tensor of the cache calls; None stands for any size in `shape`."""
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, wanted {tuple('any' if w is None else w for w in shape)}")
+
+
+def _kv_cache_want(d, codes, scales, score=None):
+    _kv_want("codes", codes, torch.int8, (d.num_blocks, 2, d.kv_heads, d.block_tokens, d.head_dim))
+    _kv_want("scales", scales, torch.float32, (d.num_blocks, 2, d.kv_heads))
+    if score is not None:
+        _kv_want("score", score, torch.float32, (d.num_blocks, d.kv_heads, d.block_tokens))
+
+
+def _kv_batch(starts, lens, table):
+    """(batch, max_blocks) of a batch's device arrays, checked."""
+    batch = lens.shape[0]
+    _kv_want("lens", lens, torch.int32, (None,))
+    _kv_want("table", table, torch.int32, (batch, None))
+    if starts is not None:
+        _kv_want("starts", starts, torch.int32, (batch + 1,))
+    return batch, table.shape[1]
+
+
+def _kv_rows(name, t, heads, dim):
+    """(pointer, row stride) of bf16 rows [m, heads, dim] whose rows may lie apart."""
+    _kv_want(name, t, torch.bfloat16, (None, heads, dim))
+    if not t.is_cuda:
+        raise ValueError("tensors must live on a CUDA device")
+    if t.shape[0] > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim)):
+        raise ValueError(f"{name}: the heads of a row must lie one behind the other")
+    return c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else heads * dim)
+
+
+def qalora_kv_append(d: KvDesc, max_new: int, starts, lens, table, k, v, codes, scales, score=None, dev_status=None,
+                     stream=None):
+    """Stores the new tokens' keys and values (rows k, v bf16 [m, kv_heads, head_dim]) in the cache."""
+    batch, max_blocks = _kv_batch(starts, lens, table)
+    _kv_cache_want(d, codes, scales, score)
+    k_ptr, k_stride = _kv_rows("k", k, d.kv_heads, d.head_dim)
+    v_ptr, v_stride = _kv_rows("v", v, d.kv_heads, d.head_dim)
+    if v.shape[0] != k.shape[0]:
+        raise ValueError("k and v have different numbers of rows")
+    _check("qalora_kv_append", load().qalora_kv_append(byref(d), batch, k.shape[0], max_new, _ptr(starts), _ptr(lens), _ptr(table),
+                                                       max_blocks, k_ptr, k_stride, v_ptr, v_stride, _ptr(codes), _ptr(scales),
+                                                       _ptr(score), _ptr(dev_status), _stream(stream)))
+
+
+def qalora_kv_read(d: KvDesc, max_new: int, starts, first, table, codes, scales, k, v, stream=None):
+    """Reads tokens back: row i of sequence b is its token first[b] + i, into k, v [m, kv_heads, head_dim] (float32 or
+    bfloat16; one of the two may be None)."""
+    batch, max_blocks = _kv_batch(starts, first, table)
+    _kv_cache_want(d, codes, scales)
+    out = k if k is not None else v
+    if out is None:
+        raise ValueError("k and v are both None")
+    if out.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("k and v must be float32 or bfloat16")
+    for name, t in (("k", k), ("v", v)):
+        if t is not None:
+            _kv_want(name, t, out.dtype, (out.shape[0], d.kv_heads, d.head_dim))
+    _check("qalora_kv_read", load().qalora_kv_read(byref(d), batch, out.shape[0], max_new, _ptr(starts), _ptr(first), _ptr(table),
+                                                   max_blocks, _ptr(codes), _ptr(scales), _ptr(k), _ptr(v),
+                                                   1 if out.dtype == torch.bfloat16 else 0, _stream(stream)))
+
+
+def qalora_kv_attention_workspace_bytes(d: KvDesc, batch: int, m: int, max_new: int, max_len: int, with_score: bool) -> int:
+    b = c_size_t()
+    _check("qalora_kv_attention_workspace_bytes", load().qalora_kv_attention_workspace_bytes(
+        byref(d), batch, m, max_new, max_len, 1 if with_score else 0, byref(b)))
+    return b.value
+
+
+def alloc_kv_workspace(d: KvDesc, batch: int, m: int, max_new: int, max_len: int, with_score: bool = False,
+                       device="cuda") -> torch.Tensor:
+    """Scratch of qalora_kv_attention_workspace_bytes() bytes; workspace_status() reads its status word."""
+    return torch.zeros(max(qalora_kv_attention_workspace_bytes(d, batch, m, max_new, max_len, with_score), 16),
+                       dtype=torch.uint8, device=device)
+
+
+def qalora_kv_attention(d: KvDesc, max_new: int, max_len: int, starts, lens, table, q, codes, scales, softmax_scale: float, out,
+                        lse=None, score_in=None, score_out=None, workspace=None, stream=None):
+    """out bf16 [m, heads, head_dim] = attention of the new tokens (rows q) over their sequences in the cache; lse float32
+    [m, heads]; score_out = score_in + the attention weight that each cached token gathered."""
+    batch, max_blocks = _kv_batch(starts, lens, table)
+    _kv_cache_want(d, codes, scales)
+    q_ptr, q_stride = _kv_rows("q", q, d.heads, d.head_dim)
+    m = q.shape[0]
+    _kv_want("out", out, torch.bfloat16, (m, d.heads, d.head_dim))
+    if lse is not None:
+        _kv_want("lse", lse, torch.float32, (m, d.heads))
+    for t in (score_in, score_out):
+        if t is not None:
+            _kv_want("score", t, torch.float32, (d.num_blocks, d.kv_heads, d.block_tokens))
+    _check("qalora_kv_attention", load().qalora_kv_attention(
+        byref(d), batch, m, max_new, max_len, _ptr(starts), _ptr(lens), _ptr(table), max_blocks, q_ptr, q_stride, _ptr(codes),
+        _ptr(scales), softmax_scale, _ptr(out), _ptr(lse), _ptr(score_in), _ptr(score_out), _ptr(workspace),
+        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream(stream)))
+
+
+def qalora_kv_evict(d: KvDesc, max_len: int, budget: int, recent: int, lens, table, codes, scales, score, dst_table, dst_lens, kept,
+                    stream=None):
+    """Copies at most `budget` tokens of each sequence and kv head (the last `recent` and those of largest score) to the
+    blocks of dst_table; dst_lens int32 [batch] and kept int32 [batch, kv_heads, budget] say how many and which."""
+    batch, max_blocks = _kv_batch(None, lens, table)
+    _kv_cache_want(d, codes, scales, score)
+    _kv_want("dst_table", dst_table, torch.int32, (batch, None))
+    _kv_want("dst_lens", dst_lens, torch.int32, (batch,))
+    _kv_want("kept", kept, torch.int32, (batch, d.kv_heads, budget))
+    _check("qalora_kv_evict", load().qalora_kv_evict(
+        byref(d), batch, max_len, budget, recent, _ptr(lens), _ptr(table), max_blocks, _ptr(codes), _ptr(scales), _ptr(score),
+        _ptr(dst_table), dst_table.shape[1], _ptr(dst_lens), _ptr(kept), _stream(stream)))
 
 
 def qalora_kernel_launches() -> int:

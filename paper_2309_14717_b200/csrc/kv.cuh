@@ -1,0 +1,111 @@
+// Shared helpers of the key/value cache kernels: the description of a batch, the checks of its
+// device-side entries, and conversions between values and 8-bit codes.
+#pragma once
+#include "common.cuh"
+
+namespace qalora {
+
+struct KvShape {
+  int heads, kv_heads, group, dim, block, num_blocks;
+};
+
+// A batch as the kernels see it.
+struct KvBatch {
+  const int32_t* starts;   // [batch + 1]
+  const int32_t* lens;     // [batch]
+  const int32_t* table;    // [batch][max_blocks]
+  int batch, max_blocks;
+  int m, max_new;          // rows in all / of one sequence
+  int max_len;             // tokens of one sequence that a kernel may visit: min(max_len, max_blocks * block)
+};
+
+int check_kv_desc(const qalora_kv_desc* desc, KvShape* sh);
+
+int launch_kv_append(const KvShape& sh, const KvBatch& b, const __nv_bfloat16* k, int64_t k_stride, const __nv_bfloat16* v,
+                     int64_t v_stride, int8_t* codes, float* scales, float* score, int32_t* dev_status, cudaStream_t st);
+int launch_kv_read(const KvShape& sh, const KvBatch& b, const int8_t* codes, const float* scales, void* k, void* v, bool bf16,
+                   cudaStream_t st);
+
+struct KvAttention {
+  const __nv_bfloat16* q;
+  int64_t q_stride;
+  const int8_t* codes;
+  const float* scales;
+  float softmax_scale;
+  __nv_bfloat16* out;
+  float* lse;
+  const float* score_in;
+  float* score_out;
+};
+size_t kv_attention_workspace(const KvShape& sh, int batch, int64_t m, int max_new, int max_len, bool with_score, Workspace* guards);
+int launch_kv_attention(const KvShape& sh, const KvBatch& b, const KvAttention& a, void* workspace, int max_len, cudaStream_t st);
+
+int launch_kv_evict(const KvShape& sh, const KvBatch& b, int budget, int recent, int8_t* codes, float* scales, float* score,
+                    const int32_t* dst_table, int dst_max_blocks, int32_t* dst_lens, int32_t* kept, cudaStream_t st);
+
+#ifdef __CUDACC__
+// Rows and tokens of sequence b; n == 0 where the entries break the call's bounds.
+struct KvSeq {
+  int row0, n;     // its rows are row0 .. row0 + n - 1
+  int len;         // tokens to visit, 0 .. max_len
+  int first;       // position of row row0 (negative: that row is not there)
+};
+__device__ __forceinline__ KvSeq kv_seq(const KvBatch& kb, int b) {
+  KvSeq s;
+  const int r0 = kb.starts[b], r1 = kb.starts[b + 1], len = kb.lens[b];
+  s.row0 = r0;
+  s.n = (r0 >= 0 && r1 >= r0 && r1 <= kb.m && r1 - r0 <= kb.max_new) ? r1 - r0 : 0;
+  s.len = len < 0 ? 0 : (len > kb.max_len ? kb.max_len : len);
+  s.first = s.len - s.n;
+  return s;
+}
+
+// Block that holds token t (0 <= t < max_blocks * block) of sequence b, or -1 when the entry is outside the pool.
+__device__ __forceinline__ int kv_block(const int32_t* table, int max_blocks, int num_blocks, int b, int j) {
+  const int id = table[(size_t)b * max_blocks + j];
+  return (id >= 0 && id < num_blocks) ? id : -1;
+}
+
+// Code of v under scale s > 0: clamp(rint(v / s), -127, 127) with the IEEE quotient.  v * (1/s) is
+// within 4e-5 of it for |v / s| <= 128 (two roundings of 2^-24 each), so that the division is
+// needed only where that product lies nearer than 1e-4 to a half-integer, where alone the two
+// could round apart.  `fast`: 1/s is neither zero nor infinite nor a subnormal.
+__device__ __forceinline__ bool kv_near_half(float t, float r) { return fabsf(t - r) > 0.4999f; }
+__device__ __forceinline__ float kv_code_div(float v, float s) {
+  const float t = __fdiv_rn(v, s);
+  return fminf(fmaxf(rintf(t), -127.f), 127.f);
+}
+__device__ __forceinline__ bool kv_fast_scale(float s) { return s > 1e-30f && s < 1e30f; }
+
+__device__ __forceinline__ uint32_t kv_pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {   // the low byte of each
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+
+// Four codes; `inv` = 1 / s.  The low byte of x / s + 1.5 * 2^23 is the rounded quotient in two's
+// complement, so no float-to-integer conversion is needed.
+__device__ __forceinline__ uint32_t kv_codes4(const float (&v)[4], float s, float inv) {
+  uint32_t c[4];
+  bool near = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float t = __fmul_rn(v[i], inv), u = __fadd_rn(t, 12582912.f);
+    c[i] = __float_as_uint(u);
+    near |= kv_near_half(t, __fadd_rn(u, -12582912.f));
+  }
+  if (near) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = __float_as_uint(__fadd_rn(kv_code_div(v[i], s), 12582912.f));
+  }
+  return kv_pack4(c[0], c[1], c[2], c[3]);
+}
+// The same for scales whose inverse is not an ordinary number and for elements that may not be finite.
+__device__ __forceinline__ uint32_t kv_codes4_any(const float (&v)[4], float s) {
+  uint32_t c[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    c[i] = (s > 0.f && v[i] == v[i]) ? (uint32_t)(int)kv_code_div(v[i], s) : 0u;
+  return kv_pack4(c[0], c[1], c[2], c[3]);
+}
+#endif
+
+}  // namespace qalora

@@ -1,0 +1,633 @@
+// Attention of a few new tokens over the 8-bit key/value cache (the generating step of a served
+// model), bound by HBM: every cached code is read once per kv head.
+#define QALORA_TU 12
+#include <cuda_fp16.h>
+
+#include "kv_ptx.cuh"
+#include "kv.cuh"
+#include "tc_host.cuh"
+
+namespace qalora {
+
+namespace {
+
+constexpr int AT_WARPS = 4;                       // consumer warps; one more warp brings the tiles in
+constexpr int AT_THREADS = (AT_WARPS + 1) * 32;
+constexpr int AT_MAX_BATCH = 1024;                // sequences of one launch (the plan lies in shared memory)
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNoMax = -1e30f;                  // running maximum of a row that has met no token
+constexpr float kGrow = 6.f;                      // a row is rescaled when its maximum has grown by 2^6 or more
+constexpr float kLift = 8.f;                      // weights are kept times 2^8: at most 2^14 in fp16, and 2^-22 of the largest
+                                                  // weight still is an ordinary fp16 number
+
+struct AttnArgs {
+  KvShape sh;
+  KvBatch kb;
+  KvAttention at;
+  int* status;
+  uint32_t* plan;        // [batch + 2]: first unit of each sequence, their number, units per thread block
+  float* parts;          // partial results, two slots per thread block (see part_slot)
+  float* lse2;           // [m][heads] log2 of the row's sum, for the gathered weights
+  float* logits;         // [m][heads][logit_stride] scaled scores in powers of two, or NULL
+  long long logit_stride;
+  int batch0;            // first sequence of this launch
+  int units_grid;        // thread blocks of the first kernel
+};
+
+// Work is cut into units of TOK tokens of one (sequence, kv head, tile of ROWS rows), in this order;
+// every thread block takes the same number of consecutive units, whatever the sequences' lengths.
+template <int TOK, int ROWS>
+__device__ __forceinline__ void seq_units(const KvBatch& kb, const KvShape& sh, const KvSeq& s, int* row_tiles, int* tiles) {
+  *row_tiles = (s.n * sh.group + ROWS - 1) / ROWS;
+  *tiles = s.len > 0 ? (s.len + TOK - 1) / TOK : 1;           // (no tokens: one empty unit writes the zero rows)
+}
+
+struct UnitPlace {
+  int b, h, rt, tile, tiles;
+};
+template <int TOK, int ROWS>
+__device__ __forceinline__ UnitPlace find_unit(const AttnArgs& a, const uint32_t* prefix, uint32_t u) {
+  int lo = 0, hi = a.kb.batch;                                 // last b with prefix[b] <= u (its successor's is larger)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (prefix[mid] <= u) lo = mid; else hi = mid;
+  }
+  UnitPlace p;
+  p.b = lo;
+  const KvSeq s = kv_seq(a.kb, lo);
+  int row_tiles;
+  seq_units<TOK, ROWS>(a.kb, a.sh, s, &row_tiles, &p.tiles);
+  const uint32_t r = u - prefix[lo], per_head = (uint32_t)row_tiles * p.tiles;
+  p.h = (int)(r / per_head);
+  const uint32_t q = r % per_head;
+  p.rt = (int)(q / p.tiles);
+  p.tile = (int)(q % p.tiles);
+  return p;
+}
+
+template <int D, int MT, int SUB>
+struct AtSmem {
+  static constexpr int ROWS = 16 * MT, TOK = 16 * AT_WARPS * SUB, SUBS = TOK / 16;
+  static constexpr int TILE = TOK * D;                          // bytes of keys (or values) of a unit
+  static constexpr int STAGES = 65536 / (2 * TILE);
+  static constexpr int MERGE = AT_WARPS * 16 * D * 4;
+  static constexpr int OFF_MERGE = STAGES * 2 * TILE;
+  static constexpr int OFF_SCALES = OFF_MERGE + MERGE;                        // [STAGES][2][SUBS]
+  static constexpr int OFF_ML = OFF_SCALES + STAGES * 2 * SUBS * 4;           // [AT_WARPS][16][2]
+  static constexpr int OFF_BARS = OFF_ML + AT_WARPS * 16 * 2 * 4;
+  static constexpr int OFF_FLAG = OFF_BARS + STAGES * 2 * 8;
+  static constexpr int OFF_PLAN = OFF_FLAG + 16;
+  static int total(int batch) { return OFF_PLAN + (batch + 2) * 4 + 1024; }   // (the window starts on a 1 KiB boundary)
+};
+
+// Partial result `slot` = 2 * block + (0: the rows' units began in an earlier block, 1: they began here):
+// [ROWS] of {maximum, sum}, then [ROWS][D] sums of weighted values relative to that maximum.
+template <int D, int ROWS>
+__host__ __device__ constexpr long long part_floats() { return (long long)ROWS * (D + 2); }
+
+// D: head width; MT: tiles of 16 rows (new tokens x heads of a group); SUB: 16-token steps per warp and unit.
+// Keys are the B operand of m16n8k16 straight from their row-major bytes: ldmatrix hands a lane four
+// consecutive codes of one token, which are a 16-wide step's two B registers if the same permutation of the
+// channels is applied to the query; values are B through the transposing ldmatrix, whose 16-bit elements are
+// pairs of channels: the even and the odd channels become two column tiles.  Codes turn into fp16
+// exactly (1024 + 128 + c by byte permutation, minus 1152), the query is fp16 after a power-of-two scaling
+// per row (bf16 has fewer bits), so the scores are sums of exact products in float32.
+// Every warp keeps maximum, sum and output of its own tokens; the warps meet only at the end of a row tile.
+template <int D, int MT, int SUB>
+__global__ void __launch_bounds__(AT_THREADS, 2)
+kv_attend_kernel(const __grid_constant__ CUtensorMap map, AttnArgs a, int* dbg) {
+  using S = AtSmem<D, MT, SUB>;
+  constexpr int ROWS = S::ROWS, TOK = S::TOK, SUBS = S::SUBS, STAGES = S::STAGES;
+  constexpr int KSTEPS = D / 16;
+  extern __shared__ uint8_t raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t sbase = ptx::smem_u32(smem);
+  float* scale_ring = reinterpret_cast<float*>(smem + S::OFF_SCALES);
+  float* ml = reinterpret_cast<float*>(smem + S::OFF_ML);
+  float* merge = reinterpret_cast<float*>(smem + S::OFF_MERGE);
+  volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_FLAG);
+  uint32_t* prefix = reinterpret_cast<uint32_t*>(smem + S::OFF_PLAN);
+  const uint32_t bars = sbase + S::OFF_BARS;
+  auto full = [&](int s) { return bars + s * 16; };
+  auto empty = [&](int s) { return bars + s * 16 + 8; };
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const KvShape& sh = a.sh;
+
+  if (tid == 0) {
+    *flag = 0;
+    for (int s = 0; s < STAGES; ++s) { ptx::mbar_init(full(s), 1); ptx::mbar_init(empty(s), AT_WARPS); }
+    ptx::fence_mbar_init();
+    if (blockIdx.x == 0 && a.batch0 == 0) *a.status = 0;
+  }
+  // the plan: an exclusive sum over the sequences' units, by one warp
+  if (warp == AT_WARPS) {
+    ptx::prefetch_tensormap(&map);
+    uint32_t run = 0;
+    for (int b0 = 0; b0 < a.kb.batch; b0 += 32) {
+      uint32_t n = 0;
+      if (b0 + lane < a.kb.batch) {
+        const KvSeq s = kv_seq(a.kb, b0 + lane);
+        int rt, tiles;
+        seq_units<TOK, ROWS>(a.kb, sh, s, &rt, &tiles);
+        n = (uint32_t)sh.kv_heads * rt * tiles;
+      }
+      uint32_t sum = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += up;
+      }
+      if (b0 + lane < a.kb.batch) prefix[b0 + lane] = run + sum - n;
+      run += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    const uint32_t per_block = (run + gridDim.x - 1) / gridDim.x;
+    if (lane == 0) { prefix[a.kb.batch] = run; prefix[a.kb.batch + 1] = per_block; }
+    __syncwarp();
+    if (blockIdx.x == 0)
+      for (int i = lane; i < a.kb.batch + 2; i += 32) a.plan[i] = prefix[i];
+  }
+  __syncthreads();
+  const uint32_t total = prefix[a.kb.batch], per_block = prefix[a.kb.batch + 1];
+  const uint32_t u0 = blockIdx.x * per_block, u1 = u0 + per_block < total ? u0 + per_block : total;
+  if (u0 >= total) return;
+
+  if (warp == AT_WARPS) {
+    // ---- producer: the lanes look up the blocks and scales of 32 / SUBS units ahead, then issue their copies
+    constexpr int AHEAD = 32 / SUBS;
+    const int sub = lane % SUBS, box = sh.block < TOK ? sh.block : TOK;
+    struct Look { int k_row, v_row; float ks, vs; };
+    auto look = [&](uint32_t u) {
+      Look l{-1, -1, 0.f, 0.f};
+      if (u >= u1) return l;
+      const UnitPlace p = find_unit<TOK, ROWS>(a, prefix, u);
+      const KvSeq s = kv_seq(a.kb, p.b);
+      const int t = p.tile * TOK + sub * 16;
+      if (t >= s.len) return l;
+      const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, p.b, t / sh.block);
+      if (id < 0) return l;
+      const long long k_plane = ((long long)id * 2) * sh.kv_heads + p.h, v_plane = k_plane + sh.kv_heads;
+      l.ks = a.at.scales[k_plane];
+      l.vs = a.at.scales[v_plane];
+      l.k_row = (int)(k_plane * sh.block + t % sh.block);
+      l.v_row = (int)(v_plane * sh.block + t % sh.block);
+      return l;
+    };
+    Look cur = look(u0 + lane / SUBS);
+    uint32_t it = 0;
+    bool ok = true;
+    for (uint32_t base = u0; base < u1 && ok; base += AHEAD) {
+      const Look next = look(base + AHEAD + lane / SUBS);
+      for (int i = 0; i < AHEAD && base + i < u1; ++i, ++it) {
+        const int st = it % STAGES;
+        if (it >= STAGES) ok = __all_sync(0xffffffffu, ptx::mbar_wait(empty(st), ((it / STAGES) - 1) & 1, flag));
+        if (!ok) break;
+        const bool mine = lane / SUBS == i;
+        if (mine) { scale_ring[st * 2 * SUBS + sub] = cur.ks; scale_ring[st * 2 * SUBS + SUBS + sub] = cur.vs; }
+        const bool issues = mine && cur.k_row >= 0 && (sub * 16) % box == 0;
+        const int boxes = __popc(__ballot_sync(0xffffffffu, issues));
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_expect_tx(full(st), (uint32_t)(boxes * 2 * box * D));
+        __syncwarp();
+        if (issues) {
+          const uint32_t at = sbase + st * 2 * S::TILE + sub * 16 * D;
+          ptx::tma_load_2d(at, &map, 0, cur.k_row, full(st));
+          ptx::tma_load_2d(at + S::TILE, &map, 0, cur.v_row, full(st));
+        }
+      }
+      cur = next;
+    }
+  } else {
+    // ---- consumers
+    const int g8 = lane >> 2, q4 = lane & 3;          // row within 8, quad lane
+    uint32_t qf[MT][KSTEPS][4];
+    float q_scale[MT][2];                              // softmax_scale * log2(e) / (the row's power of two)
+    int limit[MT][2];                                  // last token the row sees, -1: none
+    float mrow[MT][2], lrow[MT][2], o[MT][D / 8][4], ref;
+    UnitPlace p{};
+    KvSeq s{};
+    bool fresh = true, ok = true;
+    int rows = 0, limit_lo = 0;
+    const float* logit_row[MT][2];
+    for (uint32_t u = u0, it = 0; u < u1; ++u, ++it) {
+      if (fresh) {
+        p = find_unit<TOK, ROWS>(a, prefix, u);
+        s = kv_seq(a.kb, p.b);
+        rows = s.n * sh.group - p.rt * ROWS;
+        if (rows > ROWS) rows = ROWS;
+        limit_lo = s.first + (p.rt * ROWS) / sh.group;                 // the earliest row's
+        ref = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const int r = p.rt * ROWS + mt * 16 + hf * 8 + g8, i = r / sh.group, g = r % sh.group;
+            const bool there = mt * 16 + hf * 8 + g8 < rows;
+            limit[mt][hf] = there ? s.first + i : -1;
+            uint2 w[KSTEPS];
+            uint32_t mx = 0;
+            const __nv_bfloat16* src = a.at.q + (long long)(s.row0 + i) * a.at.q_stride + (long long)(p.h * sh.group + g) * D;
+#pragma unroll
+            for (int k = 0; k < KSTEPS; ++k) {
+              w[k] = make_uint2(0, 0);
+              if (there && QALORA_CHECK(dbg, s.row0 + i, a.kb.m)) w[k] = *reinterpret_cast<const uint2*>(src + k * 16 + q4 * 4);
+              mx = __vmaxu2(__vmaxu2(mx, w[k].x & 0x7fff7fffu), w[k].y & 0x7fff7fffu);
+            }
+            mx = max(mx & 0xffffu, mx >> 16);
+            mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+            mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+            // times a power of two that brings the row's largest element to 2^14 .. 2^15: exact in fp16
+            // down to 2^-28 of it
+            int e = 268 - (int)(mx >> 7);
+            e = e > 254 ? 254 : (e < 1 ? 1 : e);
+            const float f = __uint_as_float((uint32_t)e << 23);
+            q_scale[mt][hf] = a.at.softmax_scale * kLog2e * __uint_as_float((uint32_t)(254 - e) << 23);
+            if (e == 254) q_scale[mt][hf] = a.at.softmax_scale * kLog2e * 0x1p-127f;
+#pragma unroll
+            for (int k = 0; k < KSTEPS; ++k) {
+              const float x0 = __uint_as_float(w[k].x << 16) * f, x1 = __uint_as_float(w[k].x & 0xffff0000u) * f;
+              const float x2 = __uint_as_float(w[k].y << 16) * f, x3 = __uint_as_float(w[k].y & 0xffff0000u) * f;
+              qf[mt][k][hf] = kvp::pack_half2(x0, x1);
+              qf[mt][k][2 + hf] = kvp::pack_half2(x2, x3);
+            }
+            mrow[mt][hf] = kNoMax;
+            lrow[mt][hf] = 0.f;
+            const int head = p.h * sh.group + g;
+            logit_row[mt][hf] = a.logits != nullptr && there
+                                    ? a.logits + ((long long)(s.row0 + i) * sh.heads + head) * a.logit_stride : nullptr;
+          }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[mt][n][c] = 0.f;
+        fresh = false;
+      }
+      const int st = it % STAGES;
+      ok = ok && ptx::mbar_wait(full(st), (it / STAGES) & 1, flag);
+      ok = __all_sync(0xffffffffu, ok);
+      const uint32_t k_base = sbase + st * 2 * S::TILE, v_base = k_base + S::TILE;
+#pragma unroll 1
+      for (int sb = 0; sb < SUB; ++sb) {
+        const int sub = sb * AT_WARPS + warp, t0 = p.tile * TOK + sub * 16;
+        if (t0 >= s.len || !ok) break;
+        const float ks = scale_ring[st * 2 * SUBS + sub], vs = scale_ring[st * 2 * SUBS + SUBS + sub];
+        // scores of 16 tokens: two column tiles
+        float sc[MT][2][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sc[mt][j][c] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int quarter = 0; quarter < D / 64; ++quarter) {
+            const int tok = sub * 16 + j * 8 + (lane & 7), chunk = quarter * 4 + (lane >> 3);
+            uint32_t r[4];
+            kvp::ldmatrix_x4(r, k_base + kvp::swizzled<D>(tok, chunk));
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              uint32_t b0, b1;
+              kvp::codes_to_half(r[x], b0, b1);
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) kvp::mma16816(sc[mt][j], qf[mt][quarter * 4 + x], b0, b1);
+            }
+          }
+        // scaled scores in powers of two, masked
+        const bool edge = t0 + 15 > limit_lo || rows < ROWS;
+        bool grow = false;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const float f = q_scale[mt][hf] * ks;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                float& x = sc[mt][j][hf * 2 + c];
+                x *= f;
+                if (edge && t0 + j * 8 + q4 * 2 + c > limit[mt][hf]) x = -INFINITY;
+                grow |= x > mrow[mt][hf] + kGrow;
+              }
+            if (logit_row[mt][hf] != nullptr) {
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const int t = t0 + j * 8 + q4 * 2;
+                if (QALORA_CHECK(dbg, t + 1, a.logit_stride))
+                  *reinterpret_cast<float2*>(const_cast<float*>(logit_row[mt][hf]) + t) = make_float2(sc[mt][j][hf * 2], sc[mt][j][hf * 2 + 1]);
+              }
+            }
+          }
+        if (__any_sync(0xffffffffu, grow) || vs > ref) {
+          // rare: bring the rows to their new maximum, and the outputs to the new largest value scale
+          const float ref_new = vs > ref ? vs : ref, ref_ratio = ref_new > 0.f ? ref / ref_new : 0.f;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            float by[2];
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              float mx = fmaxf(fmaxf(sc[mt][0][hf * 2], sc[mt][0][hf * 2 + 1]), fmaxf(sc[mt][1][hf * 2], sc[mt][1][hf * 2 + 1]));
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+              mx = fmaxf(mx, mrow[mt][hf]);
+              by[hf] = exp2f(mrow[mt][hf] - mx);
+              mrow[mt][hf] = mx;
+              lrow[mt][hf] *= by[hf];
+              by[hf] *= ref_ratio;
+            }
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n) {
+              o[mt][n][0] *= by[0]; o[mt][n][1] *= by[0];
+              o[mt][n][2] *= by[1]; o[mt][n][3] *= by[1];
+            }
+          }
+          ref = ref_new;
+        }
+        const float v_rel = ref > 0.f ? vs / ref : 0.f;
+        uint32_t pf[MT][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float e0 = kvp::exp2_fast(sc[mt][j][hf * 2] - (mrow[mt][hf] - kLift));
+              const float e1 = kvp::exp2_fast(sc[mt][j][hf * 2 + 1] - (mrow[mt][hf] - kLift));
+              lrow[mt][hf] += e0 + e1;
+              pf[mt][j * 2 + hf] = kvp::pack_half2(e0 * v_rel, e1 * v_rel);
+            }
+#pragma unroll
+        for (int c2 = 0; c2 < D / 32; ++c2) {
+          const int tok = sub * 16 + (lane & 15), chunk = c2 * 2 + (lane >> 4);
+          uint32_t r[4];
+          kvp::ldmatrix_x4_trans(r, v_base + kvp::swizzled<D>(tok, chunk));
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            uint32_t e0, d0, e1, d1;                    // even / odd channels of tokens 0-7 and 8-15
+            kvp::pairs_to_half(r[2 * x], e0, d0);
+            kvp::pairs_to_half(r[2 * x + 1], e1, d1);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              kvp::mma16816(o[mt][(c2 * 2 + x) * 2], pf[mt], e0, e1);
+              kvp::mma16816(o[mt][(c2 * 2 + x) * 2 + 1], pf[mt], d0, d1);
+            }
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(empty(st));
+
+      if (++p.tile == p.tiles || u + 1 == u1) {
+        // ---- the row tile ends here, or goes on in the next block: the warps' shares are added up
+        const uint32_t row_tile_first = u + 1 - p.tile;          // unit of its tile 0
+        const bool whole = row_tile_first >= u0 && p.tile == p.tiles;
+        const int slot = 2 * (int)blockIdx.x + (row_tile_first < u0 ? 0 : 1);
+        float* part = a.parts + slot * part_floats<D, ROWS>();
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            float l = lrow[mt][hf];
+            l += __shfl_xor_sync(0xffffffffu, l, 1);
+            l += __shfl_xor_sync(0xffffffffu, l, 2);
+            const int r = hf * 8 + g8;
+            if (q4 == 0) { ml[(warp * 16 + r) * 2] = mrow[mt][hf]; ml[(warp * 16 + r) * 2 + 1] = l; }
+            if (mt * 16 + r < rows)
+#pragma unroll
+              for (int jj = 0; jj < D / 16; ++jj) {
+                const float4 x = make_float4(o[mt][2 * jj][hf * 2] * ref, o[mt][2 * jj + 1][hf * 2] * ref,
+                                             o[mt][2 * jj][hf * 2 + 1] * ref, o[mt][2 * jj + 1][hf * 2 + 1] * ref);
+                *reinterpret_cast<float4*>(merge + (warp * 16 + r) * D + jj * 16 + q4 * 4) = x;
+              }
+          }
+          ptx::named_barrier(1, AT_WARPS * 32);
+          const int here = rows - mt * 16 < 16 ? rows - mt * 16 : 16;
+          for (int i = tid; i < here * (D / 4); i += AT_WARPS * 32) {
+            const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+            float mx = kNoMax, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < AT_WARPS; ++w) mx = fmaxf(mx, ml[(w * 16 + r) * 2]);
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < AT_WARPS; ++w) {
+              const float by = exp2f(ml[(w * 16 + r) * 2] - mx);
+              const float4 y = *reinterpret_cast<const float4*>(merge + (w * 16 + r) * D + d);
+              l = fmaf(by, ml[(w * 16 + r) * 2 + 1], l);
+              x.x = fmaf(by, y.x, x.x); x.y = fmaf(by, y.y, x.y); x.z = fmaf(by, y.z, x.z); x.w = fmaf(by, y.w, x.w);
+            }
+            const int row = mt * 16 + r;
+            if (whole) {
+              const int rr = p.rt * ROWS + row, tok = s.row0 + rr / sh.group, head = p.h * sh.group + rr % sh.group;
+              const long long at = (long long)tok * sh.heads + head;
+              if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) continue;
+              kvp::store_row4(a.at.out + at * D + d, x, l);
+              if (d == 0) kvp::store_lse(a.at.lse, a.lse2, at, mx, l, kLift);
+            } else if (QALORA_CHECK(dbg, slot, 2 * a.units_grid)) {
+              *reinterpret_cast<float4*>(part + 2 * ROWS + row * D + d) = x;
+              if (d == 0) *reinterpret_cast<float2*>(part + 2 * row) = make_float2(mx, l);
+            }
+          }
+          ptx::named_barrier(1, AT_WARPS * 32);
+        }
+        fresh = true;
+      }
+    }
+  }
+  if (*flag != 0 && lane == 0) *a.status = 1;
+}
+
+// Joins the partial results of row tiles that several blocks shared (first blocks of the grid), and
+// adds up the gathered weights from the stored scores (the other blocks).
+template <int D, int ROWS, int TOK>
+__global__ void __launch_bounds__(128)
+kv_join_kernel(AttnArgs a, int join_blocks, int row_tiles_max, int* dbg) {
+  __shared__ float row_lse[1024];
+  const KvShape& sh = a.sh;
+  const int b = blockIdx.y, tid = threadIdx.x;
+  const KvSeq s = kv_seq(a.kb, b);
+  if (s.n == 0) return;
+  const uint32_t per_block = a.plan[a.kb.batch + 1], first = a.plan[b];
+  int row_tiles, tiles;
+  seq_units<TOK, ROWS>(a.kb, sh, s, &row_tiles, &tiles);
+  if ((int)blockIdx.x < join_blocks) {
+    const int h = blockIdx.x / row_tiles_max, rt = blockIdx.x % row_tiles_max;
+    if (rt >= row_tiles) return;
+    const uint32_t f = first + ((uint32_t)h * row_tiles + rt) * tiles;
+    const uint32_t c0 = f / per_block, c1 = (f + tiles - 1) / per_block;
+    if (c0 == c1) return;                                       // one block had all of it
+    const int rows = s.n * sh.group - rt * ROWS < ROWS ? s.n * sh.group - rt * ROWS : ROWS;
+    for (int i = tid; i < rows * (D / 4); i += 128) {
+      const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+      float mx = kNoMax, l = 0.f;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (uint32_t c = c0; c <= c1; ++c) {                     // in the order of the tokens
+        const float* part = a.parts + (2ll * c + (f < c * per_block ? 0 : 1)) * part_floats<D, ROWS>();
+        const float2 v = *reinterpret_cast<const float2*>(part + 2 * r);
+        const float4 y = *reinterpret_cast<const float4*>(part + 2 * ROWS + r * D + d);
+        const float top = fmaxf(mx, v.x), b0 = exp2f(mx - top), b1 = exp2f(v.x - top);
+        l = l * b0 + v.y * b1;
+        x.x = x.x * b0 + y.x * b1; x.y = x.y * b0 + y.y * b1; x.z = x.z * b0 + y.z * b1; x.w = x.w * b0 + y.w * b1;
+        mx = top;
+      }
+      const int rr = rt * ROWS + r, tok = s.row0 + rr / sh.group, head = h * sh.group + rr % sh.group;
+      const long long at = (long long)tok * sh.heads + head;
+      if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) continue;
+      kvp::store_row4(a.at.out + at * D + d, x, l);
+      if (d == 0) kvp::store_lse(a.at.lse, nullptr, at, mx, l, kLift);
+    }
+    return;
+  }
+  // gathered weights: 512 tokens of one kv head, four per thread
+  const int idx = (int)blockIdx.x - join_blocks, h = idx % sh.kv_heads, t0 = (idx / sh.kv_heads) * 512;
+  if (t0 >= s.len) return;
+  const int rows = s.n * sh.group, t = t0 + tid * 4;
+  float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int r0 = 0; r0 < rows; r0 += 1024) {
+    __syncthreads();
+    for (int r = r0 + tid; r < rows && r < r0 + 1024; r += 128) {
+      const int rt = r / ROWS;
+      const uint32_t f = first + ((uint32_t)h * row_tiles + rt) * tiles;
+      const uint32_t c0 = f / per_block, c1 = (f + tiles - 1) / per_block;
+      const long long at = (long long)(s.row0 + r / sh.group) * sh.heads + h * sh.group + r % sh.group;
+      float v = 0.f;
+      if (c0 == c1) v = QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads) ? a.lse2[at] : 0.f;
+      else {
+        float mx = kNoMax, l = 0.f;
+        for (uint32_t c = c0; c <= c1; ++c) {
+          const float* part = a.parts + (2ll * c + (f < c * per_block ? 0 : 1)) * part_floats<D, ROWS>();
+          const float2 q = *reinterpret_cast<const float2*>(part + 2 * (r % ROWS));
+          const float top = fmaxf(mx, q.x);
+          l = l * exp2f(mx - top) + q.y * exp2f(q.x - top);
+          mx = top;
+        }
+        v = l > 0.f ? mx - kLift + log2f(l) : INFINITY;
+      }
+      row_lse[r - r0] = v;
+    }
+    __syncthreads();
+    if (t < s.len) {
+      const int stop = rows - r0 < 1024 ? rows - r0 : 1024;
+      for (int r = 0; r < stop; ++r) {
+        const long long at = (long long)(s.row0 + (r0 + r) / sh.group) * sh.heads + h * sh.group + (r0 + r) % sh.group;
+        const float4 x = __ldcs(reinterpret_cast<const float4*>(a.logits + at * a.logit_stride + t));
+        const float n = row_lse[r];
+        w.x += kvp::exp2_fast(x.x - n); w.y += kvp::exp2_fast(x.y - n);
+        w.z += kvp::exp2_fast(x.z - n); w.w += kvp::exp2_fast(x.w - n);
+      }
+    }
+  }
+  if (t >= s.len) return;
+  const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t / sh.block);
+  if (id < 0) return;
+  const long long at = ((long long)id * sh.kv_heads + h) * sh.block + t % sh.block;
+  const float got[4] = {w.x, w.y, w.z, w.w};
+  for (int c = 0; c < 4 && t + c < s.len; ++c)
+    a.at.score_out[at + c] = (a.at.score_in != nullptr ? a.at.score_in[at + c] : 0.f) + got[c];
+}
+
+// keys and values as one matrix of rows of `dim` bytes; a box is the part of a block that a unit takes
+bool make_cache_map(CUtensorMap* map, const int8_t* codes, const KvShape& sh, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (fn == nullptr) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)sh.dim, (cuuint64_t)sh.num_blocks * 2 * sh.kv_heads * sh.block};
+  cuuint64_t strides[1] = {(cuuint64_t)sh.dim};
+  cuuint32_t box[2] = {(cuuint32_t)sh.dim, (cuuint32_t)box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(codes), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, sh.dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int MT, int SUB>
+int attend(const AttnArgs& a, cudaStream_t st) {
+  using S = AtSmem<D, MT, SUB>;
+  CUtensorMap map;
+  if (!make_cache_map(&map, a.at.codes, a.sh, a.sh.block < S::TOK ? a.sh.block : S::TOK)) return QALORA_ERR_CUDA;
+  static PerDeviceOnce once;
+  const int ok = once.run([] {
+    return cudaFuncSetAttribute(kv_attend_kernel<D, MT, SUB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::total(AT_MAX_BATCH));
+  });
+  if (ok != QALORA_OK) return ok;
+  {
+    MainKernelProbe probe("kv_attend_kernel", st);
+    kv_attend_kernel<D, MT, SUB><<<a.units_grid, AT_THREADS, S::total(a.kb.batch), st>>>(map, a, debug_words());
+  }
+  const int row_tiles = (a.kb.max_new * a.sh.group + S::ROWS - 1) / S::ROWS, join = a.sh.kv_heads * row_tiles;
+  const int score_blocks = a.logits != nullptr ? a.sh.kv_heads * ((a.kb.max_len + 511) / 512) : 0;
+  kv_join_kernel<D, S::ROWS, S::TOK><<<dim3((unsigned)(join + score_blocks), (unsigned)a.kb.batch), 128, 0, st>>>(
+      a, join, row_tiles, debug_words());
+  count_launch(2);
+  return cuda_status(cudaGetLastError());
+}
+
+struct AttnLayout {
+  size_t status, plan, parts, lse2, logits, total;
+};
+
+int row_tiles_of(const KvShape& sh, int max_new) { return max_new * sh.group <= 16 ? 1 : 2; }     // MT
+
+AttnLayout attention_layout(const KvShape& sh, int batch, int64_t m, int max_new, int max_len, bool with_score, Workspace* guards) {
+  AttnLayout w{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += round_up(bytes, 256);
+    if (kDebugBuild) { if (guards != nullptr) guards->guard[guards->n_guard++] = off; off += kGuardBytes; }
+    return at;
+  };
+  const int rows = 16 * row_tiles_of(sh, max_new);
+  w.status = take(256);
+  w.plan = take((size_t)((batch < AT_MAX_BATCH ? batch : AT_MAX_BATCH) + 2) * 4);
+  w.parts = take((size_t)device_sm_count() * 2 * 2 * rows * (sh.dim + 2) * 4);
+  w.lse2 = take(with_score ? (size_t)m * sh.heads * 4 : 0);
+  w.logits = take(with_score ? (size_t)m * sh.heads * round_up((size_t)max_len, 128) * 4 : 0);
+  w.total = off;
+  return w;
+}
+
+}  // namespace
+
+size_t kv_attention_workspace(const KvShape& sh, int batch, int64_t m, int max_new, int max_len, bool with_score, Workspace* guards) {
+  return attention_layout(sh, batch, m, max_new, max_len, with_score, guards).total;
+}
+
+int launch_kv_attention(const KvShape& sh, const KvBatch& b, const KvAttention& at, void* workspace, int max_len, cudaStream_t st) {
+  const AttnLayout L = attention_layout(sh, b.batch, b.m, b.max_new, max_len, at.score_out != nullptr, nullptr);
+  char* base = static_cast<char*>(workspace);
+  AttnArgs a{};
+  a.sh = sh;
+  a.kb = b;
+  a.at = at;
+  a.status = reinterpret_cast<int*>(base + L.status);
+  a.plan = reinterpret_cast<uint32_t*>(base + L.plan);
+  a.parts = reinterpret_cast<float*>(base + L.parts);
+  a.lse2 = at.score_out != nullptr ? reinterpret_cast<float*>(base + L.lse2) : nullptr;
+  a.logits = at.score_out != nullptr ? reinterpret_cast<float*>(base + L.logits) : nullptr;
+  a.logit_stride = (long long)round_up((size_t)max_len, 128);
+  const int mt = row_tiles_of(sh, b.max_new), tok = sh.dim == 128 ? 64 : 128;
+  const long long tiles = b.max_len > 0 ? (b.max_len + tok - 1) / tok : 1;
+  const long long per_seq = tiles * sh.kv_heads * ((b.max_new * (long long)sh.group + 16 * mt - 1) / (16 * mt));
+  if (per_seq > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
+  // sequences of one launch: their plan fits shared memory and their units 31 bits
+  const long long fit = 0x7fffffffll / per_seq;
+  const int chunk = (int)(fit < AT_MAX_BATCH ? fit : AT_MAX_BATCH);
+  for (int b0 = 0; b0 < b.batch; b0 += chunk) {
+    a.batch0 = b0;
+    a.kb.batch = b.batch - b0 < chunk ? b.batch - b0 : chunk;
+    a.kb.starts = b.starts + b0;
+    a.kb.lens = b.lens + b0;
+    a.kb.table = b.table + (size_t)b0 * b.max_blocks;
+    const long long units = per_seq * a.kb.batch, most = 2ll * device_sm_count();
+    a.units_grid = (int)(units < most ? units : most);
+    int r;
+    if (sh.dim == 128) r = mt == 1 ? attend<128, 1, 1>(a, st) : attend<128, 2, 1>(a, st);
+    else r = mt == 1 ? attend<64, 1, 2>(a, st) : attend<64, 2, 2>(a, st);
+    if (r != QALORA_OK) return r;
+  }
+  return QALORA_OK;
+}
+
+}  // namespace qalora

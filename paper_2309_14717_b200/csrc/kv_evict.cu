@@ -1,0 +1,288 @@
+// Eviction from the key/value cache by accumulated attention weight: for every sequence and kv
+// head the places of the tokens to keep (select), then their move to new blocks (gather).
+#define QALORA_TU 11
+#include <cooperative_groups.h>
+
+#include "kv.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace qalora {
+
+namespace {
+
+constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
+constexpr int SEL_BINS = 2048;                  // 11 bits of the key per pass: 11 + 11 + 10
+constexpr int SEL_MAX_CLUSTER = 8;
+constexpr int SEL_CACHED_KEYS = 49152;          // keys of one thread block that fit its shared memory (192 KiB)
+
+// Order-preserving key of a score: larger score, larger key; -0 equals +0; NaN is the largest.
+__device__ __forceinline__ uint32_t score_key(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+struct SelectArgs {
+  const float* score;
+  int32_t* dst_lens;
+  int32_t* kept;
+  int budget, recent, cached;
+};
+
+// One cluster per (sequence, kv head); its thread blocks share the candidates (all tokens but the
+// last `recent`) as consecutive ranges.  A radix select of the (budget - recent)-th largest key:
+// three passes of 11, 11 and 10 bits, each a histogram per thread block that the cluster adds up
+// through distributed shared memory.  The keys stay in shared memory between the passes, so
+// the scores are read once.  Then every warp counts its range, one scan turns the counts into
+// offsets, and the places come out in order.
+__global__ void __launch_bounds__(SEL_THREADS)
+kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
+  extern __shared__ uint32_t keys[];            // [per] when cached
+  __shared__ uint32_t hist[SEL_BINS];
+  __shared__ uint32_t warp_part[SEL_WARPS], warp_gt[SEL_WARPS], warp_eq[SEL_WARPS];
+  __shared__ uint32_t found[3];                 // bin, keys above it, keys in it
+  __shared__ uint32_t share[2];                 // this block's keys above / at the threshold, read by its cluster
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int pair = blockIdx.x / C, b = pair / sh.kv_heads, h = pair % sh.kv_heads;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  int len = kb.lens[b];
+  len = len < 0 ? 0 : (len > kb.max_len ? kb.max_len : len);
+  const int count = len < a.budget ? len : a.budget;
+  int32_t* kept = a.kept + ((long long)b * sh.kv_heads + h) * a.budget;
+  if (h == 0 && rank == 0 && tid == 0) a.dst_lens[b] = count;
+  for (int i = count + rank * SEL_THREADS + tid; i < a.budget; i += C * SEL_THREADS) kept[i] = -1;
+  if (len <= a.budget) {                        // (the same for the whole cluster)
+    for (int i = rank * SEL_THREADS + tid; i < len; i += C * SEL_THREADS) kept[i] = i;
+    return;
+  }
+  const int cand = len - a.recent, want = a.budget - a.recent;          // cand > want >= 0
+  for (int i = rank * SEL_THREADS + tid; i < a.recent; i += C * SEL_THREADS)
+    if (QALORA_CHECK(dbg, want + i, a.budget)) kept[want + i] = cand + i;
+  if (want == 0) return;
+  const int per = (cand + C - 1) / C, begin = rank * per, end = begin + per < cand ? begin + per : cand;
+  auto fetch = [&](int t) -> uint32_t {
+    const int id = kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, t / sh.block);
+    return id < 0 ? 0u : score_key(a.score[((long long)id * sh.kv_heads + h) * sh.block + t % sh.block]);
+  };
+  if (a.cached) {
+#pragma unroll 4
+    for (int t = begin + tid; t < end; t += SEL_THREADS) keys[t - begin] = fetch(t);
+    __syncthreads();
+  }
+  auto key_at = [&](int t) -> uint32_t { return a.cached ? keys[t - begin] : fetch(t); };
+
+  uint32_t prefix = 0, mask = 0, left = (uint32_t)want;                 // keys still wanted among those that match prefix
+  constexpr int SHIFT[3] = {21, 10, 0}, BITS[3] = {11, 11, 10};
+#pragma unroll 1
+  for (int p = 0; p < 3; ++p) {
+    for (int i = tid; i < SEL_BINS; i += SEL_THREADS) hist[i] = 0;
+    __syncthreads();
+    const uint32_t digit_mask = (1u << BITS[p]) - 1;
+    for (int t = begin + tid; t < end; t += SEL_THREADS) {
+      const uint32_t key = key_at(t);
+      if ((key & mask) == prefix) atomicAdd(&hist[(key >> SHIFT[p]) & digit_mask], 1u);
+    }
+    cluster.sync();
+    // thread i owns the bins 2047 - 2i and 2046 - 2i: an inclusive scan over threads counts from the largest key down
+    uint32_t n0 = 0, n1 = 0;
+    const int hi = SEL_BINS - 1 - 2 * tid;
+    for (int r = 0; r < C; ++r) {
+      const uint32_t* other = cluster.map_shared_rank(hist, r);
+      n0 += other[hi];
+      n1 += other[hi - 1];
+    }
+    uint32_t sum = n0 + n1;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += up;
+    }
+    if (lane == 31) warp_part[warp] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int w = 0; w < warp; ++w) before += warp_part[w];
+    const uint32_t above = before + sum - n0 - n1;                      // keys in larger bins than this thread's
+    if (above < left && left <= above + n0) { found[0] = hi; found[1] = above; found[2] = n0; }
+    else if (above + n0 < left && left <= above + n0 + n1) { found[0] = hi - 1; found[1] = above + n0; found[2] = n1; }
+    cluster.sync();                                                     // (also: nobody reads this histogram any more)
+    prefix |= found[0] << SHIFT[p];
+    mask |= digit_mask << SHIFT[p];
+    left -= found[1];
+  }
+  // prefix is the want-th largest key; `left` of the keys equal to it are taken, the earliest ones
+  const int span = ((per + SEL_WARPS - 1) / SEL_WARPS + 31) & ~31;
+  const int w0 = begin + warp * span, w1 = w0 + span < end ? w0 + span : end;
+  uint32_t gt = 0, eq = 0;
+  for (int t = w0 + lane; t < w1; t += 32) {
+    const uint32_t key = key_at(t);
+    gt += key > prefix;
+    eq += key == prefix;
+  }
+  gt = __reduce_add_sync(0xffffffffu, gt);
+  eq = __reduce_add_sync(0xffffffffu, eq);
+  if (lane == 0) { warp_gt[warp] = gt; warp_eq[warp] = eq; }
+  __syncthreads();
+  uint32_t gt0 = 0, eq0 = 0;
+  for (int w = 0; w < warp; ++w) { gt0 += warp_gt[w]; eq0 += warp_eq[w]; }
+  if (warp == SEL_WARPS - 1 && lane == 0) { share[0] = gt0 + gt; share[1] = eq0 + eq; }
+  cluster.sync();
+  for (int r = 0; r < rank; ++r) {
+    const uint32_t* other = cluster.map_shared_rank(share, r);
+    gt0 += other[0];
+    eq0 += other[1];
+  }
+  for (int t0 = w0; t0 < w1; t0 += 32) {
+    const int t = t0 + lane;
+    const uint32_t key = t < w1 ? key_at(t) : 0u;
+    const bool is_gt = t < w1 && key > prefix, is_eq = t < w1 && key == prefix;
+    const uint32_t below = (1u << lane) - 1, bg = __ballot_sync(0xffffffffu, is_gt), be = __ballot_sync(0xffffffffu, is_eq);
+    const uint32_t my_eq = eq0 + __popc(be & below);
+    if (is_gt || (is_eq && my_eq < left)) {
+      const uint32_t at = gt0 + __popc(bg & below) + (my_eq < left ? my_eq : left);
+      if (QALORA_CHECK(dbg, at, a.budget)) kept[at] = t;
+    }
+    gt0 += __popc(bg);
+    eq0 += __popc(be);
+  }
+  cluster.sync();                               // a block's shared memory is read by its cluster until here
+}
+
+// One thread block per (destination block, kv head, sequence): 128 threads move the keys and 128 the
+// values.  The codes stay in registers between the maximum and the rounding.
+template <int D, int PASSES>
+__global__ void __launch_bounds__(256)
+kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__ kept, int8_t* codes, float* scales, float* score,
+                 const int32_t* __restrict__ dst_table, int dst_max_blocks, int* dbg) {
+  constexpr int CHUNKS = D / 16, ROWS = 128 / CHUNKS;
+  __shared__ float warp_max[8];
+  const int b = blockIdx.y, h = blockIdx.x % sh.kv_heads, j = blockIdx.x / sh.kv_heads;
+  int len = kb.lens[b];
+  len = len < 0 ? 0 : (len > kb.max_len ? kb.max_len : len);
+  int count = len < budget ? len : budget;
+  const int base = j * sh.block;
+  if (base >= count || j >= dst_max_blocks) return;
+  const int n = count - base < sh.block ? count - base : sh.block;
+  const int dst_id = kv_block(dst_table, dst_max_blocks, sh.num_blocks, b, j);
+  if (dst_id < 0) return;
+  const int32_t* from = kept + ((long long)b * sh.kv_heads + h) * budget + base;
+  const int which = threadIdx.x >> 7, t = threadIdx.x & 127, chunk = t % CHUNKS, row = t / CHUNKS;
+  uint4 x[PASSES];
+  float s[PASSES], mx = 0.f;
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int slot = p * ROWS + row;
+    x[p] = make_uint4(0, 0, 0, 0);
+    s[p] = 0.f;
+    if (slot < n) {
+      const int pos = from[slot];
+      const int id = QALORA_CHECK(dbg, pos, len) ? kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, pos / sh.block) : -1;
+      if (id >= 0) {
+        const long long plane = ((long long)id * 2 + which) * sh.kv_heads + h;
+        s[p] = scales[plane];
+        x[p] = *reinterpret_cast<const uint4*>(codes + (plane * sh.block + pos % sh.block) * D + chunk * 16);
+      }
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const uint32_t w[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
+    int m = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) m = max(m, abs((int)(int8_t)(w[e >> 2] >> (8 * (e & 3)))));
+    mx = fmaxf(mx, __fmul_rn((float)m, s[p]));          // (the rounded product grows with the code)
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = mx;
+  __syncthreads();
+  mx = fmaxf(fmaxf(warp_max[which * 4], warp_max[which * 4 + 1]), fmaxf(warp_max[which * 4 + 2], warp_max[which * 4 + 3]));
+  const float scale = __fdiv_rn(mx, 127.f);
+  const long long plane = ((long long)dst_id * 2 + which) * sh.kv_heads + h;
+  if (t == 0 && QALORA_CHECK(dbg, plane, (long long)sh.num_blocks * 2 * sh.kv_heads)) scales[plane] = scale;
+  const bool fast = kv_fast_scale(scale);
+  const float inv = fast ? __fdiv_rn(1.f, scale) : 0.f;
+  int8_t* dst = codes + plane * sh.block * D;
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int slot = p * ROWS + row;
+    if (slot >= n || !QALORA_CHECK(dbg, slot, sh.block)) continue;
+    const uint32_t w[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
+    uint32_t o[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = __fmul_rn((float)(int8_t)(w[q] >> (8 * e)), s[p]);
+      o[q] = fast ? kv_codes4(v, scale, inv) : kv_codes4_any(v, scale);
+    }
+    *reinterpret_cast<uint4*>(dst + slot * D + chunk * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+  for (int slot = threadIdx.x; slot < n; slot += 256) {
+    const int pos = from[slot];
+    const int id = QALORA_CHECK(dbg, pos, len) ? kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, pos / sh.block) : -1;
+    const float moved = id < 0 ? 0.f : score[((long long)id * sh.kv_heads + h) * sh.block + pos % sh.block];
+    score[((long long)dst_id * sh.kv_heads + h) * sh.block + slot] = moved;
+  }
+}
+
+template <int D>
+int gather_passes(const KvShape& sh, const KvBatch& b, dim3 grid, int budget, const int32_t* kept, int8_t* codes, float* scales,
+                  float* score, const int32_t* dst_table, int dst_max_blocks, cudaStream_t st) {
+  const int rows = 128 / (D / 16), passes = (sh.block + rows - 1) / rows;
+#define QALORA_KV_GATHER(P)                                                                                                  \
+  case P:                                                                                                                    \
+    kv_gather_kernel<D, P><<<grid, 256, 0, st>>>(sh, b, budget, kept, codes, scales, score, dst_table, dst_max_blocks,       \
+                                                 debug_words());                                                            \
+    break;
+  switch (passes) {
+    QALORA_KV_GATHER(1) QALORA_KV_GATHER(2) QALORA_KV_GATHER(4) QALORA_KV_GATHER(8)
+    default: return QALORA_ERR_UNSUPPORTED_SHAPE;
+  }
+#undef QALORA_KV_GATHER
+  count_launch();
+  return cuda_status(cudaGetLastError());
+}
+
+}  // namespace
+
+int launch_kv_evict(const KvShape& sh, const KvBatch& b, int budget, int recent, int8_t* codes, float* scales, float* score,
+                    const int32_t* dst_table, int dst_max_blocks, int32_t* dst_lens, int32_t* kept, cudaStream_t st) {
+  // Thread blocks per cluster: enough to hold every key in shared memory, and more while the
+  // grid leaves multiprocessors free and each still has some thousand keys.
+  const long long pairs = (long long)b.batch * sh.kv_heads;
+  int C = 1;
+  while (C < SEL_MAX_CLUSTER && ((b.max_len + C - 1) / C > SEL_CACHED_KEYS / 2 ||
+                                 (pairs * C * 2 <= device_sm_count() && b.max_len / C >= 4096)))
+    C *= 2;
+  const int per = (b.max_len + C - 1) / C;
+  if (pairs * C > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
+  SelectArgs a{score, dst_lens, kept, budget, recent, per <= SEL_CACHED_KEYS ? 1 : 0};
+  static PerDeviceOnce once;
+  const int ok = once.run([] {
+    return cudaFuncSetAttribute(kv_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_CACHED_KEYS * 4);
+  });
+  if (ok != QALORA_OK) return ok;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(pairs * C));
+  cfg.blockDim = dim3(SEL_THREADS);
+  cfg.dynamicSmemBytes = a.cached ? (size_t)per * 4 : 0;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)C;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kv_select_kernel, sh, b, a, debug_words()) != cudaSuccess) return QALORA_ERR_CUDA;
+  count_launch();
+  const int most = b.max_len < budget ? b.max_len : budget, blocks = (most + sh.block - 1) / sh.block;
+  if (blocks == 0) return cuda_status(cudaGetLastError());
+  if ((long long)blocks * sh.kv_heads > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
+  const dim3 grid((unsigned)(blocks * sh.kv_heads), (unsigned)b.batch);
+  return sh.dim == 128 ? gather_passes<128>(sh, b, grid, budget, kept, codes, scales, score, dst_table, dst_max_blocks, st)
+                       : gather_passes<64>(sh, b, grid, budget, kept, codes, scales, score, dst_table, dst_max_blocks, st);
+}
+
+}  // namespace qalora

@@ -1,0 +1,80 @@
+// Inline-PTX wrappers and small device functions of the attention kernels over the 8-bit cache.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "ptx.cuh"
+
+namespace qalora {
+namespace kvp {
+
+// Byte offset of 16-byte chunk `chunk` of row `row` in a tile of rows of D bytes that a TMA copy with
+// 128-byte (D = 128) or 64-byte (D = 64) swizzle wrote to a 1 KiB boundary.
+template <int D>
+__device__ __forceinline__ uint32_t swizzled(int row, int chunk) {
+  return (uint32_t)(row * D + ((D == 128 ? chunk ^ (row & 7) : chunk ^ ((row >> 1) & 3)) << 4));
+}
+
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// d += a (16 x 16, row) * b (16 x 8, col), fp16 operands, float32 accumulator
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// fp16 pairs hold 1152 + c (0x6400 is 1024, its last place 1): minus 1152 is c, exactly
+__device__ __forceinline__ uint32_t minus_1152(uint32_t w) {
+  const uint32_t k = 0x64806480u;
+  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&w), *reinterpret_cast<const __half2*>(&k));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// four codes in a row -> fp16 pairs (0, 1) and (2, 3)
+__device__ __forceinline__ void codes_to_half(uint32_t c, uint32_t& p01, uint32_t& p23) {
+  const uint32_t u = c ^ 0x80808080u;
+  p01 = minus_1152(__byte_perm(u, 0x64646464u, 0x4140));
+  p23 = minus_1152(__byte_perm(u, 0x64646464u, 0x4342));
+}
+// codes (t, d), (t, d+1), (t+1, d), (t+1, d+1) -> fp16 pairs over t for channel d and channel d+1
+__device__ __forceinline__ void pairs_to_half(uint32_t c, uint32_t& even, uint32_t& odd) {
+  const uint32_t u = c ^ 0x80808080u;
+  even = minus_1152(__byte_perm(u, 0x64646464u, 0x4240));
+  odd = minus_1152(__byte_perm(u, 0x64646464u, 0x4341));
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {           // relative error about 2^-22; exp2(-inf) = 0
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// out = x / l in bf16, zeros for a row that saw no token
+__device__ __forceinline__ void store_row4(__nv_bfloat16* out, float4 x, float l) {
+  const float by = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
+  const __nv_bfloat162 a = __floats2bfloat162_rn(x.x * by, x.y * by), b = __floats2bfloat162_rn(x.z * by, x.w * by);
+  uint2 w;
+  w.x = *reinterpret_cast<const uint32_t*>(&a);
+  w.y = *reinterpret_cast<const uint32_t*>(&b);
+  *reinterpret_cast<uint2*>(out) = w;
+}
+// lse in natural logarithms for the caller, in powers of two for the gathered weights (there +infinity
+// stands for a row without tokens, so that its weights come out as zero); the sum l carries 2^lift
+__device__ __forceinline__ void store_lse(float* lse, float* lse2, long long at, float mx, float l, float lift) {
+  const float v = mx - lift + log2f(l);
+  if (lse != nullptr) lse[at] = l == 0.f ? -INFINITY : v * 0.6931471805599453f;
+  if (lse2 != nullptr) lse2[at] = l == 0.f ? INFINITY : v;
+}
+
+}  // namespace kvp
+}  // namespace qalora
