@@ -17,6 +17,7 @@ struct KvBatch {
   int batch, max_blocks;
   int m, max_new;          // rows in all / of one sequence
   int max_len;             // tokens of one sequence that a kernel may visit: min(max_len, max_blocks * block)
+  int n_lo, n_hi;          // sequences with fewer or more new rows are another kernel's
 };
 
 int check_kv_desc(const qalora_kv_desc* desc, KvShape* sh);
@@ -40,6 +41,17 @@ struct KvAttention {
 size_t kv_attention_workspace(const KvShape& sh, int batch, int64_t m, int max_new, int max_len, bool with_score, Workspace* guards);
 int launch_kv_attention(const KvShape& sh, const KvBatch& b, const KvAttention& a, void* workspace, int max_len, cudaStream_t st);
 
+// Many new rows per sequence (kv_prompt.cu): tensor-core tiles of 128 rows x 128 tokens.
+struct KvPromptScratch {
+  int splits;              // parts of a row tile's tokens
+  long long slots;         // tiles of 128 rows of one kv head, at most
+  size_t part_ml, part_o;  // bytes: {maximum, sum} and output of each part's rows (splits > 1)
+  size_t q_image, rows;    // bytes: the queries' tiles as the tensor core reads them, {scale, lse} of their rows (gathered weights)
+};
+KvPromptScratch kv_prompt_scratch(const KvShape& sh, int batch, int64_t m, int max_len, bool with_score);
+int launch_kv_prompt(const KvShape& sh, const KvBatch& b, const KvAttention& a, const KvPromptScratch& s, float2* part_ml,
+                     float* part_o, uint8_t* q_image, float2* rows, int* status, cudaStream_t st);
+
 int launch_kv_evict(const KvShape& sh, const KvBatch& b, int budget, int recent, int8_t* codes, float* scales, float* score,
                     const int32_t* dst_table, int dst_max_blocks, int32_t* dst_lens, int32_t* kept, cudaStream_t st);
 
@@ -54,7 +66,7 @@ __device__ __forceinline__ KvSeq kv_seq(const KvBatch& kb, int b) {
   KvSeq s;
   const int r0 = kb.starts[b], r1 = kb.starts[b + 1], len = kb.lens[b];
   s.row0 = r0;
-  s.n = (r0 >= 0 && r1 >= r0 && r1 <= kb.m && r1 - r0 <= kb.max_new) ? r1 - r0 : 0;
+  s.n = (r0 >= 0 && r1 >= r0 && r1 <= kb.m && r1 - r0 <= kb.n_hi && r1 - r0 >= kb.n_lo) ? r1 - r0 : 0;
   s.len = len < 0 ? 0 : (len > kb.max_len ? kb.max_len : len);
   s.first = s.len - s.n;
   return s;

@@ -38,6 +38,8 @@ KvBatch make_batch(const KvShape& sh, const int32_t* starts, const int32_t* lens
   b.batch = batch; b.max_blocks = max_blocks;
   b.m = (int)m; b.max_new = max_new;
   b.max_len = (int)(max_len < most ? max_len : most);
+  b.n_lo = 0;
+  b.n_hi = max_new;
   return b;
 }
 

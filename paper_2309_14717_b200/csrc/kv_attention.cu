@@ -27,8 +27,8 @@ struct AttnArgs {
   int* status;
   uint32_t* plan;        // [batch + 2]: first unit of each sequence, their number, units per thread block
   float* parts;          // partial results, two slots per thread block (see part_slot)
-  float* lse2;           // [m][heads] log2 of the row's sum, for the gathered weights
-  float* logits;         // [m][heads][logit_stride] scaled scores in powers of two, or NULL
+  float* lse2;           // [sequence][n_hi][heads] log2 of the row's sum, for the gathered weights
+  float* logits;         // [sequence][n_hi][heads][logit_stride] scaled scores in powers of two, or NULL
   long long logit_stride;
   int batch0;            // first sequence of this launch
   int units_grid;        // thread blocks of the first kernel
@@ -253,7 +253,7 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, AttnArgs a, int* dbg) 
             lrow[mt][hf] = 0.f;
             const int head = p.h * sh.group + g;
             logit_row[mt][hf] = a.logits != nullptr && there
-                                    ? a.logits + ((long long)(s.row0 + i) * sh.heads + head) * a.logit_stride : nullptr;
+                                    ? a.logits + ((long long)((a.batch0 + p.b) * a.kb.n_hi + i) * sh.heads + head) * a.logit_stride : nullptr;
           }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -424,7 +424,10 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, AttnArgs a, int* dbg) 
               const long long at = (long long)tok * sh.heads + head;
               if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) continue;
               kvp::store_row4(a.at.out + at * D + d, x, l);
-              if (d == 0) kvp::store_lse(a.at.lse, a.lse2, at, mx, l, kLift);
+              if (d == 0) {
+                const long long own = (long long)((a.batch0 + p.b) * a.kb.n_hi + rr / sh.group) * sh.heads + head;
+                kvp::store_lse(a.at.lse, at, a.lse2, own, mx, l, kLift);
+              }
             } else if (QALORA_CHECK(dbg, slot, 2 * a.units_grid)) {
               *reinterpret_cast<float4*>(part + 2 * ROWS + row * D + d) = x;
               if (d == 0) *reinterpret_cast<float2*>(part + 2 * row) = make_float2(mx, l);
@@ -476,7 +479,7 @@ kv_join_kernel(AttnArgs a, int join_blocks, int row_tiles_max, int* dbg) {
       const long long at = (long long)tok * sh.heads + head;
       if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) continue;
       kvp::store_row4(a.at.out + at * D + d, x, l);
-      if (d == 0) kvp::store_lse(a.at.lse, nullptr, at, mx, l, kLift);
+      if (d == 0) kvp::store_lse(a.at.lse, at, nullptr, 0, mx, l, kLift);
     }
     return;
   }
@@ -491,9 +494,8 @@ kv_join_kernel(AttnArgs a, int join_blocks, int row_tiles_max, int* dbg) {
       const int rt = r / ROWS;
       const uint32_t f = first + ((uint32_t)h * row_tiles + rt) * tiles;
       const uint32_t c0 = f / per_block, c1 = (f + tiles - 1) / per_block;
-      const long long at = (long long)(s.row0 + r / sh.group) * sh.heads + h * sh.group + r % sh.group;
       float v = 0.f;
-      if (c0 == c1) v = QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads) ? a.lse2[at] : 0.f;
+      if (c0 == c1) v = a.lse2[(long long)((a.batch0 + b) * a.kb.n_hi + r / sh.group) * sh.heads + h * sh.group + r % sh.group];
       else {
         float mx = kNoMax, l = 0.f;
         for (uint32_t c = c0; c <= c1; ++c) {
@@ -511,7 +513,7 @@ kv_join_kernel(AttnArgs a, int join_blocks, int row_tiles_max, int* dbg) {
     if (t < s.len) {
       const int stop = rows - r0 < 1024 ? rows - r0 : 1024;
       for (int r = 0; r < stop; ++r) {
-        const long long at = (long long)(s.row0 + (r0 + r) / sh.group) * sh.heads + h * sh.group + (r0 + r) % sh.group;
+        const long long at = (long long)((a.batch0 + b) * a.kb.n_hi + (r0 + r) / sh.group) * sh.heads + h * sh.group + (r0 + r) % sh.group;
         const float4 x = __ldcs(reinterpret_cast<const float4*>(a.logits + at * a.logit_stride + t));
         const float n = row_lse[r];
         w.x += kvp::exp2_fast(x.x - n); w.y += kvp::exp2_fast(x.y - n);
@@ -564,8 +566,15 @@ int attend(const AttnArgs& a, cudaStream_t st) {
 }
 
 struct AttnLayout {
-  size_t status, plan, parts, lse2, logits, total;
+  size_t status, plan, parts, lse2, logits, pr_ml, pr_o, pr_q, pr_rows, total;
+  int few;               // new rows per sequence up to which the kernels of this file take it
+  bool any_few, any_many;
+  KvPromptScratch prompt;
 };
+
+// Rows (new tokens x heads of a group) of one kv head up to which a sequence is taken here; with more, its
+// products fill the tensor core's tiles of 128 rows.
+constexpr int kFewRows = 32;
 
 int row_tiles_of(const KvShape& sh, int max_new) { return max_new * sh.group <= 16 ? 1 : 2; }     // MT
 
@@ -578,28 +587,33 @@ AttnLayout attention_layout(const KvShape& sh, int batch, int64_t m, int max_new
     if (kDebugBuild) { if (guards != nullptr) guards->guard[guards->n_guard++] = off; off += kGuardBytes; }
     return at;
   };
-  const int rows = 16 * row_tiles_of(sh, max_new);
+  const int most_few = kFewRows / sh.group;
+  w.few = max_new < most_few ? max_new : most_few;
+  w.any_many = max_new > w.few;
+  // (with every sequence at its bound but one, that one has m - (batch - 1) * max_new rows: when even
+  // those are many, no sequence has few)
+  w.any_few = w.few > 0 && m - (int64_t)(batch - 1) * max_new <= w.few;
+  const int rows = 16 * row_tiles_of(sh, w.few);
+  const size_t few_rows = w.any_few ? (size_t)batch * w.few * sh.heads : 0;
   w.status = take(256);
   w.plan = take((size_t)((batch < AT_MAX_BATCH ? batch : AT_MAX_BATCH) + 2) * 4);
-  w.parts = take((size_t)device_sm_count() * 2 * 2 * rows * (sh.dim + 2) * 4);
-  w.lse2 = take(with_score ? (size_t)m * sh.heads * 4 : 0);
-  w.logits = take(with_score ? (size_t)m * sh.heads * round_up((size_t)max_len, 128) * 4 : 0);
+  w.parts = take(w.any_few ? (size_t)device_sm_count() * 2 * 2 * rows * (sh.dim + 2) * 4 : 0);
+  w.lse2 = take(with_score ? few_rows * 4 : 0);
+  w.logits = take(with_score ? few_rows * round_up((size_t)max_len, 128) * 4 : 0);
+  if (w.any_many) w.prompt = kv_prompt_scratch(sh, batch, m, max_len, with_score);
+  w.pr_ml = take(w.prompt.part_ml);
+  w.pr_o = take(w.prompt.part_o);
+  w.pr_q = take(w.prompt.q_image);
+  w.pr_rows = take(w.prompt.rows);
   w.total = off;
   return w;
 }
 
-}  // namespace
-
-size_t kv_attention_workspace(const KvShape& sh, int batch, int64_t m, int max_new, int max_len, bool with_score, Workspace* guards) {
-  return attention_layout(sh, batch, m, max_new, max_len, with_score, guards).total;
-}
-
-int launch_kv_attention(const KvShape& sh, const KvBatch& b, const KvAttention& at, void* workspace, int max_len, cudaStream_t st) {
-  const AttnLayout L = attention_layout(sh, b.batch, b.m, b.max_new, max_len, at.score_out != nullptr, nullptr);
-  char* base = static_cast<char*>(workspace);
+int launch_few(const KvShape& sh, const KvBatch& b, const KvAttention& at, const AttnLayout& L, char* base, int max_len, cudaStream_t st) {
   AttnArgs a{};
   a.sh = sh;
   a.kb = b;
+  a.kb.max_new = a.kb.n_hi = L.few;
   a.at = at;
   a.status = reinterpret_cast<int*>(base + L.status);
   a.plan = reinterpret_cast<uint32_t*>(base + L.plan);
@@ -607,9 +621,9 @@ int launch_kv_attention(const KvShape& sh, const KvBatch& b, const KvAttention& 
   a.lse2 = at.score_out != nullptr ? reinterpret_cast<float*>(base + L.lse2) : nullptr;
   a.logits = at.score_out != nullptr ? reinterpret_cast<float*>(base + L.logits) : nullptr;
   a.logit_stride = (long long)round_up((size_t)max_len, 128);
-  const int mt = row_tiles_of(sh, b.max_new), tok = sh.dim == 128 ? 64 : 128;
+  const int mt = row_tiles_of(sh, L.few), tok = sh.dim == 128 ? 64 : 128;
   const long long tiles = b.max_len > 0 ? (b.max_len + tok - 1) / tok : 1;
-  const long long per_seq = tiles * sh.kv_heads * ((b.max_new * (long long)sh.group + 16 * mt - 1) / (16 * mt));
+  const long long per_seq = tiles * sh.kv_heads * ((L.few * (long long)sh.group + 16 * mt - 1) / (16 * mt));
   if (per_seq > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
   // sequences of one launch: their plan fits shared memory and their units 31 bits
   const long long fit = 0x7fffffffll / per_seq;
@@ -628,6 +642,25 @@ int launch_kv_attention(const KvShape& sh, const KvBatch& b, const KvAttention& 
     if (r != QALORA_OK) return r;
   }
   return QALORA_OK;
+}
+
+}  // namespace
+
+size_t kv_attention_workspace(const KvShape& sh, int batch, int64_t m, int max_new, int max_len, bool with_score, Workspace* guards) {
+  return attention_layout(sh, batch, m, max_new, max_len, with_score, guards).total;
+}
+
+int launch_kv_attention(const KvShape& sh, const KvBatch& b, const KvAttention& at, void* workspace, int max_len, cudaStream_t st) {
+  const AttnLayout L = attention_layout(sh, b.batch, b.m, b.max_new, max_len, at.score_out != nullptr, nullptr);
+  char* base = static_cast<char*>(workspace);
+  if (!L.any_few && cudaMemsetAsync(base + L.status, 0, sizeof(int), st) != cudaSuccess) return QALORA_ERR_CUDA;
+  int r = L.any_few ? launch_few(sh, b, at, L, base, max_len, st) : QALORA_OK;
+  if (r != QALORA_OK || !L.any_many) return r;
+  KvBatch many = b;
+  many.n_lo = L.few + 1;
+  return launch_kv_prompt(sh, many, at, L.prompt, reinterpret_cast<float2*>(base + L.pr_ml), reinterpret_cast<float*>(base + L.pr_o),
+                          reinterpret_cast<uint8_t*>(base + L.pr_q), reinterpret_cast<float2*>(base + L.pr_rows),
+                          reinterpret_cast<int*>(base + L.status), st);
 }
 
 }  // namespace qalora

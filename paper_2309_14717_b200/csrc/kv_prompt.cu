@@ -1,0 +1,707 @@
+// Attention of many new tokens over the 8-bit key/value cache (a prompt, or the next piece of one) on
+// the 5th-generation tensor cores, and the weights that its cached tokens gather.
+#define QALORA_TU 14
+#include "kv.cuh"
+#include "kv_ptx.cuh"
+
+namespace qalora {
+
+namespace {
+
+constexpr int PT_THREADS = 512;               // 2 x 128 softmax, 128 conversion, 2 issuing warps (and 2 idle ones)
+constexpr int PT_TOK = 128, PT_ROWS = 128;    // a tile: tokens x rows (new tokens x heads of a group)
+constexpr int PT_RING = 8;                    // tiles whose scales are kept; the conversion is at most 3 tiles ahead
+constexpr int PT_RING_FLOATS = 32;            // ks[8], log2 of vs / ref [8], ref / vs [8], ref_before / ref, ref
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNoMax = -1e30f;
+constexpr float kGrow = 6.f, kLift = 8.f;     // as in the few-row kernel: weights at most 2^14 in fp16
+constexpr float kTiny = 1e-37f;               // stands for a smaller factor of a score (|score| < 2^30): keeps 0 * -inf away
+constexpr float kLeastValueScale = 9.094947e-13f;   // 2^-40 of the largest one met so far: below it a block's values count as 0
+
+struct PromptArgs {
+  KvShape sh;
+  KvBatch kb;
+  KvAttention at;
+  int splits;
+  long long slots;
+  float2* part_ml;       // [splits][kv_heads * slots * 128]
+  float* part_o;         // [splits][kv_heads * slots * 128][D]
+  uint8_t* q_image;      // [kv_heads * slots][128 * D * 2]
+  float2* rows;          // [kv_heads * slots * 128] {factor of a score, log2 of the row's sum}
+  int* status;
+};
+
+// Slot of the first row tile of sequence b (of every kv head): rows of 128 that no other sequence uses.
+__device__ __forceinline__ long long first_slot(const KvShape& sh, const KvSeq& s, int b) {
+  return (long long)s.row0 * sh.group / PT_ROWS + b;
+}
+
+template <int D>
+struct PtSmem {
+  static constexpr int TILE = 128 * D * 2;                    // bytes of an fp16 tile
+  static constexpr int OFF_Q = 0;                             // two row tiles
+  static constexpr int OFF_K = 2 * TILE, OFF_V = 4 * TILE;    // two stages each
+  static constexpr int OFF_RING = 6 * TILE;
+  static constexpr int OFF_BARS = OFF_RING + PT_RING * PT_RING_FLOATS * 4;
+  static constexpr int NBARS = 1 + 4 * 2 + 3 * 2;
+  static constexpr int OFF_SLOT = OFF_BARS + NBARS * 8 + 8;
+  static constexpr int TOTAL = OFF_SLOT + 16 + 1024;
+};
+
+// 16 codes to fp16 and into row `row`, 16-byte chunks 2 * piece and 2 * piece + 1, of a tile of [128][64]
+// blocks with 128-byte swizzle.  With 128 channels half of the lanes store their second chunk first, so that
+// the eight lanes of a store phase hit different banks (with 64 the swizzle of the row does that).
+template <int D>
+__device__ __forceinline__ void store_codes(uint8_t* tile, int row, int piece, const uint4& c) {
+  uint4 lo, hi;
+  kvp::codes_to_half(c.x, lo.x, lo.y);
+  kvp::codes_to_half(c.y, lo.z, lo.w);
+  kvp::codes_to_half(c.z, hi.x, hi.y);
+  kvp::codes_to_half(c.w, hi.z, hi.w);
+  const int chunk = (2 * piece) & 7;
+  uint8_t* base = tile + (piece >> 2) * 16384 + row * 128;
+  const bool swap = D == 128 && piece >= 4;
+  const int first = swap ? chunk + 1 : chunk, second = swap ? chunk : chunk + 1;
+  *reinterpret_cast<uint4*>(base + ((first ^ (row & 7)) << 4)) = swap ? hi : lo;
+  *reinterpret_cast<uint4*>(base + ((second ^ (row & 7)) << 4)) = swap ? lo : hi;
+}
+
+// The codes of one 128-token tile on their way from memory: thread t of 128 holds piece t % (D / 16) of every
+// (2048 / D)-th row.  `ids`: lane l < 8 of each warp holds the block of tokens 16 l ..., or -1.
+template <int D>
+struct TileCodes {
+  static constexpr int PIECES = D / 16, ROWS = 128 / PIECES, PASSES = 128 / ROWS;
+  uint4 c[PASSES];
+  __device__ __forceinline__ void load(const KvShape& sh, const int8_t* codes, int ids, int which, int h, int t0, int len, int t) {
+    const int piece = t % PIECES, row0 = t / PIECES;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int row = p * ROWS + row0;
+      const int id = __shfl_sync(0xffffffffu, ids, row >> 4);
+      c[p] = make_uint4(0, 0, 0, 0);
+      if (id >= 0 && t0 + row < len) {
+        const long long plane = ((long long)id * 2 + which) * sh.kv_heads + h;
+        c[p] = *reinterpret_cast<const uint4*>(codes + (plane * sh.block + ((t0 + row) & (sh.block - 1))) * D + piece * 16);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(uint8_t* tile, int t) const {
+    const int piece = t % PIECES, row0 = t / PIECES;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) store_codes<D>(tile, p * ROWS + row0, piece, c[p]);
+  }
+};
+
+// Two tiles of 128 rows of one kv head against a range of its sequence's tokens, 128 at a time:
+//   conversion warps  codes of a tile -> fp16 keys (K-major) and values (MN-major) in shared memory;
+//   issuing threads   one per row tile: S = Q K^T into tensor memory, then O += P V with P in tensor memory
+//                     (a thread issues an instruction per ~110 cycles, an N = 128 step takes 64: one
+//                     thread could not keep the tensor pipe busy, two can);
+//   softmax threads   one per row: S from tensor memory, P back over S's columns.
+// While one row tile's softmax runs, the other tile's products do.  P V of a step is issued before the next
+// S of the same tile by the same thread, so S may overwrite P; and an S that has arrived means that
+// the P V before it is done, so a softmax thread may rescale O whenever it holds a new S.
+template <int D>
+__global__ void __launch_bounds__(PT_THREADS, 1)
+kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) {
+  using S = PtSmem<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t sbase = ptx::smem_u32(smem), bars = sbase + S::OFF_BARS;
+  float* ring = reinterpret_cast<float*>(smem + S::OFF_RING);
+  const uint32_t q_full = bars;
+  auto k_full = [&](int s) { return bars + 8 + 8 * s; };
+  auto k_empty = [&](int s) { return bars + 24 + 8 * s; };
+  auto v_full = [&](int s) { return bars + 40 + 8 * s; };
+  auto v_empty = [&](int s) { return bars + 56 + 8 * s; };
+  auto s_full = [&](int i) { return bars + 72 + 8 * i; };
+  auto p_full = [&](int i) { return bars + 88 + 8 * i; };
+  auto o_full = [&](int i) { return bars + 104 + 8 * i; };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::OFF_SLOT);
+  volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_SLOT + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const KvShape& sh = a.sh;
+
+  // the work of this block, the longest row tiles of the batch first
+  const int per_pair = sh.kv_heads * a.kb.batch * a.splits;
+  const int pair = pairs_max - 1 - (int)(blockIdx.x / per_pair), rest = blockIdx.x % per_pair;
+  const int split = rest % a.splits, h = (rest / a.splits) % sh.kv_heads, b = rest / (a.splits * sh.kv_heads);
+  const KvSeq s = kv_seq(a.kb, b);
+  const int rows = s.n * sh.group;                               // of this kv head
+  if (pair * 2 * PT_ROWS >= rows) return;
+  int tiles[2], first, most;                                      // token tiles that the rows of each row tile can see
+  for (int i = 0; i < 2; ++i) {
+    const int r0 = (pair * 2 + i) * PT_ROWS, last = (r0 + PT_ROWS < rows ? r0 + PT_ROWS : rows) - 1;
+    const int lim = r0 < rows ? s.first + last / sh.group : -1;
+    tiles[i] = lim < 0 ? 0 : lim / PT_TOK + 1;
+  }
+  most = tiles[0] > tiles[1] ? tiles[0] : tiles[1];
+  const int per_split = (most + a.splits - 1) / a.splits;
+  first = split * per_split;
+  int end[2];
+  for (int i = 0; i < 2; ++i) end[i] = tiles[i] < first + per_split ? tiles[i] : first + per_split;
+  const int stop = end[0] > end[1] ? end[0] : end[1], count = stop > first ? stop - first : 0;
+
+  if (threadIdx.x == 0) {
+    *flag = 0;
+    ptx::mbar_init(q_full, 8);
+    for (int x = 0; x < 2; ++x) {
+      ptx::mbar_init(k_full(x), 4);
+      ptx::mbar_init(k_empty(x), 2);
+      ptx::mbar_init(v_full(x), 4);
+      ptx::mbar_init(v_empty(x), 2);
+      ptx::mbar_init(s_full(x), 1);
+      ptx::mbar_init(p_full(x), 4);
+      ptx::mbar_init(o_full(x), 1);
+    }
+    ptx::fence_mbar_init();
+  }
+  if (warp == 12) {
+    __syncwarp();
+    ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  constexpr uint32_t COL_O = 256;                                // S (and P) of tile i at column 128 i, O at 256 + 128 i
+
+  if (warp < 8) {
+    // ------------------------------------------------------------------------------ softmax ----
+    kvp::more_registers<184>();
+    const int i = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const int r = (pair * 2 + i) * PT_ROWS + row;
+    const bool there = r < rows;
+    const int tok = s.row0 + (there ? r / sh.group : 0), head = h * sh.group + (there ? r % sh.group : 0);
+    const int limit = there ? s.first + r / sh.group : -1;
+    const int limit_lo = __reduce_min_sync(0xffffffffu, limit);
+    const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+    const uint32_t t_s = tmem + lane_base + 128 * i, t_o = tmem + lane_base + COL_O + 128 * i;
+    const long long slot = ((long long)h * a.slots + first_slot(sh, s, b) + pair * 2 + i);
+    const bool tile_there = (pair * 2 + i) * PT_ROWS < rows;
+    float factor;                                                // softmax_scale * log2(e) / (the row's power of two)
+    {
+      // the row's largest element is brought to 2^14 .. 2^15: exact in fp16 down to 2^-28 of it
+      uint32_t mx = 0;
+      const uint4* src = reinterpret_cast<const uint4*>(a.at.q + (long long)tok * a.at.q_stride + (long long)head * D);
+      const bool load = there && QALORA_CHECK(dbg, tok, a.kb.m);
+      uint4 w[D / 8];
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) {
+        w[c] = load ? src[c] : make_uint4(0, 0, 0, 0);
+        mx = __vmaxu2(mx, w[c].x & 0x7fff7fffu); mx = __vmaxu2(mx, w[c].y & 0x7fff7fffu);
+        mx = __vmaxu2(mx, w[c].z & 0x7fff7fffu); mx = __vmaxu2(mx, w[c].w & 0x7fff7fffu);
+      }
+      mx = max(mx & 0xffffu, mx >> 16);
+      int e = 268 - (int)(mx >> 7);
+      e = e > 254 ? 254 : (e < 1 ? 1 : e);
+      const float f = __uint_as_float((uint32_t)e << 23);
+      factor = a.at.softmax_scale * kLog2e * (e == 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23));
+      uint8_t* image = a.q_image != nullptr && tile_there && split == 0 ? a.q_image + slot * S::TILE : nullptr;
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) {
+        const uint32_t in[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+        uint32_t out[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          out[x] = kvp::pack_half2(__uint_as_float(in[x] << 16) * f, __uint_as_float(in[x] & 0xffff0000u) * f);
+        const int at = (c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+        const uint4 v = make_uint4(out[0], out[1], out[2], out[3]);
+        *reinterpret_cast<uint4*>(smem + S::OFF_Q + i * S::TILE + at) = v;
+        if (image != nullptr && QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) *reinterpret_cast<uint4*>(image + at) = v;
+      }
+      ptx::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(q_full);
+    }
+    float m = kNoMax, l = 0.f, ref = 0.f;
+    bool ok = true;
+#pragma unroll 1
+    for (int j = first; j < end[i]; ++j) {
+      if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(s_full(i), (j - first) & 1, flag)))) break;
+      ptx::tc_fence_after();
+      float x[128];
+      ptx::tmem_ld32(t_s, reinterpret_cast<uint32_t*>(x));
+      ptx::tmem_ld32(t_s + 32, reinterpret_cast<uint32_t*>(x) + 32);
+      ptx::tmem_ld32(t_s + 64, reinterpret_cast<uint32_t*>(x) + 64);
+      ptx::tmem_ld32(t_s + 96, reinterpret_cast<uint32_t*>(x) + 96);
+      const float* rg = ring + ((j - first) % PT_RING) * PT_RING_FLOATS;
+      float c[8], off[8];
+#pragma unroll
+      for (int g = 0; g < 8; ++g) { c[g] = fmaxf(factor * rg[g], kTiny); off[g] = rg[8 + g]; }
+      const float ref_ratio = rg[24];
+      ref = rg[25];
+      ptx::tmem_wait_ld();
+      if (j * PT_TOK + PT_TOK - 1 > limit_lo) {                  // some row of the warp does not see all of the tile
+        const int seen = limit - j * PT_TOK;
+#pragma unroll
+        for (int t = 0; t < 128; ++t) if (t > seen) x[t] = -INFINITY;
+      }
+      float top = kNoMax;
+#pragma unroll
+      for (int g = 0; g < 8; ++g) {
+        float mg = fmaxf(x[16 * g], x[16 * g + 1]);
+#pragma unroll
+        for (int t = 2; t < 16; ++t) mg = fmaxf(mg, x[16 * g + t]);
+        top = fmaxf(top, fmaf(mg, c[g], off[g]));
+      }
+      if (__any_sync(0xffffffffu, top > m + kGrow) || ref_ratio != 1.f) {   // rare: the row's maximum has grown
+        const float m_new = fmaxf(m, top), by = exp2f(m - m_new);
+        m = m_new;
+        l *= by;
+        const float scale = by * ref_ratio;
+        if (j > first) {
+#pragma unroll
+          for (int q = 0; q < D / 16; ++q) {
+            uint32_t o[16];
+            kvp::tmem_ld16(t_o + 16 * q, o);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int t = 0; t < 16; ++t) o[t] = __float_as_uint(__uint_as_float(o[t]) * scale);
+            ptx::tmem_st16(t_o + 16 * q, o);
+          }
+        }
+      }
+      const float base = kLift - m;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {                              // 32 tokens at a time
+        uint32_t pk[16];
+#pragma unroll
+        for (int g2 = 0; g2 < 2; ++g2) {
+          const int g = 2 * q + g2;
+          const float2 cc = make_float2(c[g], c[g]), oo = make_float2(off[g] + base, off[g] + base);
+          float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int t = 0; t < 8; ++t) {
+            float2 y = ptx::ffma2(make_float2(x[16 * g + 2 * t], x[16 * g + 2 * t + 1]), cc, oo);
+            y.x = kvp::exp2_fast(y.x);
+            y.y = kvp::exp2_fast(y.y);
+            sum = ptx::fadd2(sum, y);
+            pk[8 * g2 + t] = kvp::pack_half2(y.x, y.y);
+          }
+          l = fmaf(sum.x + sum.y, rg[16 + g], l);
+        }
+        ptx::tmem_st16(t_s + 16 * q, pk);
+      }
+      ptx::tmem_wait_st();
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(p_full(i));
+    }
+    const bool some = end[i] > first;
+    if (some && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(o_full(i), 0, flag));
+    ptx::tc_fence_after();
+    const bool partial = a.splits > 1;
+    const long long prow = slot * PT_ROWS + row;
+    if (a.rows != nullptr && tile_there && !partial && QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads))
+      a.rows[prow] = make_float2(factor, there && l != 0.f ? m - kLift + log2f(l) : INFINITY);
+    if (a.rows != nullptr && tile_there && partial && split == 0) a.rows[prow] = make_float2(factor, INFINITY);
+    if (partial && tile_there) {
+      const long long at = (long long)split * a.slots * sh.kv_heads * PT_ROWS + prow;
+      if (QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) a.part_ml[at] = make_float2(m, l);
+    }
+    const float inv = partial ? ref : (l == 0.f ? 0.f : ref / l);
+    const long long at = (long long)tok * sh.heads + head;
+#pragma unroll 1
+    for (int q = 0; q < D / 32; ++q) {
+      uint32_t o[32];
+      if (some && ok) {
+        ptx::tmem_ld32(t_o + 32 * q, o);
+        ptx::tmem_wait_ld();
+      } else {
+#pragma unroll
+        for (int t = 0; t < 32; ++t) o[t] = 0u;
+      }
+      float f[32];
+#pragma unroll
+      for (int t = 0; t < 32; ++t) f[t] = l == 0.f ? 0.f : __uint_as_float(o[t]) * inv;
+      if (partial) {
+        if (!tile_there || !QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) continue;
+        float4* dst = reinterpret_cast<float4*>(a.part_o + ((long long)split * a.slots * sh.kv_heads * PT_ROWS + prow) * D + 32 * q);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) dst[t] = make_float4(f[4 * t], f[4 * t + 1], f[4 * t + 2], f[4 * t + 3]);
+      } else if (there && QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) {
+        uint4* dst = reinterpret_cast<uint4*>(a.at.out + at * D + 32 * q);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          uint32_t w[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const __nv_bfloat162 two = __floats2bfloat162_rn(f[8 * t + 2 * y], f[8 * t + 2 * y + 1]);
+            w[y] = *reinterpret_cast<const uint32_t*>(&two);
+          }
+          dst[t] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+    }
+    if (!partial && there) kvp::store_lse(a.at.lse, at, nullptr, 0, m, l, kLift);
+  } else if (warp < 12) {
+    // --------------------------------------------------------------------------- conversion ----
+    kvp::fewer_registers<104>();
+    const int t = threadIdx.x - 256;
+    struct Look { int id; float ks, vs; };
+    auto look = [&](int j) {                                     // lane l < 8: block and scales of tokens 16 l ...
+      Look k{-1, 0.f, 0.f};
+      const int t0 = j * PT_TOK + lane * 16;
+      if (lane < 8 && j < stop && t0 < s.len) {
+        k.id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t0 / sh.block);
+        if (k.id >= 0) {
+          const long long plane = ((long long)k.id * 2) * sh.kv_heads + h;
+          k.ks = a.at.scales[plane];
+          k.vs = a.at.scales[plane + sh.kv_heads];
+        }
+      }
+      return k;
+    };
+    Look cur = look(first), next = look(first + 1);
+    TileCodes<D> kc, vc;
+    if (count > 0) kc.load(sh, a.at.codes, cur.id, 0, h, first * PT_TOK, s.len, t);
+    float ref = 0.f;
+    for (int it = 0; it < count; ++it) {
+      const int j = first + it, st = it & 1;
+      // value scales relative to the largest one so far; blocks far below it (or of zeros) count as zeros
+      float top = cur.vs;
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      top = fmaxf(ref, __shfl_sync(0xffffffffu, top, 0));
+      const float ratio = ref == top ? 1.f : ref / top;
+      const float rel = top > 0.f ? cur.vs / top : 0.f, least = fmaxf(rel, kLeastValueScale);
+      ref = top;
+      vc.load(sh, a.at.codes, rel >= kLeastValueScale ? cur.id : -1, 1, h, j * PT_TOK, s.len, t);
+      if (it >= 2 && !__all_sync(0xffffffffu, ptx::mbar_wait(k_empty(st), ((it >> 1) - 1) & 1, flag))) break;
+      if (warp == 8) {
+        float* rg = ring + (it % PT_RING) * PT_RING_FLOATS;
+        if (lane < 8) { rg[lane] = cur.ks; rg[8 + lane] = log2f(least); rg[16 + lane] = 1.f / least; }
+        if (lane == 8) { rg[24] = ratio; rg[25] = ref; }
+      }
+      kc.store(smem + S::OFF_K + st * S::TILE, t);
+      ptx::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(k_full(st));
+      cur = next;
+      next = look(j + 2);
+      if (it + 1 < count) kc.load(sh, a.at.codes, cur.id, 0, h, (j + 1) * PT_TOK, s.len, t);
+      if (it >= 2 && !__all_sync(0xffffffffu, ptx::mbar_wait(v_empty(st), ((it >> 1) - 1) & 1, flag))) break;
+      vc.store(smem + S::OFF_V + st * S::TILE, t);
+      ptx::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(v_full(st));
+    }
+  } else {
+    // --------------------------------------------------------------------------- MMA issuers ----
+    kvp::fewer_registers<40>();
+    if (warp < 14 && lane == 0) {
+      const int i = warp - 12;
+      constexpr uint32_t IDESC_S = kvp::idesc_f16(128, 128, false, false), IDESC_O = kvp::idesc_f16(128, D, false, true);
+      const uint32_t t_s = tmem + 128 * i, t_o = tmem + COL_O + 128 * i;
+      const uint64_t q_desc = ptx::smem_desc(sbase + S::OFF_Q + i * S::TILE, 16, 1024);
+      bool ok = count == 0 || ptx::mbar_wait(q_full, 0, flag);
+      for (int it = 0; it < count && ok; ++it) {
+        const int st = it & 1, ph = (it >> 1) & 1;
+        const bool mine = first + it < end[i];
+        if (!(ok = ptx::mbar_wait(k_full(st), ph, flag))) break;
+        if (mine) {
+          ptx::tc_fence_after();
+          const uint64_t k_desc = ptx::smem_desc(sbase + S::OFF_K + st * S::TILE, 16, 1024);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint64_t step = (uint64_t)((k >> 2) * 1024 + (k & 3) * 2);    // 16 channels; 64 to a block of 16 KiB
+            ptx::mma_ss(t_s, q_desc + step, k_desc + step, IDESC_S, k > 0 ? 1u : 0u);
+          }
+          ptx::mma_commit(s_full(i));
+          ptx::mma_commit(k_empty(st));
+        } else {
+          ptx::mbar_arrive(k_empty(st));
+        }
+        if (mine && !(ok = ptx::mbar_wait(p_full(i), it & 1, flag))) break;
+        if (!(ok = ptx::mbar_wait(v_full(st), ph, flag))) break;
+        if (mine) {
+          ptx::tc_fence_after();
+          const uint64_t v_desc = ptx::smem_desc(sbase + S::OFF_V + st * S::TILE, 16384, 1024);
+#pragma unroll
+          for (int k = 0; k < PT_TOK / 16; ++k)
+            ptx::mma_ts(t_o, t_s + 8 * k, v_desc + (uint64_t)(k * 128), IDESC_O, it > 0 || k > 0 ? 1u : 0u);
+          ptx::mma_commit(v_empty(st));
+          if (first + it + 1 == end[i]) ptx::mma_commit(o_full(i));
+        } else {
+          ptx::mbar_arrive(v_empty(st));
+        }
+      }
+    }
+    __syncwarp();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *flag != 0) *a.status = 1;
+  if (warp == 12) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem, 512);
+  }
+}
+
+// Joins the parts of each row, in the order of the tokens: D / 4 threads per row.
+template <int D>
+__global__ void __launch_bounds__(256)
+kv_prompt_join_kernel(const __grid_constant__ PromptArgs a, int row_blocks, int* dbg) {
+  constexpr int PER_ROW = D / 4, ROWS = 256 / PER_ROW;
+  const KvShape& sh = a.sh;
+  const int b = blockIdx.y, h = blockIdx.x / row_blocks;
+  const KvSeq s = kv_seq(a.kb, b);
+  const int r = (blockIdx.x % row_blocks) * ROWS + threadIdx.x / PER_ROW, d = (threadIdx.x % PER_ROW) * 4;
+  if (r >= s.n * sh.group) return;
+  const long long prow = ((long long)h * a.slots + first_slot(sh, s, b)) * PT_ROWS + r, plane = a.slots * sh.kv_heads * PT_ROWS;
+  if (!QALORA_CHECK(dbg, prow, plane)) return;
+  float m = kNoMax, l = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p = 0; p < a.splits; ++p) {
+    const float2 v = a.part_ml[p * plane + prow];
+    const float4 y = *reinterpret_cast<const float4*>(a.part_o + (p * plane + prow) * D + d);
+    const float top = fmaxf(m, v.x), b0 = exp2f(m - top), b1 = exp2f(v.x - top);
+    l = l * b0 + v.y * b1;
+    x.x = x.x * b0 + y.x * b1; x.y = x.y * b0 + y.y * b1; x.z = x.z * b0 + y.z * b1; x.w = x.w * b0 + y.w * b1;
+    m = top;
+  }
+  const long long at = (long long)(s.row0 + r / sh.group) * sh.heads + h * sh.group + r % sh.group;
+  kvp::store_row4(a.at.out + at * D + d, x, l);
+  if (d == 0) {
+    kvp::store_lse(a.at.lse, at, nullptr, 0, m, l, kLift);
+    if (a.rows != nullptr) a.rows[prow].y = l != 0.f ? m - kLift + log2f(l) : INFINITY;
+  }
+}
+
+template <int D>
+struct PsSmem {
+  static constexpr int TILE = 128 * D * 2, STAGES = 3;
+  static constexpr int OFF_K = 0, OFF_Q = TILE;
+  static constexpr int OFF_ROWS = OFF_Q + STAGES * TILE;         // [STAGES + 4][128] float2: read after the tile itself is free
+  static constexpr int NROWS = 8;
+  static constexpr int OFF_SUM = OFF_ROWS + NROWS * 128 * 8;     // [128] sums of the second half
+  static constexpr int OFF_BARS = OFF_SUM + 512;
+  static constexpr int NBARS = 1 + 2 * STAGES + 2 * 4;
+  static constexpr int OFF_SLOT = OFF_BARS + NBARS * 8 + 8;
+  static constexpr int TOTAL = OFF_SLOT + 16 + 1024;
+};
+
+// The weights that 128 tokens of one kv head gather: S^T = K Q^T with the tokens as the rows of the product, so
+// that a thread owns a token and adds up exp2(S * factor - lse) over the rows without any exchange.
+// The row tiles come as the images that kv_prompt_kernel left.  Two groups of 128 threads take the
+// row tiles in turn; four accumulators.
+template <int D>
+__global__ void __launch_bounds__(320, 1)
+kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, int* dbg) {
+  using S = PsSmem<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t sbase = ptx::smem_u32(smem), bars = sbase + S::OFF_BARS;
+  const uint32_t k_full = bars;
+  auto q_full = [&](int x) { return bars + 8 + 8 * x; };
+  auto q_empty = [&](int x) { return bars + 8 + 8 * (S::STAGES + x); };
+  auto s_full = [&](int x) { return bars + 8 + 8 * (2 * S::STAGES + x); };
+  auto s_empty = [&](int x) { return bars + 8 + 8 * (2 * S::STAGES + 4 + x); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::OFF_SLOT);
+  volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_SLOT + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const KvShape& sh = a.sh;
+  const int b = blockIdx.y, h = blockIdx.x % sh.kv_heads, j = blockIdx.x / sh.kv_heads, t0 = j * PT_TOK;
+  const KvSeq s = kv_seq(a.kb, b);
+  if (s.n == 0 || t0 >= s.len) return;
+  const int rows = s.n * sh.group, row_tiles = (rows + PT_ROWS - 1) / PT_ROWS;
+  const int rt0 = t0 > s.first ? (int)(((long long)(t0 - s.first) * sh.group) / PT_ROWS) : 0;   // the first that sees a token of the tile
+  const int count = row_tiles - rt0;
+  const long long slot0 = (long long)h * a.slots + first_slot(sh, s, b) + rt0;
+
+  if (threadIdx.x == 0) {
+    *flag = 0;
+    ptx::mbar_init(k_full, 8);
+    for (int x = 0; x < S::STAGES; ++x) { ptx::mbar_init(q_full(x), 1); ptx::mbar_init(q_empty(x), 1); }
+    for (int x = 0; x < 4; ++x) { ptx::mbar_init(s_full(x), 1); ptx::mbar_init(s_empty(x), 4); }
+    ptx::fence_mbar_init();
+  }
+  if (warp == 8) {
+    __syncwarp();
+    ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp < 8) {
+    const int half = warp >> 2, quarter = warp & 3, token = quarter * 32 + lane;
+    // keys of the tile: the first group converts rows' even passes and the second the odd ones
+    {
+      constexpr int PIECES = D / 16, ROWS = 256 / PIECES;
+      const int piece = threadIdx.x % PIECES, row0 = threadIdx.x / PIECES;
+#pragma unroll
+      for (int p = 0; p < 128 / ROWS; ++p) {
+        const int row = p * ROWS + row0, t = t0 + row;
+        uint4 c = make_uint4(0, 0, 0, 0);
+        if (t < s.len) {
+          const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t / sh.block);
+          if (id >= 0)
+            c = *reinterpret_cast<const uint4*>(a.at.codes + ((((long long)id * 2) * sh.kv_heads + h) * sh.block + (t & (sh.block - 1))) * D + piece * 16);
+        }
+        store_codes<D>(smem + S::OFF_K, row, piece, c);
+      }
+      ptx::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(k_full);
+    }
+    const int t = t0 + token;
+    const int id = t < s.len ? kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t / sh.block) : -1;
+    const float ks = id >= 0 ? a.at.scales[((long long)id * 2) * sh.kv_heads + h] : 0.f;
+    // the first row of this tile's first row tile that sees the token (rows before it are masked)
+    const long long sees = t > s.first ? (long long)(t - s.first) * sh.group - (long long)rt0 * PT_ROWS : 0;
+    float sum = 0.f;
+    bool ok = true;
+#pragma unroll 1
+    for (int it = half; it < count; it += 2) {
+      const int buf = it & 3;
+      if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(s_full(buf), (it >> 2) & 1, flag)))) break;
+      ptx::tc_fence_after();
+      const float4* rw = reinterpret_cast<const float4*>(smem + S::OFF_ROWS) + (it % S::NROWS) * 64;
+      const int skip = sees > (long long)it * PT_ROWS ? (int)(sees - (long long)it * PT_ROWS < 128 ? sees - (long long)it * PT_ROWS : 128) : 0;
+      const bool edge = __any_sync(0xffffffffu, skip > 0);
+      float part[2] = {0.f, 0.f};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t v[32];
+        ptx::tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + 128 * buf + 32 * q, v);
+        ptx::tmem_wait_ld();
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const float4 f = rw[16 * q + x];                       // {factor, lse} of two rows
+          float e0 = kvp::exp2_fast(fmaf(__uint_as_float(v[2 * x]) * ks, f.x, -f.y));
+          float e1 = kvp::exp2_fast(fmaf(__uint_as_float(v[2 * x + 1]) * ks, f.z, -f.w));
+          if (edge) {
+            if (32 * q + 2 * x < skip) e0 = 0.f;
+            if (32 * q + 2 * x + 1 < skip) e1 = 0.f;
+          }
+          part[0] += e0;
+          part[1] += e1;
+        }
+      }
+      sum += part[0] + part[1];
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(s_empty(buf));
+    }
+    float* other = reinterpret_cast<float*>(smem + S::OFF_SUM);
+    if (half == 1) other[token] = sum;
+    ptx::named_barrier(1, 256);
+    if (half == 0 && id >= 0) {
+      const long long at = ((long long)id * sh.kv_heads + h) * sh.block + (t & (sh.block - 1));
+      if (QALORA_CHECK(dbg, at, (long long)sh.num_blocks * sh.kv_heads * sh.block))
+        a.at.score_out[at] = (a.at.score_in != nullptr ? a.at.score_in[at] : 0.f) + (sum + other[token]);
+    }
+  } else if (warp == 8) {
+    if (lane == 0) {
+      constexpr uint32_t IDESC = kvp::idesc_f16(128, 128, false, false);
+      const uint64_t k_desc = ptx::smem_desc(sbase + S::OFF_K, 16, 1024);
+      bool ok = ptx::mbar_wait(k_full, 0, flag);
+      for (int it = 0; it < count && ok; ++it) {
+        const int st = it % S::STAGES, buf = it & 3;
+        if (!(ok = ptx::mbar_wait(q_full(st), (it / S::STAGES) & 1, flag))) break;
+        if (it >= 4 && !(ok = ptx::mbar_wait(s_empty(buf), ((it >> 2) - 1) & 1, flag))) break;
+        ptx::tc_fence_after();
+        const uint64_t q_desc = ptx::smem_desc(sbase + S::OFF_Q + st * S::TILE, 16, 1024);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint64_t step = (uint64_t)((k >> 2) * 1024 + (k & 3) * 2);
+          ptx::mma_ss(tmem + 128 * buf, k_desc + step, q_desc + step, IDESC, k > 0 ? 1u : 0u);
+        }
+        ptx::mma_commit(s_full(buf));
+        ptx::mma_commit(q_empty(st));
+      }
+    }
+    __syncwarp();
+  } else {
+    if (lane == 0) {
+      for (int it = 0; it < count; ++it) {
+        const int st = it % S::STAGES;
+        if (it >= S::STAGES && !ptx::mbar_wait(q_empty(st), ((it / S::STAGES) - 1) & 1, flag)) break;
+        // (the rows' entry was last read eight tiles ago: that tile's accumulator has since been handed
+        // back, or this tile's predecessor by four could not have been issued)
+        if (!QALORA_CHECK(dbg, slot0 + it, a.slots * sh.kv_heads)) break;
+        ptx::mbar_arrive_expect_tx(q_full(st), S::TILE + 1024);
+        ptx::bulk_load(sbase + S::OFF_Q + st * S::TILE, a.q_image + (slot0 + it) * S::TILE, S::TILE, q_full(st));
+        ptx::bulk_load(sbase + S::OFF_ROWS + (it % S::NROWS) * 1024, a.rows + (slot0 + it) * PT_ROWS, 1024, q_full(st));
+      }
+    }
+    __syncwarp();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *flag != 0) *a.status = 1;
+  if (warp == 8) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int D>
+int prompt(const PromptArgs& a, cudaStream_t st) {
+  static PerDeviceOnce once, once_score;
+  int ok = once.run([] {
+    return cudaFuncSetAttribute(kv_prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PtSmem<D>::TOTAL);
+  });
+  if (ok != QALORA_OK) return ok;
+  const KvShape& sh = a.sh;
+  const long long rows_max = (long long)a.kb.max_new * sh.group;
+  const int pairs = (int)((rows_max + 2 * PT_ROWS - 1) / (2 * PT_ROWS));
+  const long long blocks = (long long)pairs * sh.kv_heads * a.kb.batch * a.splits;
+  if (blocks > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
+  {
+    MainKernelProbe probe("kv_prompt_kernel", st);
+    kv_prompt_kernel<D><<<(unsigned)blocks, PT_THREADS, PtSmem<D>::TOTAL, st>>>(a, pairs, debug_words());
+  }
+  count_launch();
+  if (a.splits > 1) {
+    constexpr int ROWS = 256 / (D / 4);
+    const int row_blocks = (int)((rows_max + ROWS - 1) / ROWS);
+    if ((long long)row_blocks * sh.kv_heads > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
+    kv_prompt_join_kernel<D><<<dim3((unsigned)(row_blocks * sh.kv_heads), (unsigned)a.kb.batch), 256, 0, st>>>(a, row_blocks, debug_words());
+    count_launch();
+  }
+  if (a.at.score_out != nullptr && a.kb.max_len > 0) {
+    ok = once_score.run([] {
+      return cudaFuncSetAttribute(kv_prompt_score_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PsSmem<D>::TOTAL);
+    });
+    if (ok != QALORA_OK) return ok;
+    const int tiles = (a.kb.max_len + PT_TOK - 1) / PT_TOK;
+    if ((long long)tiles * sh.kv_heads > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
+    kv_prompt_score_kernel<D><<<dim3((unsigned)(tiles * sh.kv_heads), (unsigned)a.kb.batch), 320, PsSmem<D>::TOTAL, st>>>(a, tiles, debug_words());
+    count_launch();
+  }
+  return cuda_status(cudaGetLastError());
+}
+
+}  // namespace
+
+KvPromptScratch kv_prompt_scratch(const KvShape& sh, int batch, int64_t m, int max_len, bool with_score) {
+  KvPromptScratch s{};
+  s.slots = (long long)m * sh.group / PT_ROWS + batch;
+  // A row tile's tokens are cut into parts only where the row tiles leave multiprocessors free, and into
+  // parts of at least eight tiles (a part costs about four tiles' time: its rows go through memory in float32).
+  const long long blocks = sh.kv_heads * ((long long)m * sh.group / (2 * PT_ROWS) + 1), tiles = (max_len + PT_TOK - 1) / PT_TOK;
+  long long splits = device_sm_count() / blocks;
+  if (splits > tiles / 8) splits = tiles / 8;
+  s.splits = splits < 1 ? 1 : (int)splits;
+  const size_t rows = (size_t)s.slots * sh.kv_heads * PT_ROWS;
+  s.part_ml = s.splits > 1 ? rows * s.splits * sizeof(float2) : 0;
+  s.part_o = s.splits > 1 ? rows * s.splits * sh.dim * 4 : 0;
+  s.q_image = with_score ? rows * sh.dim * 2 : 0;
+  s.rows = with_score ? rows * sizeof(float2) : 0;
+  return s;
+}
+
+int launch_kv_prompt(const KvShape& sh, const KvBatch& b, const KvAttention& at, const KvPromptScratch& s, float2* part_ml,
+                     float* part_o, uint8_t* q_image, float2* rows, int* status, cudaStream_t st) {
+  const bool scores = at.score_out != nullptr;
+  PromptArgs a{sh, b, at, s.splits, s.slots, part_ml, part_o, scores ? q_image : nullptr, scores ? rows : nullptr, status};
+  return sh.dim == 128 ? prompt<128>(a, st) : prompt<64>(a, st);
+}
+
+}  // namespace qalora

@@ -68,13 +68,30 @@ __device__ __forceinline__ void store_row4(__nv_bfloat16* out, float4 x, float l
   w.y = *reinterpret_cast<const uint32_t*>(&b);
   *reinterpret_cast<uint2*>(out) = w;
 }
-// lse in natural logarithms for the caller, in powers of two for the gathered weights (there +infinity
-// stands for a row without tokens, so that its weights come out as zero); the sum l carries 2^lift
-__device__ __forceinline__ void store_lse(float* lse, float* lse2, long long at, float mx, float l, float lift) {
+// lse[at] in natural logarithms for the caller, lse2[own] in powers of two for the gathered weights (there
+// +infinity stands for a row without tokens, so that its weights come out as zero); the sum l carries 2^lift
+__device__ __forceinline__ void store_lse(float* lse, long long at, float* lse2, long long own, float mx, float l, float lift) {
   const float v = mx - lift + log2f(l);
   if (lse != nullptr) lse[at] = l == 0.f ? -INFINITY : v * 0.6931471805599453f;
-  if (lse2 != nullptr) lse2[at] = l == 0.f ? INFINITY : v;
+  if (lse2 != nullptr) lse2[own] = l == 0.f ? INFINITY : v;
 }
+
+// ---- tensor memory ----
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
+      : "memory");
+}
+// Instruction descriptor of kind::f16 with fp16 operands and float32 accumulation.
+__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool a_mn_major, bool b_mn_major) {
+  return (1u << 4) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(m >> 4) << 24);
+}
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 }  // namespace kvp
 }  // namespace qalora
