@@ -8,10 +8,13 @@ namespace qalora {
 
 namespace {
 
-constexpr int PT_THREADS = 512;               // 2 x 128 softmax, 128 conversion, 2 issuing warps (and 2 idle ones)
+constexpr int PT_CONV = 8;                     // conversion warps
+constexpr int PT_THREADS = 256 + PT_CONV * 32 + 128;   // 2 x 128 softmax, conversion, 2 issuing warps (and 2 idle ones)
+constexpr int PT_ISSUE = 8 + PT_CONV;          // first issuing warp
 constexpr int PT_TOK = 128, PT_ROWS = 128;    // a tile: tokens x rows (new tokens x heads of a group)
-constexpr int PT_RING = 8;                    // tiles whose scales are kept; the conversion is at most 3 tiles ahead
-constexpr int PT_RING_FLOATS = 32;            // ks[8], log2 of vs / ref [8], ref / vs [8], ref_before / ref, ref
+constexpr int PT_RING = 8;                    // tiles whose blocks and scales are kept
+constexpr int PT_RING_FLOATS = 48;            // ks[8], log2 of vs / ref [8], ref / vs [8], {ref_before / ref, ref, all there}, blocks of
+                                              // keys [8] at 32 and of values [8] at 40
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoMax = -1e30f;
 constexpr float kGrow = 6.f, kLift = 8.f;     // as in the few-row kernel: weights at most 2^14 in fp16
@@ -43,15 +46,13 @@ struct PtSmem {
   static constexpr int OFF_K = 2 * TILE, OFF_V = 4 * TILE;    // two stages each
   static constexpr int OFF_RING = 6 * TILE;
   static constexpr int OFF_BARS = OFF_RING + PT_RING * PT_RING_FLOATS * 4;
-  static constexpr int NBARS = 1 + 4 * 2 + 3 * 2;
+  static constexpr int NBARS = 1 + 4 * 2 + 4 * 2 + 2 * PT_RING;
   static constexpr int OFF_SLOT = OFF_BARS + NBARS * 8 + 8;
   static constexpr int TOTAL = OFF_SLOT + 16 + 1024;
 };
 
 // 16 codes to fp16 and into row `row`, 16-byte chunks 2 * piece and 2 * piece + 1, of a tile of [128][64]
-// blocks with 128-byte swizzle.  With 128 channels half of the lanes store their second chunk first, so that
-// the eight lanes of a store phase hit different banks (with 64 the swizzle of the row does that).
-template <int D>
+// blocks with 128-byte swizzle.
 __device__ __forceinline__ void store_codes(uint8_t* tile, int row, int piece, const uint4& c) {
   uint4 lo, hi;
   kvp::codes_to_half(c.x, lo.x, lo.y);
@@ -60,37 +61,138 @@ __device__ __forceinline__ void store_codes(uint8_t* tile, int row, int piece, c
   kvp::codes_to_half(c.w, hi.z, hi.w);
   const int chunk = (2 * piece) & 7;
   uint8_t* base = tile + (piece >> 2) * 16384 + row * 128;
-  const bool swap = D == 128 && piece >= 4;
-  const int first = swap ? chunk + 1 : chunk, second = swap ? chunk : chunk + 1;
-  *reinterpret_cast<uint4*>(base + ((first ^ (row & 7)) << 4)) = swap ? hi : lo;
-  *reinterpret_cast<uint4*>(base + ((second ^ (row & 7)) << 4)) = swap ? lo : hi;
+  *reinterpret_cast<uint4*>(base + ((chunk ^ (row & 7)) << 4)) = lo;
+  *reinterpret_cast<uint4*>(base + (((chunk + 1) ^ (row & 7)) << 4)) = hi;
 }
 
-// The codes of one 128-token tile on their way from memory: thread t of 128 holds piece t % (D / 16) of every
-// (2048 / D)-th row.  `ids`: lane l < 8 of each warp holds the block of tokens 16 l ..., or -1.
+// Which 16 codes of every pass over a tile thread t of `THREADS` takes: eight neighbouring lanes hold four pieces of
+// an even and of an odd row, whose swizzled chunks lie in different banks.
+template <int D, int THREADS>
+struct TileMap {
+  static constexpr int PIECES = D / 16, ROWS = THREADS / PIECES, PASSES = 128 / ROWS;
+  int piece, row0;
+  __device__ __forceinline__ explicit TileMap(int t)
+      : piece(D == 128 ? (t & 3) | ((t >> 3) & 1) << 2 : t & 3), row0(D == 128 ? ((t >> 2) & 1) | (t >> 4) << 1 : t >> 2) {}
+};
+
+// The codes of one 128-token tile on their way from memory.
 template <int D>
 struct TileCodes {
-  static constexpr int PIECES = D / 16, ROWS = 128 / PIECES, PASSES = 128 / ROWS;
-  uint4 c[PASSES];
-  __device__ __forceinline__ void load(const KvShape& sh, const int8_t* codes, int ids, int which, int h, int t0, int len, int t) {
-    const int piece = t % PIECES, row0 = t / PIECES;
+  using Map = TileMap<D, PT_CONV * 32>;
+  uint4 c[Map::PASSES];
+  // `src`: this head's keys (or values) of block 0, at this thread's piece; `ids`: the blocks of the tile's groups of
+  // 16 tokens.  Blocks that are not there are read at block 0: a load under a condition, or a select behind
+  // it, would make the thread wait for it here.
+  __device__ __forceinline__ void load(const int8_t* src, long long block_bytes, int block, const int* ids, const Map& map) {
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      const int row = p * ROWS + row0;
-      const int id = __shfl_sync(0xffffffffu, ids, row >> 4);
-      c[p] = make_uint4(0, 0, 0, 0);
-      if (id >= 0 && t0 + row < len) {
-        const long long plane = ((long long)id * 2 + which) * sh.kv_heads + h;
-        c[p] = *reinterpret_cast<const uint4*>(codes + (plane * sh.block + ((t0 + row) & (sh.block - 1))) * D + piece * 16);
-      }
+    for (int p = 0; p < Map::PASSES; ++p) {
+      const int row = p * Map::ROWS + map.row0, id = ids[row >> 4];
+      c[p] = *reinterpret_cast<const uint4*>(src + (id < 0 ? 0 : id) * block_bytes + (row & (block - 1)) * D);
     }
   }
-  __device__ __forceinline__ void store(uint8_t* tile, int t) const {
-    const int piece = t % PIECES, row0 = t / PIECES;
+  // unless all of the tile is there, rows from `rows` on and those of blocks that are not there become zeros
+  __device__ __forceinline__ void store(uint8_t* tile, bool all, const int* ids, int rows, const Map& map) const {
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) store_codes<D>(tile, p * ROWS + row0, piece, c[p]);
+    for (int p = 0; p < Map::PASSES; ++p) {
+      const int row = p * Map::ROWS + map.row0;
+      uint4 v = c[p];
+      if (!all && (row >= rows || ids[row >> 4] < 0)) v = make_uint4(0, 0, 0, 0);
+      store_codes(tile, row, map.piece, v);
+    }
   }
 };
+
+// A softmax thread's row.
+struct SoftmaxRow {
+  float factor;            // softmax_scale * log2(e) / (the row's power of two)
+  float m, l;              // running maximum of score + log2 of the relative value scale, in powers of two; sum
+  float ref;               // value scale that the outputs are relative to
+};
+
+struct TileScales {
+  float c[8], off[8], inv[8];    // of 16 tokens each: factor of a score, log2 of the relative value scale, its inverse
+};
+
+// First look at a tile of S (t_s: 128 columns of this thread's lane): whether a row's maximum has grown by 2^kGrow or
+// more, or the values' reference has changed (rare; and always on the first tile); the maximum and the outputs are
+// then brought up to date.  EDGE: columns beyond `seen` are masked.
+template <int D, bool EDGE>
+__device__ __forceinline__ void softmax_settle(SoftmaxRow& w, const TileScales& sc, float ref_ratio, uint32_t t_s, uint32_t t_o, int seen, bool first) {
+  float top = kNoMax;
+  float x[2][32];
+  ptx::tmem_ld32(t_s, reinterpret_cast<uint32_t*>(x[0]));
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    ptx::tmem_wait_ld();
+    if (q < 3) ptx::tmem_ld32(t_s + 32 * (q + 1), reinterpret_cast<uint32_t*>(x[(q + 1) & 1]));
+    float* v = x[q & 1];
+    if (EDGE) {
+#pragma unroll
+      for (int t = 0; t < 32; ++t) if (32 * q + t > seen) v[t] = -INFINITY;
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float a = fmaxf(v[16 * g], v[16 * g + 1]), b = fmaxf(v[16 * g + 2], v[16 * g + 3]);
+#pragma unroll
+      for (int t = 4; t < 16; t += 4) {
+        a = kvp::max3(a, v[16 * g + t], v[16 * g + t + 1]);
+        b = kvp::max3(b, v[16 * g + t + 2], v[16 * g + t + 3]);
+      }
+      top = fmaxf(top, fmaf(fmaxf(a, b), sc.c[2 * q + g], sc.off[2 * q + g]));
+    }
+  }
+  if (!__any_sync(0xffffffffu, top > w.m + kGrow) && ref_ratio == 1.f) return;
+  top = fmaxf(top, w.m);
+  const float by = exp2f(w.m - top), scale = by * ref_ratio;
+  w.m = top;
+  w.l *= by;
+  if (first) return;
+#pragma unroll 1
+  for (int q = 0; q < D / 16; ++q) {
+    uint32_t o[16];
+    kvp::tmem_ld16(t_o + 16 * q, o);
+    ptx::tmem_wait_ld();
+#pragma unroll
+    for (int t = 0; t < 16; ++t) o[t] = __float_as_uint(__uint_as_float(o[t]) * scale);
+    ptx::tmem_st16(t_o + 16 * q, o);
+  }
+}
+
+// S to P, over columns of S that have been read: 32 columns at a time with the next 32 on their way.
+template <bool EDGE>
+__device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const TileScales& sc, uint32_t t_s, int seen) {
+  const float base = kLift - w.m;
+  float x[2][32];
+  ptx::tmem_ld32(t_s, reinterpret_cast<uint32_t*>(x[0]));
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    ptx::tmem_wait_ld();
+    if (q < 3) ptx::tmem_ld32(t_s + 32 * (q + 1), reinterpret_cast<uint32_t*>(x[(q + 1) & 1]));
+    const float* v = x[q & 1];
+    uint32_t pk[16];
+#pragma unroll
+    for (int g2 = 0; g2 < 2; ++g2) {
+      const int g = 2 * q + g2;
+      const float off = sc.off[g] + base;
+      const float2 cc = make_float2(sc.c[g], sc.c[g]), oo = make_float2(off, off);
+      float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        float2 y = ptx::ffma2(make_float2(v[16 * g2 + 2 * t], v[16 * g2 + 2 * t + 1]), cc, oo);
+        if (EDGE) {
+          if (16 * g + 2 * t > seen) y.x = -INFINITY;
+          if (16 * g + 2 * t + 1 > seen) y.y = -INFINITY;
+        }
+        y.x = kvp::exp2_fast(y.x);
+        y.y = kvp::exp2_fast(y.y);
+        sum = ptx::fadd2(sum, y);
+        pk[8 * g2 + t] = kvp::pack_half2(y.x, y.y);
+      }
+      w.l = fmaf(sum.x + sum.y, sc.inv[g], w.l);
+    }
+    ptx::tmem_st16(t_s + 16 * q, pk);
+  }
+}
 
 // Two tiles of 128 rows of one kv head against a range of its sequence's tokens, 128 at a time:
 //   conversion warps  codes of a tile -> fp16 keys (K-major) and values (MN-major) in shared memory;
@@ -117,6 +219,9 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
   auto s_full = [&](int i) { return bars + 72 + 8 * i; };
   auto p_full = [&](int i) { return bars + 88 + 8 * i; };
   auto o_full = [&](int i) { return bars + 104 + 8 * i; };
+  auto turn = [&](int i) { return bars + 120 + 8 * i; };
+  auto r_full = [&](int x) { return bars + 136 + 8 * x; };              // blocks and scales of a tile are there
+  auto r_used = [&](int x) { return bars + 136 + 8 * (PT_RING + x); };  // its codes have been converted
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::OFF_SLOT);
   volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_SLOT + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -146,17 +251,19 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
     *flag = 0;
     ptx::mbar_init(q_full, 8);
     for (int x = 0; x < 2; ++x) {
-      ptx::mbar_init(k_full(x), 4);
+      ptx::mbar_init(k_full(x), PT_CONV);
       ptx::mbar_init(k_empty(x), 2);
-      ptx::mbar_init(v_full(x), 4);
+      ptx::mbar_init(v_full(x), PT_CONV);
       ptx::mbar_init(v_empty(x), 2);
       ptx::mbar_init(s_full(x), 1);
       ptx::mbar_init(p_full(x), 4);
       ptx::mbar_init(o_full(x), 1);
+      ptx::mbar_init(turn(x), 4);
     }
+    for (int x = 0; x < PT_RING; ++x) { ptx::mbar_init(r_full(x), 1); ptx::mbar_init(r_used(x), PT_CONV); }
     ptx::fence_mbar_init();
   }
-  if (warp == 12) {
+  if (warp == PT_ISSUE) {
     __syncwarp();
     ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
     ptx::tmem_relinquish();
@@ -169,7 +276,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
 
   if (warp < 8) {
     // ------------------------------------------------------------------------------ softmax ----
-    kvp::more_registers<184>();
+    kvp::more_registers<152>();
     const int i = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
     const int r = (pair * 2 + i) * PT_ROWS + row;
     const bool there = r < rows;
@@ -215,80 +322,42 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(q_full);
     }
-    float m = kNoMax, l = 0.f, ref = 0.f;
+    SoftmaxRow w{factor, kNoMax, 0.f, 0.f};
     bool ok = true;
+    // whole tiles first, then the ones that some row of the warp does not see all of
+    const int whole = (limit_lo + 1) / PT_TOK < end[i] ? (limit_lo + 1) / PT_TOK : end[i];
 #pragma unroll 1
     for (int j = first; j < end[i]; ++j) {
-      if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(s_full(i), (j - first) & 1, flag)))) break;
+      const int step = j - first, others = end[1 - i] - first;
+      if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(s_full(i), step & 1, flag)))) break;
       ptx::tc_fence_after();
-      float x[128];
-      ptx::tmem_ld32(t_s, reinterpret_cast<uint32_t*>(x));
-      ptx::tmem_ld32(t_s + 32, reinterpret_cast<uint32_t*>(x) + 32);
-      ptx::tmem_ld32(t_s + 64, reinterpret_cast<uint32_t*>(x) + 64);
-      ptx::tmem_ld32(t_s + 96, reinterpret_cast<uint32_t*>(x) + 96);
-      const float* rg = ring + ((j - first) % PT_RING) * PT_RING_FLOATS;
-      float c[8], off[8];
+      const float4* rg = reinterpret_cast<const float4*>(ring + (step % PT_RING) * PT_RING_FLOATS);
+      TileScales sc;
 #pragma unroll
-      for (int g = 0; g < 8; ++g) { c[g] = fmaxf(factor * rg[g], kTiny); off[g] = rg[8 + g]; }
-      const float ref_ratio = rg[24];
-      ref = rg[25];
-      ptx::tmem_wait_ld();
-      if (j * PT_TOK + PT_TOK - 1 > limit_lo) {                  // some row of the warp does not see all of the tile
-        const int seen = limit - j * PT_TOK;
-#pragma unroll
-        for (int t = 0; t < 128; ++t) if (t > seen) x[t] = -INFINITY;
+      for (int g = 0; g < 2; ++g) {
+        const float4 k = rg[g], o = rg[2 + g], v = rg[4 + g];
+        sc.c[4 * g] = fmaxf(factor * k.x, kTiny); sc.c[4 * g + 1] = fmaxf(factor * k.y, kTiny);
+        sc.c[4 * g + 2] = fmaxf(factor * k.z, kTiny); sc.c[4 * g + 3] = fmaxf(factor * k.w, kTiny);
+        sc.off[4 * g] = o.x; sc.off[4 * g + 1] = o.y; sc.off[4 * g + 2] = o.z; sc.off[4 * g + 3] = o.w;
+        sc.inv[4 * g] = v.x; sc.inv[4 * g + 1] = v.y; sc.inv[4 * g + 2] = v.z; sc.inv[4 * g + 3] = v.w;
       }
-      float top = kNoMax;
-#pragma unroll
-      for (int g = 0; g < 8; ++g) {
-        float mg = fmaxf(x[16 * g], x[16 * g + 1]);
-#pragma unroll
-        for (int t = 2; t < 16; ++t) mg = fmaxf(mg, x[16 * g + t]);
-        top = fmaxf(top, fmaf(mg, c[g], off[g]));
-      }
-      if (__any_sync(0xffffffffu, top > m + kGrow) || ref_ratio != 1.f) {   // rare: the row's maximum has grown
-        const float m_new = fmaxf(m, top), by = exp2f(m - m_new);
-        m = m_new;
-        l *= by;
-        const float scale = by * ref_ratio;
-        if (j > first) {
-#pragma unroll
-          for (int q = 0; q < D / 16; ++q) {
-            uint32_t o[16];
-            kvp::tmem_ld16(t_o + 16 * q, o);
-            ptx::tmem_wait_ld();
-#pragma unroll
-            for (int t = 0; t < 16; ++t) o[t] = __float_as_uint(__uint_as_float(o[t]) * scale);
-            ptx::tmem_st16(t_o + 16 * q, o);
-          }
-        }
-      }
-      const float base = kLift - m;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {                              // 32 tokens at a time
-        uint32_t pk[16];
-#pragma unroll
-        for (int g2 = 0; g2 < 2; ++g2) {
-          const int g = 2 * q + g2;
-          const float2 cc = make_float2(c[g], c[g]), oo = make_float2(off[g] + base, off[g] + base);
-          float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-          for (int t = 0; t < 8; ++t) {
-            float2 y = ptx::ffma2(make_float2(x[16 * g + 2 * t], x[16 * g + 2 * t + 1]), cc, oo);
-            y.x = kvp::exp2_fast(y.x);
-            y.y = kvp::exp2_fast(y.y);
-            sum = ptx::fadd2(sum, y);
-            pk[8 * g2 + t] = kvp::pack_half2(y.x, y.y);
-          }
-          l = fmaf(sum.x + sum.y, rg[16 + g], l);
-        }
-        ptx::tmem_st16(t_s + 16 * q, pk);
-      }
+      const float4 rr = rg[6];                                    // {reference before / now, reference now}
+      w.ref = rr.y;
+      if (j < whole) softmax_settle<D, false>(w, sc, rr.x, t_s, t_o, 0, step == 0);
+      else softmax_settle<D, true>(w, sc, rr.x, t_s, t_o, limit - j * PT_TOK, step == 0);
+      // The two row tiles' exponentials take turns: side by side they would share the exponential unit and then the
+      // tensor core, each idle while the other works.  (Waits only for a step that the other tile has.)
+      if (i == 0 ? step >= 1 && step - 1 < others : step < others)
+        if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(turn(i), (i == 0 ? step - 1 : step) & 1, flag)))) break;
+      if (j < whole) softmax_exp<false>(w, sc, t_s, 0);
+      else softmax_exp<true>(w, sc, t_s, limit - j * PT_TOK);
+      if (lane == 0) ptx::mbar_arrive(turn(1 - i));
       ptx::tmem_wait_st();
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(p_full(i));
     }
+    const float m = w.m, l = w.l, ref = w.ref;
     const bool some = end[i] > first;
     if (some && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(o_full(i), 0, flag));
     ptx::tc_fence_after();
@@ -336,97 +405,128 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       }
     }
     if (!partial && there) kvp::store_lse(a.at.lse, at, nullptr, 0, m, l, kLift);
-  } else if (warp < 12) {
+  } else if (warp < PT_ISSUE) {
     // --------------------------------------------------------------------------- conversion ----
-    kvp::fewer_registers<104>();
-    const int t = threadIdx.x - 256;
-    struct Look { int id; float ks, vs; };
-    auto look = [&](int j) {                                     // lane l < 8: block and scales of tokens 16 l ...
-      Look k{-1, 0.f, 0.f};
-      const int t0 = j * PT_TOK + lane * 16;
-      if (lane < 8 && j < stop && t0 < s.len) {
-        k.id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t0 / sh.block);
-        if (k.id >= 0) {
-          const long long plane = ((long long)k.id * 2) * sh.kv_heads + h;
-          k.ks = a.at.scales[plane];
-          k.vs = a.at.scales[plane + sh.kv_heads];
-        }
-      }
-      return k;
-    };
-    Look cur = look(first), next = look(first + 1);
+    kvp::fewer_registers<64>();
+    const TileMap<D, PT_CONV * 32> map(threadIdx.x - 256);
+    const long long block_bytes = 2ll * sh.kv_heads * sh.block * D;
+    const int8_t* k_src = a.at.codes + (long long)h * sh.block * D + map.piece * 16;
+    const int8_t* v_src = k_src + (long long)sh.kv_heads * sh.block * D;
+    auto ring_ids = [&](int it) { return reinterpret_cast<const int*>(ring + (it % PT_RING) * PT_RING_FLOATS) + 32; };
+    auto known = [&](int it) { return __all_sync(0xffffffffu, ptx::mbar_wait(r_full(it % PT_RING), (it / PT_RING) & 1, flag)); };
     TileCodes<D> kc, vc;
-    if (count > 0) kc.load(sh, a.at.codes, cur.id, 0, h, first * PT_TOK, s.len, t);
-    float ref = 0.f;
-    for (int it = 0; it < count; ++it) {
-      const int j = first + it, st = it & 1;
-      // value scales relative to the largest one so far; blocks far below it (or of zeros) count as zeros
-      float top = cur.vs;
-#pragma unroll
-      for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      top = fmaxf(ref, __shfl_sync(0xffffffffu, top, 0));
-      const float ratio = ref == top ? 1.f : ref / top;
-      const float rel = top > 0.f ? cur.vs / top : 0.f, least = fmaxf(rel, kLeastValueScale);
-      ref = top;
-      vc.load(sh, a.at.codes, rel >= kLeastValueScale ? cur.id : -1, 1, h, j * PT_TOK, s.len, t);
+    bool ok = count == 0 || known(0);
+    if (count > 0 && ok) kc.load(k_src, block_bytes, sh.block, ring_ids(0), map);
+    for (int it = 0; it < count && ok; ++it) {
+      const int st = it & 1, rows_here = s.len - (first + it) * PT_TOK;
+      const int* ids = ring_ids(it);
+      const bool all = ids[-6] != 0;
+      vc.load(v_src, block_bytes, sh.block, ids + 8, map);
       if (it >= 2 && !__all_sync(0xffffffffu, ptx::mbar_wait(k_empty(st), ((it >> 1) - 1) & 1, flag))) break;
-      if (warp == 8) {
-        float* rg = ring + (it % PT_RING) * PT_RING_FLOATS;
-        if (lane < 8) { rg[lane] = cur.ks; rg[8 + lane] = log2f(least); rg[16 + lane] = 1.f / least; }
-        if (lane == 8) { rg[24] = ratio; rg[25] = ref; }
-      }
-      kc.store(smem + S::OFF_K + st * S::TILE, t);
+      kc.store(smem + S::OFF_K + st * S::TILE, all, ids, rows_here, map);
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(k_full(st));
-      cur = next;
-      next = look(j + 2);
-      if (it + 1 < count) kc.load(sh, a.at.codes, cur.id, 0, h, (j + 1) * PT_TOK, s.len, t);
+      if (it + 1 < count) {
+        if (!(ok = known(it + 1))) break;
+        kc.load(k_src, block_bytes, sh.block, ring_ids(it + 1), map);
+      }
       if (it >= 2 && !__all_sync(0xffffffffu, ptx::mbar_wait(v_empty(st), ((it >> 1) - 1) & 1, flag))) break;
-      vc.store(smem + S::OFF_V + st * S::TILE, t);
+      vc.store(smem + S::OFF_V + st * S::TILE, all, ids + 8, rows_here, map);
       ptx::fence_proxy_async();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(v_full(st));
+      if (lane == 0) { ptx::mbar_arrive(v_full(st)); ptx::mbar_arrive(r_used(it % PT_RING)); }
     }
   } else {
     // --------------------------------------------------------------------------- MMA issuers ----
-    kvp::fewer_registers<40>();
-    if (warp < 14 && lane == 0) {
-      const int i = warp - 12;
+    kvp::fewer_registers<48>();
+    const int i = __shfl_sync(0xffffffffu, warp, 0) - PT_ISSUE;
+    if (i < 2) {
+      const uint32_t leader = kvp::elect_one();
       constexpr uint32_t IDESC_S = kvp::idesc_f16(128, 128, false, false), IDESC_O = kvp::idesc_f16(128, D, false, true);
       const uint32_t t_s = tmem + 128 * i, t_o = tmem + COL_O + 128 * i;
       const uint64_t q_desc = ptx::smem_desc(sbase + S::OFF_Q + i * S::TILE, 16, 1024);
-      bool ok = count == 0 || ptx::mbar_wait(q_full, 0, flag);
+      auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, flag)); };
+      bool ok = count == 0 || wait(q_full, 0);
       for (int it = 0; it < count && ok; ++it) {
         const int st = it & 1, ph = (it >> 1) & 1;
         const bool mine = first + it < end[i];
-        if (!(ok = ptx::mbar_wait(k_full(st), ph, flag))) break;
+        if (!(ok = wait(k_full(st), ph))) break;
         if (mine) {
           ptx::tc_fence_after();
           const uint64_t k_desc = ptx::smem_desc(sbase + S::OFF_K + st * S::TILE, 16, 1024);
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
             const uint64_t step = (uint64_t)((k >> 2) * 1024 + (k & 3) * 2);    // 16 channels; 64 to a block of 16 KiB
-            ptx::mma_ss(t_s, q_desc + step, k_desc + step, IDESC_S, k > 0 ? 1u : 0u);
+            kvp::mma_ss(leader, t_s, q_desc + step, k_desc + step, IDESC_S, k > 0 ? 1u : 0u);
           }
-          ptx::mma_commit(s_full(i));
-          ptx::mma_commit(k_empty(st));
-        } else {
+          kvp::mma_commit(leader, s_full(i));
+          kvp::mma_commit(leader, k_empty(st));
+        } else if (leader) {
           ptx::mbar_arrive(k_empty(st));
         }
-        if (mine && !(ok = ptx::mbar_wait(p_full(i), it & 1, flag))) break;
-        if (!(ok = ptx::mbar_wait(v_full(st), ph, flag))) break;
+        __syncwarp();
+        if (mine && !(ok = wait(p_full(i), it & 1))) break;
+        if (!(ok = wait(v_full(st), ph))) break;
         if (mine) {
           ptx::tc_fence_after();
           const uint64_t v_desc = ptx::smem_desc(sbase + S::OFF_V + st * S::TILE, 16384, 1024);
 #pragma unroll
           for (int k = 0; k < PT_TOK / 16; ++k)
-            ptx::mma_ts(t_o, t_s + 8 * k, v_desc + (uint64_t)(k * 128), IDESC_O, it > 0 || k > 0 ? 1u : 0u);
-          ptx::mma_commit(v_empty(st));
-          if (first + it + 1 == end[i]) ptx::mma_commit(o_full(i));
-        } else {
+            kvp::mma_ts(leader, t_o, t_s + 8 * k, v_desc + (uint64_t)(k * 128), IDESC_O, it > 0 || k > 0 ? 1u : 0u);
+          kvp::mma_commit(leader, v_empty(st));
+          if (first + it + 1 == end[i]) kvp::mma_commit(leader, o_full(i));
+        } else if (leader) {
           ptx::mbar_arrive(v_empty(st));
         }
+        __syncwarp();
+      }
+    } else if (i == 2) {
+      // ------------------------------------------------------------------------- look-ups ----
+      // lane l < 8: block and scales of tokens 16 l ... of a tile, each step of the chain table -> scales asked for one
+      // tile before it is needed
+      auto entry = [&](int it) {
+        const int t0 = (first + it) * PT_TOK + lane * 16;
+        return lane < 8 && it < count && t0 < s.len ? a.kb.table[(size_t)b * a.kb.max_blocks + t0 / sh.block] : -1;
+      };
+      struct Look { int id; float ks, vs; };
+      auto look = [&](int raw) {
+        const int id = raw >= 0 && raw < sh.num_blocks ? raw : -1;
+        const long long plane = ((long long)(id < 0 ? 0 : id) * 2) * sh.kv_heads + h;
+        return Look{id, a.at.scales[plane], a.at.scales[plane + sh.kv_heads]};
+      };
+      Look next = look(entry(0));
+      int after = entry(1);
+      float ref = 0.f;
+      for (int it = 0; it < count; ++it) {
+        const Look cur = next;
+        next = look(after);
+        after = entry(it + 2);
+        // value scales relative to the largest one so far; blocks far below it (or of zeros) count as zeros
+        const float ks = cur.id >= 0 ? cur.ks : 0.f, vs = cur.id >= 0 ? cur.vs : 0.f;
+        float top = vs;
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        top = fmaxf(ref, __shfl_sync(0xffffffffu, top, 0));
+        const float ratio = ref == top ? 1.f : ref / top;
+        const float rel = top > 0.f ? vs / top : 0.f, least = fmaxf(rel, kLeastValueScale);
+        const int v_id = rel >= kLeastValueScale ? cur.id : -1;
+        const bool all = __all_sync(0xffffffffu, lane >= 8 || v_id >= 0) && (first + it + 1) * PT_TOK <= s.len;
+        ref = top;
+        // The ring's entry is free once tile it - 4 has been converted: its values waited for P V of tile it - 6, hence
+        // for that tile's softmax, which came after the one that read this entry (tile it - 8).
+        if (it >= PT_RING && !__all_sync(0xffffffffu, ptx::mbar_wait(r_used((it - 4) % PT_RING), ((it - 4) / PT_RING) & 1, flag))) break;
+        float* rg = ring + (it % PT_RING) * PT_RING_FLOATS;
+        if (lane < 8) {
+          rg[lane] = ks;
+          rg[8 + lane] = log2f(least);
+          rg[16 + lane] = 1.f / least;
+          reinterpret_cast<int*>(rg)[32 + lane] = cur.id;
+          reinterpret_cast<int*>(rg)[40 + lane] = v_id;
+        }
+        if (lane == 8) { rg[24] = ratio; rg[25] = ref; reinterpret_cast<int*>(rg)[26] = all ? 1 : 0; }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(r_full(it % PT_RING));
       }
     }
     __syncwarp();
@@ -434,7 +534,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
   ptx::tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *flag != 0) *a.status = 1;
-  if (warp == 12) {
+  if (warp == PT_ISSUE) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem, 512);
   }
@@ -530,20 +630,19 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, in
 
   if (warp < 8) {
     const int half = warp >> 2, quarter = warp & 3, token = quarter * 32 + lane;
-    // keys of the tile: the first group converts rows' even passes and the second the odd ones
     {
-      constexpr int PIECES = D / 16, ROWS = 256 / PIECES;
-      const int piece = threadIdx.x % PIECES, row0 = threadIdx.x / PIECES;
+      using Map = TileMap<D, 256>;
+      const Map map(threadIdx.x);
 #pragma unroll
-      for (int p = 0; p < 128 / ROWS; ++p) {
-        const int row = p * ROWS + row0, t = t0 + row;
+      for (int p = 0; p < Map::PASSES; ++p) {
+        const int row = p * Map::ROWS + map.row0, t = t0 + row;
         uint4 c = make_uint4(0, 0, 0, 0);
         if (t < s.len) {
           const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t / sh.block);
           if (id >= 0)
-            c = *reinterpret_cast<const uint4*>(a.at.codes + ((((long long)id * 2) * sh.kv_heads + h) * sh.block + (t & (sh.block - 1))) * D + piece * 16);
+            c = *reinterpret_cast<const uint4*>(a.at.codes + ((((long long)id * 2) * sh.kv_heads + h) * sh.block + (t & (sh.block - 1))) * D + map.piece * 16);
         }
-        store_codes<D>(smem + S::OFF_K, row, piece, c);
+        store_codes(smem + S::OFF_K, row, map.piece, c);
       }
       ptx::fence_proxy_async();
       __syncwarp();
