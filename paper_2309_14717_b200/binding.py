@@ -368,39 +368,60 @@ def alloc_kv_cache(d: KvDesc, device="cuda"):
     return codes, scales, score
 
 
+# The cache calls are made once per layer and generated token, beside kernels of a few microseconds: their checks take
+# a fast path that only compares, pointers go to ctypes as plain integers, and the current stream is asked for as its
+# handle (constructing torch.cuda.current_stream() alone takes 3 us).
 def _kv_want(name, t, dtype, shape):
-    """Checks a tensor of the cache calls; None stands for any size in `shape`."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, wanted {tuple('any' if w is None else w for w in shape)}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, wanted {shape}")
 
 
 def _kv_cache_want(d, codes, scales, score=None):
-    _kv_want("codes", codes, torch.int8, (d.num_blocks, 2, d.kv_heads, d.block_tokens, d.head_dim))
-    _kv_want("scales", scales, torch.float32, (d.num_blocks, 2, d.kv_heads))
+    n, h, b = d.num_blocks, d.kv_heads, d.block_tokens
+    _kv_want("codes", codes, torch.int8, (n, 2, h, b, d.head_dim))
+    _kv_want("scales", scales, torch.float32, (n, 2, h))
     if score is not None:
-        _kv_want("score", score, torch.float32, (d.num_blocks, d.kv_heads, d.block_tokens))
+        _kv_want("score", score, torch.float32, (n, h, b))
 
 
 def _kv_batch(starts, lens, table):
     """(batch, max_blocks) of a batch's device arrays, checked."""
-    batch = lens.shape[0]
-    _kv_want("lens", lens, torch.int32, (None,))
-    _kv_want("table", table, torch.int32, (batch, None))
+    batch = lens.shape[0] if lens.dim() == 1 else -1
+    max_blocks = table.shape[-1]
+    _kv_want("lens", lens, torch.int32, (batch,))
+    _kv_want("table", table, torch.int32, (batch, max_blocks))
     if starts is not None:
         _kv_want("starts", starts, torch.int32, (batch + 1,))
-    return batch, table.shape[1]
+    return batch, max_blocks
 
 
 def _kv_rows(name, t, heads, dim):
-    """(pointer, row stride) of bf16 rows [m, heads, dim] whose rows may lie apart."""
-    _kv_want(name, t, torch.bfloat16, (None, heads, dim))
+    """Row stride of bf16 rows [m, heads, dim] whose rows may lie apart, checked."""
+    _kv_want(name, t, torch.bfloat16, (t.shape[0], heads, dim))
     if not t.is_cuda:
         raise ValueError("tensors must live on a CUDA device")
-    if t.shape[0] > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim)):
+    if t.is_contiguous():
+        return heads * dim
+    row, head, last = t.stride()
+    if last != 1 or (heads > 1 and head != dim):
         raise ValueError(f"{name}: the heads of a row must lie one behind the other")
-    return c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else heads * dim)
+    return row if t.shape[0] > 1 else heads * dim
+
+
+def _kv_ptr(t):
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("tensors must live on a CUDA device")
+    if not t.is_contiguous():
+        raise ValueError("tensors must be contiguous")
+    return t.data_ptr()
+
+
+def _kv_stream(stream, t):
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def qalora_kv_append(d: KvDesc, max_new: int, starts, lens, table, k, v, codes, scales, score=None, dev_status=None,
@@ -408,13 +429,13 @@ def qalora_kv_append(d: KvDesc, max_new: int, starts, lens, table, k, v, codes, 
     """Stores the new tokens' keys and values (rows k, v bf16 [m, kv_heads, head_dim]) in the cache."""
     batch, max_blocks = _kv_batch(starts, lens, table)
     _kv_cache_want(d, codes, scales, score)
-    k_ptr, k_stride = _kv_rows("k", k, d.kv_heads, d.head_dim)
-    v_ptr, v_stride = _kv_rows("v", v, d.kv_heads, d.head_dim)
+    k_stride = _kv_rows("k", k, d.kv_heads, d.head_dim)
+    v_stride = _kv_rows("v", v, d.kv_heads, d.head_dim)
     if v.shape[0] != k.shape[0]:
         raise ValueError("k and v have different numbers of rows")
-    _check("qalora_kv_append", load().qalora_kv_append(byref(d), batch, k.shape[0], max_new, _ptr(starts), _ptr(lens), _ptr(table),
-                                                       max_blocks, k_ptr, k_stride, v_ptr, v_stride, _ptr(codes), _ptr(scales),
-                                                       _ptr(score), _ptr(dev_status), _stream(stream)))
+    _check("qalora_kv_append", load().qalora_kv_append(byref(d), batch, k.shape[0], max_new, _kv_ptr(starts), _kv_ptr(lens), _kv_ptr(table),
+                                                       max_blocks, k.data_ptr(), k_stride, v.data_ptr(), v_stride, _kv_ptr(codes), _kv_ptr(scales),
+                                                       _kv_ptr(score), _kv_ptr(dev_status), _kv_stream(stream, codes)))
 
 
 def qalora_kv_read(d: KvDesc, max_new: int, starts, first, table, codes, scales, k, v, stream=None):
@@ -430,9 +451,9 @@ def qalora_kv_read(d: KvDesc, max_new: int, starts, first, table, codes, scales,
     for name, t in (("k", k), ("v", v)):
         if t is not None:
             _kv_want(name, t, out.dtype, (out.shape[0], d.kv_heads, d.head_dim))
-    _check("qalora_kv_read", load().qalora_kv_read(byref(d), batch, out.shape[0], max_new, _ptr(starts), _ptr(first), _ptr(table),
-                                                   max_blocks, _ptr(codes), _ptr(scales), _ptr(k), _ptr(v),
-                                                   1 if out.dtype == torch.bfloat16 else 0, _stream(stream)))
+    _check("qalora_kv_read", load().qalora_kv_read(byref(d), batch, out.shape[0], max_new, _kv_ptr(starts), _kv_ptr(first), _kv_ptr(table),
+                                                   max_blocks, _kv_ptr(codes), _kv_ptr(scales), _kv_ptr(k), _kv_ptr(v),
+                                                   1 if out.dtype == torch.bfloat16 else 0, _kv_stream(stream, codes)))
 
 
 def qalora_kv_attention_workspace_bytes(d: KvDesc, batch: int, m: int, max_new: int, max_len: int, with_score: bool) -> int:
@@ -455,7 +476,7 @@ def qalora_kv_attention(d: KvDesc, max_new: int, max_len: int, starts, lens, tab
     [m, heads]; score_out = score_in + the attention weight that each cached token gathered."""
     batch, max_blocks = _kv_batch(starts, lens, table)
     _kv_cache_want(d, codes, scales)
-    q_ptr, q_stride = _kv_rows("q", q, d.heads, d.head_dim)
+    q_stride = _kv_rows("q", q, d.heads, d.head_dim)
     m = q.shape[0]
     _kv_want("out", out, torch.bfloat16, (m, d.heads, d.head_dim))
     if lse is not None:
@@ -464,9 +485,9 @@ def qalora_kv_attention(d: KvDesc, max_new: int, max_len: int, starts, lens, tab
         if t is not None:
             _kv_want("score", t, torch.float32, (d.num_blocks, d.kv_heads, d.block_tokens))
     _check("qalora_kv_attention", load().qalora_kv_attention(
-        byref(d), batch, m, max_new, max_len, _ptr(starts), _ptr(lens), _ptr(table), max_blocks, q_ptr, q_stride, _ptr(codes),
-        _ptr(scales), softmax_scale, _ptr(out), _ptr(lse), _ptr(score_in), _ptr(score_out), _ptr(workspace),
-        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream(stream)))
+        byref(d), batch, m, max_new, max_len, _kv_ptr(starts), _kv_ptr(lens), _kv_ptr(table), max_blocks, q.data_ptr(), q_stride, _kv_ptr(codes),
+        _kv_ptr(scales), softmax_scale, _kv_ptr(out), _kv_ptr(lse), _kv_ptr(score_in), _kv_ptr(score_out), _kv_ptr(workspace),
+        workspace.numel() * workspace.element_size() if workspace is not None else 0, _kv_stream(stream, codes)))
 
 
 def qalora_kv_evict(d: KvDesc, max_len: int, budget: int, recent: int, lens, table, codes, scales, score, dst_table, dst_lens, kept,
@@ -475,12 +496,12 @@ def qalora_kv_evict(d: KvDesc, max_len: int, budget: int, recent: int, lens, tab
     blocks of dst_table; dst_lens int32 [batch] and kept int32 [batch, kv_heads, budget] say how many and which."""
     batch, max_blocks = _kv_batch(None, lens, table)
     _kv_cache_want(d, codes, scales, score)
-    _kv_want("dst_table", dst_table, torch.int32, (batch, None))
+    _kv_want("dst_table", dst_table, torch.int32, (batch, dst_table.shape[-1]))
     _kv_want("dst_lens", dst_lens, torch.int32, (batch,))
     _kv_want("kept", kept, torch.int32, (batch, d.kv_heads, budget))
     _check("qalora_kv_evict", load().qalora_kv_evict(
-        byref(d), batch, max_len, budget, recent, _ptr(lens), _ptr(table), max_blocks, _ptr(codes), _ptr(scales), _ptr(score),
-        _ptr(dst_table), dst_table.shape[1], _ptr(dst_lens), _ptr(kept), _stream(stream)))
+        byref(d), batch, max_len, budget, recent, _kv_ptr(lens), _kv_ptr(table), max_blocks, _kv_ptr(codes), _kv_ptr(scales), _kv_ptr(score),
+        _kv_ptr(dst_table), dst_table.shape[1], _kv_ptr(dst_lens), _kv_ptr(kept), _kv_stream(stream, codes)))
 
 
 def qalora_kernel_launches() -> int:

@@ -2,11 +2,12 @@
 // device-side entries, and conversions between values and 8-bit codes.
 #pragma once
 #include "common.cuh"
+#include "ptx.cuh"
 
 namespace qalora {
 
 struct KvShape {
-  int heads, kv_heads, group, dim, block, num_blocks;
+  int heads, kv_heads, group, dim, block, log_block, num_blocks;
 };
 
 // A batch as the kernels see it.
@@ -56,6 +57,30 @@ int launch_kv_evict(const KvShape& sh, const KvBatch& b, int budget, int recent,
                     const int32_t* dst_table, int dst_max_blocks, int32_t* dst_lens, int32_t* kept, cudaStream_t st);
 
 #ifdef __CUDACC__
+// Launches a kernel of the cache so that its blocks may be set up while the kernel before it in the stream ends
+// (programmatic dependent launch); kv_begin() is the first thing such a kernel does that touches memory.
+template <class... P, class... A>
+inline int kv_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) return QALORA_ERR_CUDA;
+  count_launch();
+  return QALORA_OK;
+}
+// Waits for the kernel before, and only then lets the one after be set up: it can never run beside one before this.
+__device__ __forceinline__ void kv_begin() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+}
+
 // Rows and tokens of sequence b; n == 0 where the entries break the call's bounds.
 struct KvSeq {
   int row0, n;     // its rows are row0 .. row0 + n - 1
@@ -82,7 +107,6 @@ __device__ __forceinline__ int kv_block(const int32_t* table, int max_blocks, in
 // within 4e-5 of it for |v / s| <= 128 (two roundings of 2^-24 each), so that the division is
 // needed only where that product lies nearer than 1e-4 to a half-integer, where alone the two
 // could round apart.  `fast`: 1/s is neither zero nor infinite nor a subnormal.
-__device__ __forceinline__ bool kv_near_half(float t, float r) { return fabsf(t - r) > 0.4999f; }
 __device__ __forceinline__ float kv_code_div(float v, float s) {
   const float t = __fdiv_rn(v, s);
   return fminf(fmaxf(rintf(t), -127.f), 127.f);
@@ -93,30 +117,34 @@ __device__ __forceinline__ uint32_t kv_pack4(uint32_t a, uint32_t b, uint32_t c,
   return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
 
-// Four codes; `inv` = 1 / s.  The low byte of x / s + 1.5 * 2^23 is the rounded quotient in two's
-// complement, so no float-to-integer conversion is needed.
-__device__ __forceinline__ uint32_t kv_codes4(const float (&v)[4], float s, float inv) {
+// Four codes as floats: 2^23 + (c + 128) by byte permutation (its last place is 1), minus 2^23 + 128.  (The
+// conversion unit runs at a quarter of the rate.)
+__device__ __forceinline__ void kv_floats4(uint32_t w, float2& a, float2& b) {
+  const uint32_t u = w ^ 0x80808080u;
+  const float2 k = make_float2(8388736.f, 8388736.f);
+  a = ptx::fsub2(make_float2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7541))), k);
+  b = ptx::fsub2(make_float2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7542)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7543))), k);
+}
+
+// Four codes by division, for elements near a tie, scales whose inverse is not an ordinary number and elements that
+// may not be finite.  A call, not inlined: unrolled into every pass it made the kernels wait for instructions.
+static __device__ __noinline__ uint32_t kv_codes4_any(float v0, float v1, float v2, float v3, float s) {
+  const float v[4] = {v0, v1, v2, v3};
   uint32_t c[4];
-  bool near = false;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float t = __fmul_rn(v[i], inv), u = __fadd_rn(t, 12582912.f);
-    c[i] = __float_as_uint(u);
-    near |= kv_near_half(t, __fadd_rn(u, -12582912.f));
-  }
-  if (near) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = __float_as_uint(__fadd_rn(kv_code_div(v[i], s), 12582912.f));
-  }
+  for (int i = 0; i < 4; ++i) c[i] = (s > 0.f && v[i] == v[i]) ? (uint32_t)(int)kv_code_div(v[i], s) : 0u;
   return kv_pack4(c[0], c[1], c[2], c[3]);
 }
-// The same for scales whose inverse is not an ordinary number and for elements that may not be finite.
-__device__ __forceinline__ uint32_t kv_codes4_any(const float (&v)[4], float s) {
-  uint32_t c[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    c[i] = (s > 0.f && v[i] == v[i]) ? (uint32_t)(int)kv_code_div(v[i], s) : 0u;
-  return kv_pack4(c[0], c[1], c[2], c[3]);
+// Four codes; `inv` = 1 / s, or 0 where every element goes through the division.  The low byte of x / s + 1.5 * 2^23
+// is the rounded quotient in two's complement, so no float-to-integer conversion is needed.
+__device__ __forceinline__ uint32_t kv_codes4(float2 a, float2 b, float s, float inv) {
+  const float2 ii = make_float2(inv, inv), up = make_float2(12582912.f, 12582912.f), down = make_float2(-12582912.f, -12582912.f);
+  const float2 t0 = ptx::fmul2(a, ii), t1 = ptx::fmul2(b, ii);
+  const float2 u0 = ptx::fadd2(t0, up), u1 = ptx::fadd2(t1, up);
+  const float2 d0 = ptx::fsub2(t0, ptx::fadd2(u0, down)), d1 = ptx::fsub2(t1, ptx::fadd2(u1, down));
+  const float far = fmaxf(fmaxf(fabsf(d0.x), fabsf(d0.y)), fmaxf(fabsf(d1.x), fabsf(d1.y)));
+  if (!(far <= 0.4999f) || inv == 0.f) return kv_codes4_any(a.x, a.y, b.x, b.y, s);
+  return kv_pack4(__float_as_uint(u0.x), __float_as_uint(u0.y), __float_as_uint(u1.x), __float_as_uint(u1.y));
 }
 #endif
 

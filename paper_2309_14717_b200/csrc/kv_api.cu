@@ -14,7 +14,8 @@ int check_kv_desc(const qalora_kv_desc* d, KvShape* sh) {
     return QALORA_ERR_UNSUPPORTED_SHAPE;
   if ((long long)d->num_blocks * 2 * d->kv_heads > 0x7fffffffll / d->block_tokens) return QALORA_ERR_UNSUPPORTED_SHAPE;
   sh->heads = d->heads; sh->kv_heads = d->kv_heads; sh->group = d->heads / d->kv_heads;
-  sh->dim = d->head_dim; sh->block = d->block_tokens; sh->num_blocks = d->num_blocks;
+  sh->dim = d->head_dim; sh->block = d->block_tokens; sh->log_block = d->block_tokens == 16 ? 4 : d->block_tokens == 32 ? 5 : d->block_tokens == 64 ? 6 : 7;
+  sh->num_blocks = d->num_blocks;
   return QALORA_OK;
 }
 

@@ -65,16 +65,17 @@ __device__ __forceinline__ UnitPlace find_unit(const AttnArgs& a, const uint32_t
   return p;
 }
 
-template <int D, int MT, int SUB>
+template <int D, int NT, int SUB>
 struct AtSmem {
-  static constexpr int ROWS = 16 * MT, TOK = 16 * AT_WARPS * SUB, SUBS = TOK / 16;
+  static constexpr int ROWS = 8 * NT, TOK = 16 * AT_WARPS * SUB, SUBS = TOK / 16;
   static constexpr int TILE = TOK * D;                          // bytes of keys (or values) of a unit
-  static constexpr int STAGES = 65536 / (2 * TILE);
-  static constexpr int MERGE = AT_WARPS * 16 * D * 4;
+  static constexpr int STAGES = NT == 1 ? 3 : 4;
+  static constexpr int BLOCKS = NT == 1 ? 3 : 2;                // thread blocks per multiprocessor
+  static constexpr int MERGE = AT_WARPS * ROWS * D * 4;
   static constexpr int OFF_MERGE = STAGES * 2 * TILE;
   static constexpr int OFF_SCALES = OFF_MERGE + MERGE;                        // [STAGES][2][SUBS]
-  static constexpr int OFF_ML = OFF_SCALES + STAGES * 2 * SUBS * 4;           // [AT_WARPS][16][2]
-  static constexpr int OFF_BARS = OFF_ML + AT_WARPS * 16 * 2 * 4;
+  static constexpr int OFF_ML = OFF_SCALES + STAGES * 2 * SUBS * 4;           // [AT_WARPS][ROWS][2]
+  static constexpr int OFF_BARS = OFF_ML + AT_WARPS * ROWS * 2 * 4;
   static constexpr int OFF_FLAG = OFF_BARS + STAGES * 2 * 8;
   static constexpr int OFF_PLAN = OFF_FLAG + 16;
   static int total(int batch) { return OFF_PLAN + (batch + 2) * 4 + 1024; }   // (the window starts on a 1 KiB boundary)
@@ -85,18 +86,21 @@ struct AtSmem {
 template <int D, int ROWS>
 __host__ __device__ constexpr long long part_floats() { return (long long)ROWS * (D + 2); }
 
-// D: head width; MT: tiles of 16 rows (new tokens x heads of a group); SUB: 16-token steps per warp and unit.
-// Keys are the B operand of m16n8k16 straight from their row-major bytes: ldmatrix hands a lane four
-// consecutive codes of one token, which are a 16-wide step's two B registers if the same permutation of the
-// channels is applied to the query; values are B through the transposing ldmatrix, whose 16-bit elements are
-// pairs of channels: the even and the odd channels become two column tiles.  Codes turn into fp16
-// exactly (1024 + 128 + c by byte permutation, minus 1152), the query is fp16 after a power-of-two scaling
-// per row (bf16 has fewer bits), so the scores are sums of exact products in float32.
+// D: head width; NT: tiles of 8 rows (new tokens x heads of a group); SUB: 16-token steps per warp and unit.
+// Both products have the tokens or channels as the 16 rows of m16n8k16 and the few query rows as its 8 columns:
+//   S^T = K Q^T   ldmatrix hands a lane four consecutive codes of one token, which are two A registers of a 16-channel
+//                 step if the same permutation of the channels is applied to the query;
+//   O^T = V^T P^T the transposing ldmatrix, whose 16-bit elements are pairs of channels, gives the even and the odd
+//                 channels as rows 0-7 and 8-15 of A; P^T is S^T's result through movmatrix.
+// (With the query rows as the 16 rows of the product, most of them padding, the same work took twice the products and
+// 450 instead of 250 instructions per 16 tokens: 32 conversations of up to 4096 tokens 181 us, now NNN us.)
+// Codes turn into fp16 exactly (1024 + 128 + c by byte permutation, minus 1152), the query is fp16 after a
+// power-of-two scaling per row (bf16 has fewer bits), so the scores are sums of exact products in float32.
 // Every warp keeps maximum, sum and output of its own tokens; the warps meet only at the end of a row tile.
-template <int D, int MT, int SUB>
-__global__ void __launch_bounds__(AT_THREADS, 2)
-kv_attend_kernel(const __grid_constant__ CUtensorMap map, AttnArgs a, int* dbg) {
-  using S = AtSmem<D, MT, SUB>;
+template <int D, int NT, int SUB>
+__global__ void __launch_bounds__(AT_THREADS, AtSmem<D, NT, SUB>::BLOCKS)
+kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnArgs a, int* dbg) {
+  using S = AtSmem<D, NT, SUB>;
   constexpr int ROWS = S::ROWS, TOK = S::TOK, SUBS = S::SUBS, STAGES = S::STAGES;
   constexpr int KSTEPS = D / 16;
   extern __shared__ uint8_t raw[];
@@ -117,8 +121,9 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, AttnArgs a, int* dbg) 
     *flag = 0;
     for (int s = 0; s < STAGES; ++s) { ptx::mbar_init(full(s), 1); ptx::mbar_init(empty(s), AT_WARPS); }
     ptx::fence_mbar_init();
-    if (blockIdx.x == 0 && a.batch0 == 0) *a.status = 0;
   }
+  kv_begin();
+  if (tid == 0 && blockIdx.x == 0 && a.batch0 == 0) *a.status = 0;
   // the plan: an exclusive sum over the sequences' units, by one warp
   if (warp == AT_WARPS) {
     ptx::prefetch_tensormap(&map);
@@ -163,13 +168,13 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, AttnArgs a, int* dbg) 
       const KvSeq s = kv_seq(a.kb, p.b);
       const int t = p.tile * TOK + sub * 16;
       if (t >= s.len) return l;
-      const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, p.b, t / sh.block);
+      const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, p.b, t >> sh.log_block);
       if (id < 0) return l;
       const long long k_plane = ((long long)id * 2) * sh.kv_heads + p.h, v_plane = k_plane + sh.kv_heads;
       l.ks = a.at.scales[k_plane];
       l.vs = a.at.scales[v_plane];
-      l.k_row = (int)(k_plane * sh.block + t % sh.block);
-      l.v_row = (int)(v_plane * sh.block + t % sh.block);
+      l.k_row = (int)(k_plane * sh.block + (t & (sh.block - 1)));
+      l.v_row = (int)(v_plane * sh.block + (t & (sh.block - 1)));
       return l;
     };
     Look cur = look(u0 + lane / SUBS);
@@ -198,16 +203,16 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, AttnArgs a, int* dbg) 
     }
   } else {
     // ---- consumers
-    const int g8 = lane >> 2, q4 = lane & 3;          // row within 8, quad lane
-    uint32_t qf[MT][KSTEPS][4];
-    float q_scale[MT][2];                              // softmax_scale * log2(e) / (the row's power of two)
-    int limit[MT][2];                                  // last token the row sees, -1: none
-    float mrow[MT][2], lrow[MT][2], o[MT][D / 8][4], ref;
+    const int g8 = lane >> 2, q4 = lane & 3;          // token (or channel pair) within 8, quad lane: rows 2 q4 and 2 q4 + 1
+    uint32_t qf[NT][KSTEPS][2];
+    float q_scale[NT][2];                              // softmax_scale * log2(e) / (the row's power of two)
+    int limit[NT][2];                                  // last token the row sees, -1: none
+    float mrow[NT][2], lrow[NT][2], o[NT][KSTEPS][4], ref = 0.f, inv_ref = 0.f;
+    float* logit_row[NT][2];
     UnitPlace p{};
     KvSeq s{};
     bool fresh = true, ok = true;
     int rows = 0, limit_lo = 0;
-    const float* logit_row[MT][2];
     for (uint32_t u = u0, it = 0; u < u1; ++u, ++it) {
       if (fresh) {
         p = find_unit<TOK, ROWS>(a, prefix, u);
@@ -215,52 +220,51 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, AttnArgs a, int* dbg) 
         rows = s.n * sh.group - p.rt * ROWS;
         if (rows > ROWS) rows = ROWS;
         limit_lo = s.first + (p.rt * ROWS) / sh.group;                 // the earliest row's
-        ref = 0.f;
+        ref = inv_ref = 0.f;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < NT; ++nt) {
+          // this lane's part of row g8 of the tile, as the B operand
+          const int mine = nt * 8 + g8, r = p.rt * ROWS + mine, i = r / sh.group, g = r % sh.group;
+          const bool load = mine < rows && QALORA_CHECK(dbg, s.row0 + i, a.kb.m);
+          const __nv_bfloat16* src = a.at.q + (long long)(s.row0 + i) * a.at.q_stride + (long long)(p.h * sh.group + g) * D;
+          uint2 w[KSTEPS];
+          uint32_t mx = 0;
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            const int r = p.rt * ROWS + mt * 16 + hf * 8 + g8, i = r / sh.group, g = r % sh.group;
-            const bool there = mt * 16 + hf * 8 + g8 < rows;
-            limit[mt][hf] = there ? s.first + i : -1;
-            uint2 w[KSTEPS];
-            uint32_t mx = 0;
-            const __nv_bfloat16* src = a.at.q + (long long)(s.row0 + i) * a.at.q_stride + (long long)(p.h * sh.group + g) * D;
+          for (int k = 0; k < KSTEPS; ++k) w[k] = load ? *reinterpret_cast<const uint2*>(src + k * 16 + q4 * 4) : make_uint2(0, 0);
 #pragma unroll
-            for (int k = 0; k < KSTEPS; ++k) {
-              w[k] = make_uint2(0, 0);
-              if (there && QALORA_CHECK(dbg, s.row0 + i, a.kb.m)) w[k] = *reinterpret_cast<const uint2*>(src + k * 16 + q4 * 4);
-              mx = __vmaxu2(__vmaxu2(mx, w[k].x & 0x7fff7fffu), w[k].y & 0x7fff7fffu);
-            }
-            mx = max(mx & 0xffffu, mx >> 16);
-            mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-            mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            // times a power of two that brings the row's largest element to 2^14 .. 2^15: exact in fp16
-            // down to 2^-28 of it
-            int e = 268 - (int)(mx >> 7);
-            e = e > 254 ? 254 : (e < 1 ? 1 : e);
-            const float f = __uint_as_float((uint32_t)e << 23);
-            q_scale[mt][hf] = a.at.softmax_scale * kLog2e * __uint_as_float((uint32_t)(254 - e) << 23);
-            if (e == 254) q_scale[mt][hf] = a.at.softmax_scale * kLog2e * 0x1p-127f;
+          for (int k = 0; k < KSTEPS; ++k) mx = __vmaxu2(__vmaxu2(mx, w[k].x & 0x7fff7fffu), w[k].y & 0x7fff7fffu);
+          mx = max(mx & 0xffffu, mx >> 16);
+          mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+          mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+          // times a power of two that brings the row's largest element to 2^14 .. 2^15: exact in fp16
+          // down to 2^-28 of it
+          int e = 268 - (int)(mx >> 7);
+          e = e > 254 ? 254 : (e < 1 ? 1 : e);
+          const float f = __uint_as_float((uint32_t)e << 23);
+          const float back = a.at.softmax_scale * kLog2e * (e == 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23));
 #pragma unroll
-            for (int k = 0; k < KSTEPS; ++k) {
-              const float x0 = __uint_as_float(w[k].x << 16) * f, x1 = __uint_as_float(w[k].x & 0xffff0000u) * f;
-              const float x2 = __uint_as_float(w[k].y << 16) * f, x3 = __uint_as_float(w[k].y & 0xffff0000u) * f;
-              qf[mt][k][hf] = kvp::pack_half2(x0, x1);
-              qf[mt][k][2 + hf] = kvp::pack_half2(x2, x3);
-            }
-            mrow[mt][hf] = kNoMax;
-            lrow[mt][hf] = 0.f;
-            const int head = p.h * sh.group + g;
-            logit_row[mt][hf] = a.logits != nullptr && there
-                                    ? a.logits + ((long long)((a.batch0 + p.b) * a.kb.n_hi + i) * sh.heads + head) * a.logit_stride : nullptr;
+          for (int k = 0; k < KSTEPS; ++k) {
+            qf[nt][k][0] = kvp::pack_half2(__uint_as_float(w[k].x << 16) * f, __uint_as_float(w[k].x & 0xffff0000u) * f);
+            qf[nt][k][1] = kvp::pack_half2(__uint_as_float(w[k].y << 16) * f, __uint_as_float(w[k].y & 0xffff0000u) * f);
+          }
+          // and what belongs to the rows 2 q4, 2 q4 + 1 whose scores this lane holds
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const int own = nt * 8 + q4 * 2 + c, ro = p.rt * ROWS + own, io = ro / sh.group;
+            q_scale[nt][c] = __shfl_sync(0xffffffffu, back, (q4 * 2 + c) * 4);
+            limit[nt][c] = own < rows ? s.first + io : -1;
+            mrow[nt][c] = kNoMax;
+            lrow[nt][c] = 0.f;
+            logit_row[nt][c] = a.logits != nullptr && own < rows
+                                   ? a.logits + ((long long)((a.batch0 + p.b) * a.kb.n_hi + io) * sh.heads + p.h * sh.group + ro % sh.group) *
+                                                    a.logit_stride
+                                   : nullptr;
           }
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+          for (int k = 0; k < KSTEPS; ++k)
 #pragma unroll
-          for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) o[mt][n][c] = 0.f;
+            for (int c = 0; c < 4; ++c) o[nt][k][c] = 0.f;
+        }
         fresh = false;
       }
       const int st = it % STAGES;
@@ -272,108 +276,96 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, AttnArgs a, int* dbg) 
         const int sub = sb * AT_WARPS + warp, t0 = p.tile * TOK + sub * 16;
         if (t0 >= s.len || !ok) break;
         const float ks = scale_ring[st * 2 * SUBS + sub], vs = scale_ring[st * 2 * SUBS + SUBS + sub];
-        // scores of 16 tokens: two column tiles
-        float sc[MT][2][4];
+        // scores of 16 tokens: rows of the product are tokens g8 and g8 + 8
+        float sc[NT][4];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+          for (int c = 0; c < 4; ++c) sc[nt][c] = 0.f;
+        const int tok = sub * 16 + (lane & 15);        // ldmatrix: lanes 0-15 the tokens of one chunk, 16-31 of the next
 #pragma unroll
-            for (int c = 0; c < 4; ++c) sc[mt][j][c] = 0.f;
+        for (int c2 = 0; c2 < D / 32; ++c2) {
+          uint32_t r[4];
+          kvp::ldmatrix_x4(r, k_base + kvp::swizzled<D>(tok, c2 * 2 + (lane >> 4)));
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+          for (int x = 0; x < 2; ++x) {
+            uint32_t f[4];                             // {token g8, +8} x {channels 0-1, 2-3 of the lane's four}
+            kvp::codes_to_half(r[2 * x], f[0], f[2]);
+            kvp::codes_to_half(r[2 * x + 1], f[1], f[3]);
 #pragma unroll
-          for (int quarter = 0; quarter < D / 64; ++quarter) {
-            const int tok = sub * 16 + j * 8 + (lane & 7), chunk = quarter * 4 + (lane >> 3);
-            uint32_t r[4];
-            kvp::ldmatrix_x4(r, k_base + kvp::swizzled<D>(tok, chunk));
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              uint32_t b0, b1;
-              kvp::codes_to_half(r[x], b0, b1);
-#pragma unroll
-              for (int mt = 0; mt < MT; ++mt) kvp::mma16816(sc[mt][j], qf[mt][quarter * 4 + x], b0, b1);
-            }
+            for (int nt = 0; nt < NT; ++nt) kvp::mma16816(sc[nt], f, qf[nt][c2 * 2 + x][0], qf[nt][c2 * 2 + x][1]);
           }
+        }
         // scaled scores in powers of two, masked
         const bool edge = t0 + 15 > limit_lo || rows < ROWS;
         bool grow = false;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            const float f = q_scale[mt][hf] * ks;
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                float& x = sc[mt][j][hf * 2 + c];
-                x *= f;
-                if (edge && t0 + j * 8 + q4 * 2 + c > limit[mt][hf]) x = -INFINITY;
-                grow |= x > mrow[mt][hf] + kGrow;
-              }
-            if (logit_row[mt][hf] != nullptr) {
-#pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const int t = t0 + j * 8 + q4 * 2;
-                if (QALORA_CHECK(dbg, t + 1, a.logit_stride))
-                  *reinterpret_cast<float2*>(const_cast<float*>(logit_row[mt][hf]) + t) = make_float2(sc[mt][j][hf * 2], sc[mt][j][hf * 2 + 1]);
-              }
+          for (int c = 0; c < 2; ++c) {
+            const float f = q_scale[nt][c] * ks;
+            float &x0 = sc[nt][c], &x1 = sc[nt][2 + c];
+            x0 *= f;
+            x1 *= f;
+            if (edge) {
+              if (t0 + g8 > limit[nt][c]) x0 = -INFINITY;
+              if (t0 + g8 + 8 > limit[nt][c]) x1 = -INFINITY;
+            }
+            grow |= fmaxf(x0, x1) > mrow[nt][c] + kGrow;
+            if (logit_row[nt][c] != nullptr && QALORA_CHECK(dbg, t0 + g8 + 8, a.logit_stride)) {
+              logit_row[nt][c][t0 + g8] = x0;
+              logit_row[nt][c][t0 + g8 + 8] = x1;
             }
           }
         if (__any_sync(0xffffffffu, grow) || vs > ref) {
           // rare: bring the rows to their new maximum, and the outputs to the new largest value scale
           const float ref_new = vs > ref ? vs : ref, ref_ratio = ref_new > 0.f ? ref / ref_new : 0.f;
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
+          for (int nt = 0; nt < NT; ++nt) {
             float by[2];
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              float mx = fmaxf(fmaxf(sc[mt][0][hf * 2], sc[mt][0][hf * 2 + 1]), fmaxf(sc[mt][1][hf * 2], sc[mt][1][hf * 2 + 1]));
-              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-              mx = fmaxf(mx, mrow[mt][hf]);
-              by[hf] = exp2f(mrow[mt][hf] - mx);
-              mrow[mt][hf] = mx;
-              lrow[mt][hf] *= by[hf];
-              by[hf] *= ref_ratio;
+            for (int c = 0; c < 2; ++c) {
+              float mx = fmaxf(sc[nt][c], sc[nt][2 + c]);
+#pragma unroll
+              for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+              mx = fmaxf(mx, mrow[nt][c]);
+              by[c] = exp2f(mrow[nt][c] - mx);
+              mrow[nt][c] = mx;
+              lrow[nt][c] *= by[c];
+              by[c] *= ref_ratio;
             }
 #pragma unroll
-            for (int n = 0; n < D / 8; ++n) {
-              o[mt][n][0] *= by[0]; o[mt][n][1] *= by[0];
-              o[mt][n][2] *= by[1]; o[mt][n][3] *= by[1];
+            for (int k = 0; k < KSTEPS; ++k) {
+              o[nt][k][0] *= by[0]; o[nt][k][1] *= by[1];
+              o[nt][k][2] *= by[0]; o[nt][k][3] *= by[1];
             }
           }
           ref = ref_new;
+          inv_ref = ref > 0.f ? 1.f / ref : 0.f;
         }
-        const float v_rel = ref > 0.f ? vs / ref : 0.f;
-        uint32_t pf[MT][4];
+        const float v_rel = vs * inv_ref;
+        uint32_t pf[NT][2];                            // P^T as the B operand: tokens 0-7 and 8-15
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < NT; ++nt) {
+          float e[4];
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const float e0 = kvp::exp2_fast(sc[mt][j][hf * 2] - (mrow[mt][hf] - kLift));
-              const float e1 = kvp::exp2_fast(sc[mt][j][hf * 2 + 1] - (mrow[mt][hf] - kLift));
-              lrow[mt][hf] += e0 + e1;
-              pf[mt][j * 2 + hf] = kvp::pack_half2(e0 * v_rel, e1 * v_rel);
-            }
+          for (int c = 0; c < 4; ++c) e[c] = kvp::exp2_fast(sc[nt][c] - (mrow[nt][c & 1] - kLift));
+          lrow[nt][0] += e[0] + e[2];
+          lrow[nt][1] += e[1] + e[3];
+          pf[nt][0] = kvp::movmatrix(kvp::pack_half2(e[0] * v_rel, e[1] * v_rel));
+          pf[nt][1] = kvp::movmatrix(kvp::pack_half2(e[2] * v_rel, e[3] * v_rel));
+        }
 #pragma unroll
         for (int c2 = 0; c2 < D / 32; ++c2) {
-          const int tok = sub * 16 + (lane & 15), chunk = c2 * 2 + (lane >> 4);
           uint32_t r[4];
-          kvp::ldmatrix_x4_trans(r, v_base + kvp::swizzled<D>(tok, chunk));
+          kvp::ldmatrix_x4_trans(r, v_base + kvp::swizzled<D>(tok, c2 * 2 + (lane >> 4)));
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            uint32_t e0, d0, e1, d1;                    // even / odd channels of tokens 0-7 and 8-15
-            kvp::pairs_to_half(r[2 * x], e0, d0);
-            kvp::pairs_to_half(r[2 * x + 1], e1, d1);
+            uint32_t f[4];                             // {even, odd channels} x {tokens 0-7, 8-15}
+            kvp::pairs_to_half(r[2 * x], f[0], f[1]);
+            kvp::pairs_to_half(r[2 * x + 1], f[2], f[3]);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              kvp::mma16816(o[mt][(c2 * 2 + x) * 2], pf[mt], e0, e1);
-              kvp::mma16816(o[mt][(c2 * 2 + x) * 2 + 1], pf[mt], d0, d1);
-            }
+            for (int nt = 0; nt < NT; ++nt) kvp::mma16816(o[nt][c2 * 2 + x], f, pf[nt][0], pf[nt][1]);
           }
         }
       }
@@ -387,54 +379,49 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, AttnArgs a, int* dbg) 
         const int slot = 2 * (int)blockIdx.x + (row_tile_first < u0 ? 0 : 1);
         float* part = a.parts + slot * part_floats<D, ROWS>();
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            float l = lrow[mt][hf];
-            l += __shfl_xor_sync(0xffffffffu, l, 1);
-            l += __shfl_xor_sync(0xffffffffu, l, 2);
-            const int r = hf * 8 + g8;
-            if (q4 == 0) { ml[(warp * 16 + r) * 2] = mrow[mt][hf]; ml[(warp * 16 + r) * 2 + 1] = l; }
-            if (mt * 16 + r < rows)
+          for (int c = 0; c < 2; ++c) {
+            float l = lrow[nt][c];
 #pragma unroll
-              for (int jj = 0; jj < D / 16; ++jj) {
-                const float4 x = make_float4(o[mt][2 * jj][hf * 2] * ref, o[mt][2 * jj + 1][hf * 2] * ref,
-                                             o[mt][2 * jj][hf * 2 + 1] * ref, o[mt][2 * jj + 1][hf * 2 + 1] * ref);
-                *reinterpret_cast<float4*>(merge + (warp * 16 + r) * D + jj * 16 + q4 * 4) = x;
-              }
-          }
-          ptx::named_barrier(1, AT_WARPS * 32);
-          const int here = rows - mt * 16 < 16 ? rows - mt * 16 : 16;
-          for (int i = tid; i < here * (D / 4); i += AT_WARPS * 32) {
-            const int r = i / (D / 4), d = (i % (D / 4)) * 4;
-            float mx = kNoMax, l = 0.f;
+            for (int w = 4; w < 32; w <<= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
+            const int r = nt * 8 + q4 * 2 + c;
+            if (g8 == 0) { ml[(warp * ROWS + r) * 2] = mrow[nt][c]; ml[(warp * ROWS + r) * 2 + 1] = l; }
+            if (r < rows) {
 #pragma unroll
-            for (int w = 0; w < AT_WARPS; ++w) mx = fmaxf(mx, ml[(w * 16 + r) * 2]);
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < AT_WARPS; ++w) {
-              const float by = exp2f(ml[(w * 16 + r) * 2] - mx);
-              const float4 y = *reinterpret_cast<const float4*>(merge + (w * 16 + r) * D + d);
-              l = fmaf(by, ml[(w * 16 + r) * 2 + 1], l);
-              x.x = fmaf(by, y.x, x.x); x.y = fmaf(by, y.y, x.y); x.z = fmaf(by, y.z, x.z); x.w = fmaf(by, y.w, x.w);
-            }
-            const int row = mt * 16 + r;
-            if (whole) {
-              const int rr = p.rt * ROWS + row, tok = s.row0 + rr / sh.group, head = p.h * sh.group + rr % sh.group;
-              const long long at = (long long)tok * sh.heads + head;
-              if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) continue;
-              kvp::store_row4(a.at.out + at * D + d, x, l);
-              if (d == 0) {
-                const long long own = (long long)((a.batch0 + p.b) * a.kb.n_hi + rr / sh.group) * sh.heads + head;
-                kvp::store_lse(a.at.lse, at, a.lse2, own, mx, l, kLift);
-              }
-            } else if (QALORA_CHECK(dbg, slot, 2 * a.units_grid)) {
-              *reinterpret_cast<float4*>(part + 2 * ROWS + row * D + d) = x;
-              if (d == 0) *reinterpret_cast<float2*>(part + 2 * row) = make_float2(mx, l);
+              for (int k = 0; k < KSTEPS; ++k)
+                *reinterpret_cast<float2*>(merge + (warp * ROWS + r) * D + k * 16 + g8 * 2) = make_float2(o[nt][k][c] * ref, o[nt][k][2 + c] * ref);
             }
           }
-          ptx::named_barrier(1, AT_WARPS * 32);
+        ptx::named_barrier(1, AT_WARPS * 32);
+        for (int i = tid; i < rows * (D / 4); i += AT_WARPS * 32) {
+          const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+          float mx = kNoMax, l = 0.f;
+#pragma unroll
+          for (int w = 0; w < AT_WARPS; ++w) mx = fmaxf(mx, ml[(w * ROWS + r) * 2]);
+          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int w = 0; w < AT_WARPS; ++w) {
+            const float by = exp2f(ml[(w * ROWS + r) * 2] - mx);
+            const float4 y = *reinterpret_cast<const float4*>(merge + (w * ROWS + r) * D + d);
+            l = fmaf(by, ml[(w * ROWS + r) * 2 + 1], l);
+            x.x = fmaf(by, y.x, x.x); x.y = fmaf(by, y.y, x.y); x.z = fmaf(by, y.z, x.z); x.w = fmaf(by, y.w, x.w);
+          }
+          if (whole) {
+            const int rr = p.rt * ROWS + r, i_new = rr / sh.group, head = p.h * sh.group + rr % sh.group;
+            const long long at = (long long)(s.row0 + i_new) * sh.heads + head;
+            if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) continue;
+            kvp::store_row4(a.at.out + at * D + d, x, l);
+            if (d == 0) {
+              const long long own = (long long)((a.batch0 + p.b) * a.kb.n_hi + i_new) * sh.heads + head;
+              kvp::store_lse(a.at.lse, at, a.lse2, own, mx, l, kLift);
+            }
+          } else if (QALORA_CHECK(dbg, slot, 2 * a.units_grid)) {
+            *reinterpret_cast<float4*>(part + 2 * ROWS + r * D + d) = x;
+            if (d == 0) *reinterpret_cast<float2*>(part + 2 * r) = make_float2(mx, l);
+          }
         }
+        ptx::named_barrier(1, AT_WARPS * 32);
         fresh = true;
       }
     }
@@ -446,8 +433,9 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, AttnArgs a, int* dbg) 
 // adds up the gathered weights from the stored scores (the other blocks).
 template <int D, int ROWS, int TOK>
 __global__ void __launch_bounds__(128)
-kv_join_kernel(AttnArgs a, int join_blocks, int row_tiles_max, int* dbg) {
+kv_join_kernel(const __grid_constant__ AttnArgs a, int join_blocks, int row_tiles_max, int* dbg) {
   __shared__ float row_lse[1024];
+  kv_begin();
   const KvShape& sh = a.sh;
   const int b = blockIdx.y, tid = threadIdx.x;
   const KvSeq s = kv_seq(a.kb, b);
@@ -522,9 +510,9 @@ kv_join_kernel(AttnArgs a, int join_blocks, int row_tiles_max, int* dbg) {
     }
   }
   if (t >= s.len) return;
-  const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t / sh.block);
+  const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t >> sh.log_block);
   if (id < 0) return;
-  const long long at = ((long long)id * sh.kv_heads + h) * sh.block + t % sh.block;
+  const long long at = ((long long)id * sh.kv_heads + h) * sh.block + (t & (sh.block - 1));
   const float got[4] = {w.x, w.y, w.z, w.w};
   for (int c = 0; c < 4 && t + c < s.len; ++c)
     a.at.score_out[at + c] = (a.at.score_in != nullptr ? a.at.score_in[at + c] : 0.f) + got[c];
@@ -543,26 +531,26 @@ bool make_cache_map(CUtensorMap* map, const int8_t* codes, const KvShape& sh, in
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int MT, int SUB>
+template <int D, int NT, int SUB>
 int attend(const AttnArgs& a, cudaStream_t st) {
-  using S = AtSmem<D, MT, SUB>;
+  using S = AtSmem<D, NT, SUB>;
   CUtensorMap map;
   if (!make_cache_map(&map, a.at.codes, a.sh, a.sh.block < S::TOK ? a.sh.block : S::TOK)) return QALORA_ERR_CUDA;
   static PerDeviceOnce once;
   const int ok = once.run([] {
-    return cudaFuncSetAttribute(kv_attend_kernel<D, MT, SUB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::total(AT_MAX_BATCH));
+    return cudaFuncSetAttribute(kv_attend_kernel<D, NT, SUB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::total(AT_MAX_BATCH));
   });
   if (ok != QALORA_OK) return ok;
+  int r;
   {
     MainKernelProbe probe("kv_attend_kernel", st);
-    kv_attend_kernel<D, MT, SUB><<<a.units_grid, AT_THREADS, S::total(a.kb.batch), st>>>(map, a, debug_words());
+    r = kv_launch(kv_attend_kernel<D, NT, SUB>, dim3((unsigned)a.units_grid), AT_THREADS, (size_t)S::total(a.kb.batch), st, map, a, debug_words());
   }
+  if (r != QALORA_OK) return r;
   const int row_tiles = (a.kb.max_new * a.sh.group + S::ROWS - 1) / S::ROWS, join = a.sh.kv_heads * row_tiles;
   const int score_blocks = a.logits != nullptr ? a.sh.kv_heads * ((a.kb.max_len + 511) / 512) : 0;
-  kv_join_kernel<D, S::ROWS, S::TOK><<<dim3((unsigned)(join + score_blocks), (unsigned)a.kb.batch), 128, 0, st>>>(
-      a, join, row_tiles, debug_words());
-  count_launch(2);
-  return cuda_status(cudaGetLastError());
+  return kv_launch(kv_join_kernel<D, S::ROWS, S::TOK>, dim3((unsigned)(join + score_blocks), (unsigned)a.kb.batch), 128, 0, st, a, join,
+                   row_tiles, debug_words());
 }
 
 struct AttnLayout {
@@ -574,9 +562,9 @@ struct AttnLayout {
 
 // Rows (new tokens x heads of a group) of one kv head up to which a sequence is taken here; with more, its
 // products fill the tensor core's tiles of 128 rows.
-constexpr int kFewRows = 32;
+constexpr int kFewRows = 16;
 
-int row_tiles_of(const KvShape& sh, int max_new) { return max_new * sh.group <= 16 ? 1 : 2; }     // MT
+int column_tiles(const KvShape& sh, int max_new) { return max_new * sh.group <= 8 ? 1 : 2; }     // NT
 
 AttnLayout attention_layout(const KvShape& sh, int batch, int64_t m, int max_new, int max_len, bool with_score, Workspace* guards) {
   AttnLayout w{};
@@ -593,11 +581,11 @@ AttnLayout attention_layout(const KvShape& sh, int batch, int64_t m, int max_new
   // (with every sequence at its bound but one, that one has m - (batch - 1) * max_new rows: when even
   // those are many, no sequence has few)
   w.any_few = w.few > 0 && m - (int64_t)(batch - 1) * max_new <= w.few;
-  const int rows = 16 * row_tiles_of(sh, w.few);
+  const int rows = 8 * column_tiles(sh, w.few);
   const size_t few_rows = w.any_few ? (size_t)batch * w.few * sh.heads : 0;
   w.status = take(256);
   w.plan = take((size_t)((batch < AT_MAX_BATCH ? batch : AT_MAX_BATCH) + 2) * 4);
-  w.parts = take(w.any_few ? (size_t)device_sm_count() * 2 * 2 * rows * (sh.dim + 2) * 4 : 0);
+  w.parts = take(w.any_few ? (size_t)device_sm_count() * 3 * 2 * rows * (sh.dim + 2) * 4 : 0);   // (two for each of up to three blocks)
   w.lse2 = take(with_score ? few_rows * 4 : 0);
   w.logits = take(with_score ? few_rows * round_up((size_t)max_len, 128) * 4 : 0);
   if (w.any_many) w.prompt = kv_prompt_scratch(sh, batch, m, max_len, with_score);
@@ -621,9 +609,9 @@ int launch_few(const KvShape& sh, const KvBatch& b, const KvAttention& at, const
   a.lse2 = at.score_out != nullptr ? reinterpret_cast<float*>(base + L.lse2) : nullptr;
   a.logits = at.score_out != nullptr ? reinterpret_cast<float*>(base + L.logits) : nullptr;
   a.logit_stride = (long long)round_up((size_t)max_len, 128);
-  const int mt = row_tiles_of(sh, L.few), tok = sh.dim == 128 ? 64 : 128;
+  const int nt = column_tiles(sh, L.few), tok = sh.dim == 128 ? 64 : 128;
   const long long tiles = b.max_len > 0 ? (b.max_len + tok - 1) / tok : 1;
-  const long long per_seq = tiles * sh.kv_heads * ((L.few * (long long)sh.group + 16 * mt - 1) / (16 * mt));
+  const long long per_seq = tiles * sh.kv_heads * ((L.few * (long long)sh.group + 8 * nt - 1) / (8 * nt));
   if (per_seq > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
   // sequences of one launch: their plan fits shared memory and their units 31 bits
   const long long fit = 0x7fffffffll / per_seq;
@@ -634,11 +622,11 @@ int launch_few(const KvShape& sh, const KvBatch& b, const KvAttention& at, const
     a.kb.starts = b.starts + b0;
     a.kb.lens = b.lens + b0;
     a.kb.table = b.table + (size_t)b0 * b.max_blocks;
-    const long long units = per_seq * a.kb.batch, most = 2ll * device_sm_count();
+    const long long units = per_seq * a.kb.batch, most = (nt == 1 ? 3ll : 2ll) * device_sm_count();
     a.units_grid = (int)(units < most ? units : most);
     int r;
-    if (sh.dim == 128) r = mt == 1 ? attend<128, 1, 1>(a, st) : attend<128, 2, 1>(a, st);
-    else r = mt == 1 ? attend<64, 1, 2>(a, st) : attend<64, 2, 2>(a, st);
+    if (sh.dim == 128) r = nt == 1 ? attend<128, 1, 1>(a, st) : attend<128, 2, 1>(a, st);
+    else r = nt == 1 ? attend<64, 1, 2>(a, st) : attend<64, 2, 2>(a, st);
     if (r != QALORA_OK) return r;
   }
   return QALORA_OK;

@@ -23,22 +23,19 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
                  float* __restrict__ score, int32_t* __restrict__ dev_status, int* dbg) {
   constexpr int CHUNKS = D / 8, ROWS = 128 / CHUNKS;
   __shared__ uint32_t warp_max[8];
+  kv_begin();
   const int b = blockIdx.y, h = blockIdx.x % sh.kv_heads, j = blockIdx.x / sh.kv_heads;
   const KvSeq s = kv_seq(kb, b);
   if (s.n == 0) return;
   const int lo = s.first > 0 ? s.first : 0;
-  const int jb = lo / sh.block + j, base = jb * sh.block;
+  const int jb = (lo >> sh.log_block) + j, base = jb * sh.block;
   if (base >= s.len) return;
   const int s0 = lo > base ? lo - base : 0;                                       // slots s0 .. s1 - 1 are new
   const int s1 = s.len - base < sh.block ? s.len - base : sh.block;
-  const int id = kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, jb);
-  if (id < 0) return;
+  const int raw = kb.table[(size_t)b * kb.max_blocks + jb];
   const int which = threadIdx.x >> 7, t = threadIdx.x & 127, chunk = t % CHUNKS, row = t / CHUNKS;
   const __nv_bfloat16* src = which == 0 ? k : v;
   const long long stride = which == 0 ? k_stride : v_stride;
-  const long long plane = ((long long)id * 2 + which) * sh.kv_heads + h;
-  int8_t* dst = codes + plane * sh.block * D;
-  const float before = scales[plane];
 
   uint4 x[PASSES];
   uint32_t mx = 0;
@@ -52,6 +49,11 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
         x[p] = __ldcs(reinterpret_cast<const uint4*>(src + r * stride + (long long)h * D + chunk * 8));
     }
   }
+  const int id = raw >= 0 && raw < sh.num_blocks ? raw : -1;      // (looked up while the rows are on their way)
+  if (id < 0) return;
+  const long long plane = ((long long)id * 2 + which) * sh.kv_heads + h;
+  int8_t* dst = codes + plane * sh.block * D;
+  const float before = scales[plane];
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) mx = max_abs2(max_abs2(max_abs2(max_abs2(mx, x[p].x), x[p].y), x[p].z), x[p].w);
   mx = max(mx & 0xffffu, mx >> 16);
@@ -89,26 +91,26 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
       uint32_t* w = reinterpret_cast<uint32_t*>(&c);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
+        float2 f0, f1;
+        kv_floats4(w[q], f0, f1);
+        // (scalar operations: of a packed product and sum ptxas makes one rounding)
+        const float p[4] = {f0.x, f0.y, f1.x, f1.y};
         uint32_t r[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          r[e] = __float_as_uint(__fadd_rn(__fmul_rn((float)(int8_t)(w[q] >> (8 * e)), ratio), 12582912.f));
+        for (int e = 0; e < 4; ++e) r[e] = __float_as_uint(__fadd_rn(__fmul_rn(p[e], ratio), 12582912.f));
         w[q] = kv_pack4(r[0], r[1], r[2], r[3]);
       }
       if (QALORA_CHECK(dbg, i, sh.block * (D / 16))) reinterpret_cast<uint4*>(dst)[i] = c;
     }
   }
-  const bool fast = !odd && kv_fast_scale(scale);
-  const float inv = fast ? __fdiv_rn(1.f, scale) : 0.f;
+  const float inv = !odd && kv_fast_scale(scale) ? __fdiv_rn(1.f, scale) : 0.f;
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const int slot = p * ROWS + row;
     if (slot < s0 || slot >= s1 || !QALORA_CHECK(dbg, slot, sh.block)) continue;
-    const float a[4] = {bf16_lo(x[p].x), bf16_hi(x[p].x), bf16_lo(x[p].y), bf16_hi(x[p].y)};
-    const float c[4] = {bf16_lo(x[p].z), bf16_hi(x[p].z), bf16_lo(x[p].w), bf16_hi(x[p].w)};
     uint2 out;
-    if (fast) { out.x = kv_codes4(a, scale, inv); out.y = kv_codes4(c, scale, inv); }
-    else { out.x = kv_codes4_any(a, scale); out.y = kv_codes4_any(c, scale); }
+    out.x = kv_codes4(make_float2(bf16_lo(x[p].x), bf16_hi(x[p].x)), make_float2(bf16_lo(x[p].y), bf16_hi(x[p].y)), scale, inv);
+    out.y = kv_codes4(make_float2(bf16_lo(x[p].z), bf16_hi(x[p].z)), make_float2(bf16_lo(x[p].w), bf16_hi(x[p].w)), scale, inv);
     *reinterpret_cast<uint2*>(dst + slot * D + chunk * 8) = out;
   }
   if (score != nullptr)
@@ -116,43 +118,56 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
       score[((long long)id * sh.kv_heads + h) * sh.block + slot] = 0.f;
 }
 
-// READ_ROWS tokens of one sequence per thread block; a thread converts 16 codes at a time.
-constexpr int READ_ROWS = 8;
-
-template <bool BF16>
+// One thread block per (block of tokens that is read from, kv head, sequence), half of it for keys and half for
+// values: one look-up and one scale each, 16 codes per thread and pass.
+template <int D, int PASSES, bool BF16>
 __global__ void __launch_bounds__(KV_THREADS)
 kv_read_kernel(KvShape sh, KvBatch kb, const int8_t* __restrict__ codes, const float* __restrict__ scales,
                void* __restrict__ k, void* __restrict__ v, int* dbg) {
-  const int b = blockIdx.y;
-  const int r0 = kb.starts[b], r1 = kb.starts[b + 1];
+  constexpr int CHUNKS = D / 16, ROWS = 128 / CHUNKS;
+  kv_begin();
+  const int b = blockIdx.y, h = blockIdx.x % sh.kv_heads, j = blockIdx.x / sh.kv_heads;
+  const int r0 = kb.starts[b], r1 = kb.starts[b + 1], first = kb.lens[b];         // (lens: position of the first token read)
   if (r0 < 0 || r1 < r0 || r1 > kb.m || r1 - r0 > kb.max_new) return;
-  const int row0 = blockIdx.x * READ_ROWS;
-  const int rows = r1 - r0 - row0 < READ_ROWS ? r1 - r0 - row0 : READ_ROWS;
-  if (rows <= 0) return;
-  const long long pos0 = (long long)kb.lens[b] + row0;          // (lens: position of the first token read)
-  const int per_head = sh.dim / 16, per_plane = sh.kv_heads * per_head, per_row = 2 * per_plane;
-  for (int i = threadIdx.x; i < rows * per_row; i += KV_THREADS) {
-    const int row = i / per_row, rest = i % per_row, which = rest / per_plane, col = rest % per_plane;
-    void* out = which == 0 ? k : v;
-    const long long pos = pos0 + row;
-    if (out == nullptr || pos < 0 || pos >= (long long)kb.max_blocks * sh.block) continue;
-    const int h = col / per_head, part = col % per_head, slot = (int)(pos % sh.block);
-    const int id = kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, (int)(pos / sh.block));
-    if (id < 0) continue;
-    const long long plane = ((long long)id * 2 + which) * sh.kv_heads + h;
-    if (!QALORA_CHECK(dbg, plane, (long long)sh.num_blocks * 2 * sh.kv_heads)) continue;
-    const float s = scales[plane];
-    const uint4 c = __ldcs(reinterpret_cast<const uint4*>(codes + (plane * sh.block + slot) * sh.dim + part * 16));
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    const long long at = ((long long)(r0 + row0 + row) * sh.kv_heads + h) * sh.dim + part * 16;
-    float f[16];
+  const long long stop = (long long)first + (r1 - r0), room = (long long)kb.max_blocks * sh.block;
+  const int lo = first > 0 ? first : 0, hi = (int)(stop < room ? stop : room);    // positions read: lo .. hi - 1
+  const int jb = (lo >> sh.log_block) + j, base = jb * sh.block;
+  if (base >= hi) return;
+  const int s0 = lo > base ? lo - base : 0, s1 = hi - base < sh.block ? hi - base : sh.block;
+  const int which = threadIdx.x >> 7, t = threadIdx.x & 127, chunk = t % CHUNKS, row = t / CHUNKS;
+  void* out = which == 0 ? k : v;
+  const int id = kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, jb);
+  if (id < 0 || out == nullptr) return;
+  const long long plane = ((long long)id * 2 + which) * sh.kv_heads + h;
+  const int8_t* src = codes + plane * sh.block * D + chunk * 16;
+  const float s = scales[plane];
+  uint4 c[PASSES];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) f[e] = __fmul_rn((float)(int8_t)(w[e >> 2] >> (8 * (e & 3))), s);
+  for (int p = 0; p < PASSES; ++p) {
+    const int slot = p * ROWS + row;
+    c[p] = make_uint4(0, 0, 0, 0);
+    if (slot >= s0 && slot < s1) c[p] = __ldcs(reinterpret_cast<const uint4*>(src + slot * D));
+  }
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int slot = p * ROWS + row;
+    const long long out_row = (long long)r0 + (base + slot - first);
+    if (slot < s0 || slot >= s1 || !QALORA_CHECK(dbg, out_row, kb.m)) continue;
+    const uint32_t w[4] = {c[p].x, c[p].y, c[p].z, c[p].w};
+    const long long at = (out_row * sh.kv_heads + h) * D + chunk * 16;
+    float2 f[8];
+    const float2 ss = make_float2(s, s);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      kv_floats4(w[e], f[2 * e], f[2 * e + 1]);
+      f[2 * e] = ptx::fmul2(f[2 * e], ss);
+      f[2 * e + 1] = ptx::fmul2(f[2 * e + 1], ss);
+    }
     if (BF16) {
       uint32_t o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const __nv_bfloat162 two = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+        const __nv_bfloat162 two = __floats2bfloat162_rn(f[e].x, f[e].y);
         o[e] = *reinterpret_cast<const uint32_t*>(&two);
       }
       uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out) + at);
@@ -161,9 +176,21 @@ kv_read_kernel(KvShape sh, KvBatch kb, const int8_t* __restrict__ codes, const f
     } else {
       float4* dst = reinterpret_cast<float4*>(static_cast<float*>(out) + at);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) __stcs(dst + e, make_float4(f[4 * e], f[4 * e + 1], f[4 * e + 2], f[4 * e + 3]));
+      for (int e = 0; e < 4; ++e) __stcs(dst + e, make_float4(f[2 * e].x, f[2 * e].y, f[2 * e + 1].x, f[2 * e + 1].y));
     }
   }
+}
+
+template <int D, bool BF16>
+int read_passes(const KvShape& sh, const KvBatch& b, dim3 grid, const int8_t* codes, const float* scales, void* k, void* v, cudaStream_t st) {
+  const int rows = 128 / (D / 16), passes = (sh.block + rows - 1) / rows;
+#define QALORA_KV_READ(P) \
+  case P: return kv_launch(kv_read_kernel<D, P, BF16>, grid, KV_THREADS, 0, st, sh, b, codes, scales, k, v, debug_words());
+  switch (passes) {
+    QALORA_KV_READ(1) QALORA_KV_READ(2) QALORA_KV_READ(4) QALORA_KV_READ(8)
+    default: return QALORA_ERR_UNSUPPORTED_SHAPE;
+  }
+#undef QALORA_KV_READ
 }
 
 template <int D>
@@ -172,25 +199,26 @@ int append_passes(const KvShape& sh, const KvBatch& b, dim3 grid, const __nv_bfl
   const int passes = sh.block * D / 1024;
 #define QALORA_KV_APPEND(P)                                                                                              \
   case P:                                                                                                                \
-    kv_append_kernel<D, P><<<grid, KV_THREADS, 0, st>>>(sh, b, k, k_stride, v, v_stride, codes, scales, score, dev_status, \
-                                                        debug_words());                                                  \
-    break;
+    return kv_launch(kv_append_kernel<D, P>, grid, KV_THREADS, 0, st, sh, b, k, (long long)k_stride, v, (long long)v_stride, codes, \
+                     scales, score, dev_status, debug_words());
   switch (passes) {
     QALORA_KV_APPEND(1) QALORA_KV_APPEND(2) QALORA_KV_APPEND(4) QALORA_KV_APPEND(8) QALORA_KV_APPEND(16)
     default: return QALORA_ERR_UNSUPPORTED_SHAPE;
   }
 #undef QALORA_KV_APPEND
-  count_launch();
-  return cuda_status(cudaGetLastError());
 }
 
 }  // namespace
 
+// Blocks that `n` consecutive tokens can lie in, wherever the first one lies in its block.
+static int touched_blocks(const KvShape& sh, const KvBatch& b, int n) {
+  const int touched = (n + sh.block - 2) / sh.block + 1;
+  return touched < b.max_blocks ? touched : b.max_blocks;
+}
+
 int launch_kv_append(const KvShape& sh, const KvBatch& b, const __nv_bfloat16* k, int64_t k_stride, const __nv_bfloat16* v,
                      int64_t v_stride, int8_t* codes, float* scales, float* score, int32_t* dev_status, cudaStream_t st) {
-  // blocks that max_new consecutive tokens can enter, wherever the first one lies in its block
-  const int touched = (b.max_new + sh.block - 2) / sh.block + 1;
-  const int bound = touched < b.max_blocks ? touched : b.max_blocks;
+  const int bound = touched_blocks(sh, b, b.max_new);
   if ((long long)bound * sh.kv_heads > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
   const dim3 grid((unsigned)(bound * sh.kv_heads), (unsigned)b.batch);
   return sh.dim == 128 ? append_passes<128>(sh, b, grid, k, k_stride, v, v_stride, codes, scales, score, dev_status, st)
@@ -199,11 +227,12 @@ int launch_kv_append(const KvShape& sh, const KvBatch& b, const __nv_bfloat16* k
 
 int launch_kv_read(const KvShape& sh, const KvBatch& b, const int8_t* codes, const float* scales, void* k, void* v, bool bf16,
                    cudaStream_t st) {
-  const dim3 grid((unsigned)((b.max_new + READ_ROWS - 1) / READ_ROWS), (unsigned)b.batch);
-  if (bf16) kv_read_kernel<true><<<grid, KV_THREADS, 0, st>>>(sh, b, codes, scales, k, v, debug_words());
-  else kv_read_kernel<false><<<grid, KV_THREADS, 0, st>>>(sh, b, codes, scales, k, v, debug_words());
-  count_launch();
-  return cuda_status(cudaGetLastError());
+  const int bound = touched_blocks(sh, b, b.max_new);
+  if ((long long)bound * sh.kv_heads > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
+  const dim3 grid((unsigned)(bound * sh.kv_heads), (unsigned)b.batch);
+  if (sh.dim == 128)
+    return bf16 ? read_passes<128, true>(sh, b, grid, codes, scales, k, v, st) : read_passes<128, false>(sh, b, grid, codes, scales, k, v, st);
+  return bf16 ? read_passes<64, true>(sh, b, grid, codes, scales, k, v, st) : read_passes<64, false>(sh, b, grid, codes, scales, k, v, st);
 }
 
 }  // namespace qalora

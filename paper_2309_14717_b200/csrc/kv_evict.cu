@@ -43,6 +43,7 @@ kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
   __shared__ uint32_t warp_part[SEL_WARPS], warp_gt[SEL_WARPS], warp_eq[SEL_WARPS];
   __shared__ uint32_t found[3];                 // bin, keys above it, keys in it
   __shared__ uint32_t share[2];                 // this block's keys above / at the threshold, read by its cluster
+  kv_begin();
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int pair = blockIdx.x / C, b = pair / sh.kv_heads, h = pair % sh.kv_heads;
@@ -63,8 +64,8 @@ kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
   if (want == 0) return;
   const int per = (cand + C - 1) / C, begin = rank * per, end = begin + per < cand ? begin + per : cand;
   auto fetch = [&](int t) -> uint32_t {
-    const int id = kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, t / sh.block);
-    return id < 0 ? 0u : score_key(a.score[((long long)id * sh.kv_heads + h) * sh.block + t % sh.block]);
+    const int id = kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, t >> sh.log_block);
+    return id < 0 ? 0u : score_key(a.score[((long long)id * sh.kv_heads + h) * sh.block + (t & (sh.block - 1))]);
   };
   if (a.cached) {
 #pragma unroll 4
@@ -101,8 +102,7 @@ kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
     }
     if (lane == 31) warp_part[warp] = sum;
     __syncthreads();
-    uint32_t before = 0;
-    for (int w = 0; w < warp; ++w) before += warp_part[w];
+    const uint32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? warp_part[lane] : 0u);
     const uint32_t above = before + sum - n0 - n1;                      // keys in larger bins than this thread's
     if (above < left && left <= above + n0) { found[0] = hi; found[1] = above; found[2] = n0; }
     else if (above + n0 < left && left <= above + n0 + n1) { found[0] = hi - 1; found[1] = above + n0; found[2] = n1; }
@@ -124,8 +124,8 @@ kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
   eq = __reduce_add_sync(0xffffffffu, eq);
   if (lane == 0) { warp_gt[warp] = gt; warp_eq[warp] = eq; }
   __syncthreads();
-  uint32_t gt0 = 0, eq0 = 0;
-  for (int w = 0; w < warp; ++w) { gt0 += warp_gt[w]; eq0 += warp_eq[w]; }
+  uint32_t gt0 = __reduce_add_sync(0xffffffffu, lane < warp ? warp_gt[lane] : 0u);
+  uint32_t eq0 = __reduce_add_sync(0xffffffffu, lane < warp ? warp_eq[lane] : 0u);
   if (warp == SEL_WARPS - 1 && lane == 0) { share[0] = gt0 + gt; share[1] = eq0 + eq; }
   cluster.sync();
   for (int r = 0; r < rank; ++r) {
@@ -157,6 +157,7 @@ kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__
                  const int32_t* __restrict__ dst_table, int dst_max_blocks, int* dbg) {
   constexpr int CHUNKS = D / 16, ROWS = 128 / CHUNKS;
   __shared__ float warp_max[8];
+  kv_begin();
   const int b = blockIdx.y, h = blockIdx.x % sh.kv_heads, j = blockIdx.x / sh.kv_heads;
   int len = kb.lens[b];
   len = len < 0 ? 0 : (len > kb.max_len ? kb.max_len : len);
@@ -177,21 +178,27 @@ kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__
     s[p] = 0.f;
     if (slot < n) {
       const int pos = from[slot];
-      const int id = QALORA_CHECK(dbg, pos, len) ? kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, pos / sh.block) : -1;
+      const int id = QALORA_CHECK(dbg, pos, len) ? kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, pos >> sh.log_block) : -1;
       if (id >= 0) {
         const long long plane = ((long long)id * 2 + which) * sh.kv_heads + h;
         s[p] = scales[plane];
-        x[p] = *reinterpret_cast<const uint4*>(codes + (plane * sh.block + pos % sh.block) * D + chunk * 16);
+        x[p] = *reinterpret_cast<const uint4*>(codes + (plane * sh.block + (pos & (sh.block - 1))) * D + chunk * 16);
       }
     }
   }
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const uint32_t w[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
-    int m = 0;
+    float m = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) m = max(m, abs((int)(int8_t)(w[e >> 2] >> (8 * (e & 3)))));
-    mx = fmaxf(mx, __fmul_rn((float)m, s[p]));          // (the rounded product grows with the code)
+    for (int q = 0; q < 4; ++q) {
+      float2 f0, f1;
+      kv_floats4(w[q], f0, f1);
+      m = fmaxf(fmaxf(m, fmaxf(fabsf(f0.x), fabsf(f0.y))), fmaxf(fabsf(f1.x), fabsf(f1.y)));
+    }
+    // (the codes are converted again below: kept as floats they would cost four times the registers)
+    asm volatile("" : "+r"(x[p].x), "+r"(x[p].y), "+r"(x[p].z), "+r"(x[p].w));
+    mx = fmaxf(mx, __fmul_rn(m, s[p]));                 // (the rounded product grows with the code)
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -201,28 +208,27 @@ kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__
   const float scale = __fdiv_rn(mx, 127.f);
   const long long plane = ((long long)dst_id * 2 + which) * sh.kv_heads + h;
   if (t == 0 && QALORA_CHECK(dbg, plane, (long long)sh.num_blocks * 2 * sh.kv_heads)) scales[plane] = scale;
-  const bool fast = kv_fast_scale(scale);
-  const float inv = fast ? __fdiv_rn(1.f, scale) : 0.f;
+  const float inv = kv_fast_scale(scale) ? __fdiv_rn(1.f, scale) : 0.f;
   int8_t* dst = codes + plane * sh.block * D;
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const int slot = p * ROWS + row;
     if (slot >= n || !QALORA_CHECK(dbg, slot, sh.block)) continue;
     const uint32_t w[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
+    const float2 ss = make_float2(s[p], s[p]);
     uint32_t o[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      float v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = __fmul_rn((float)(int8_t)(w[q] >> (8 * e)), s[p]);
-      o[q] = fast ? kv_codes4(v, scale, inv) : kv_codes4_any(v, scale);
+      float2 f0, f1;
+      kv_floats4(w[q], f0, f1);
+      o[q] = kv_codes4(ptx::fmul2(f0, ss), ptx::fmul2(f1, ss), scale, inv);
     }
     *reinterpret_cast<uint4*>(dst + slot * D + chunk * 16) = make_uint4(o[0], o[1], o[2], o[3]);
   }
   for (int slot = threadIdx.x; slot < n; slot += 256) {
     const int pos = from[slot];
-    const int id = QALORA_CHECK(dbg, pos, len) ? kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, pos / sh.block) : -1;
-    const float moved = id < 0 ? 0.f : score[((long long)id * sh.kv_heads + h) * sh.block + pos % sh.block];
+    const int id = QALORA_CHECK(dbg, pos, len) ? kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, pos >> sh.log_block) : -1;
+    const float moved = id < 0 ? 0.f : score[((long long)id * sh.kv_heads + h) * sh.block + (pos & (sh.block - 1))];
     score[((long long)dst_id * sh.kv_heads + h) * sh.block + slot] = moved;
   }
 }
@@ -233,16 +239,13 @@ int gather_passes(const KvShape& sh, const KvBatch& b, dim3 grid, int budget, co
   const int rows = 128 / (D / 16), passes = (sh.block + rows - 1) / rows;
 #define QALORA_KV_GATHER(P)                                                                                                  \
   case P:                                                                                                                    \
-    kv_gather_kernel<D, P><<<grid, 256, 0, st>>>(sh, b, budget, kept, codes, scales, score, dst_table, dst_max_blocks,       \
-                                                 debug_words());                                                            \
-    break;
+    return kv_launch(kv_gather_kernel<D, P>, grid, 256, 0, st, sh, b, budget, kept, codes, scales, score, dst_table,        \
+                     dst_max_blocks, debug_words());
   switch (passes) {
     QALORA_KV_GATHER(1) QALORA_KV_GATHER(2) QALORA_KV_GATHER(4) QALORA_KV_GATHER(8)
     default: return QALORA_ERR_UNSUPPORTED_SHAPE;
   }
 #undef QALORA_KV_GATHER
-  count_launch();
-  return cuda_status(cudaGetLastError());
 }
 
 }  // namespace
@@ -269,12 +272,14 @@ int launch_kv_evict(const KvShape& sh, const KvBatch& b, int budget, int recent,
   cfg.blockDim = dim3(SEL_THREADS);
   cfg.dynamicSmemBytes = a.cached ? (size_t)per * 4 : 0;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)C;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   if (cudaLaunchKernelEx(&cfg, kv_select_kernel, sh, b, a, debug_words()) != cudaSuccess) return QALORA_ERR_CUDA;
   count_launch();
   const int most = b.max_len < budget ? b.max_len : budget, blocks = (most + sh.block - 1) / sh.block;

@@ -227,6 +227,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const KvShape& sh = a.sh;
 
+  kv_begin();
   // the work of this block, the longest row tiles of the batch first
   const int per_pair = sh.kv_heads * a.kb.batch * a.splits;
   const int pair = pairs_max - 1 - (int)(blockIdx.x / per_pair), rest = blockIdx.x % per_pair;
@@ -487,7 +488,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       // tile before it is needed
       auto entry = [&](int it) {
         const int t0 = (first + it) * PT_TOK + lane * 16;
-        return lane < 8 && it < count && t0 < s.len ? a.kb.table[(size_t)b * a.kb.max_blocks + t0 / sh.block] : -1;
+        return lane < 8 && it < count && t0 < s.len ? a.kb.table[(size_t)b * a.kb.max_blocks + (t0 >> sh.log_block)] : -1;
       };
       struct Look { int id; float ks, vs; };
       auto look = [&](int raw) {
@@ -545,6 +546,7 @@ template <int D>
 __global__ void __launch_bounds__(256)
 kv_prompt_join_kernel(const __grid_constant__ PromptArgs a, int row_blocks, int* dbg) {
   constexpr int PER_ROW = D / 4, ROWS = 256 / PER_ROW;
+  kv_begin();
   const KvShape& sh = a.sh;
   const int b = blockIdx.y, h = blockIdx.x / row_blocks;
   const KvSeq s = kv_seq(a.kb, b);
@@ -602,6 +604,7 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, in
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::OFF_SLOT);
   volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_SLOT + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  kv_begin();
   const KvShape& sh = a.sh;
   const int b = blockIdx.y, h = blockIdx.x % sh.kv_heads, j = blockIdx.x / sh.kv_heads, t0 = j * PT_TOK;
   const KvSeq s = kv_seq(a.kb, b);
@@ -638,7 +641,7 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, in
         const int row = p * Map::ROWS + map.row0, t = t0 + row;
         uint4 c = make_uint4(0, 0, 0, 0);
         if (t < s.len) {
-          const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t / sh.block);
+          const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t >> sh.log_block);
           if (id >= 0)
             c = *reinterpret_cast<const uint4*>(a.at.codes + ((((long long)id * 2) * sh.kv_heads + h) * sh.block + (t & (sh.block - 1))) * D + map.piece * 16);
         }
@@ -649,7 +652,7 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, in
       if (lane == 0) ptx::mbar_arrive(k_full);
     }
     const int t = t0 + token;
-    const int id = t < s.len ? kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t / sh.block) : -1;
+    const int id = t < s.len ? kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t >> sh.log_block) : -1;
     const float ks = id >= 0 ? a.at.scales[((long long)id * 2) * sh.kv_heads + h] : 0.f;
     // the first row of this tile's first row tile that sees the token (rows before it are masked)
     const long long sees = t > s.first ? (long long)(t - s.first) * sh.group - (long long)rt0 * PT_ROWS : 0;
@@ -754,15 +757,15 @@ int prompt(const PromptArgs& a, cudaStream_t st) {
   if (blocks > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
   {
     MainKernelProbe probe("kv_prompt_kernel", st);
-    kv_prompt_kernel<D><<<(unsigned)blocks, PT_THREADS, PtSmem<D>::TOTAL, st>>>(a, pairs, debug_words());
+    ok = kv_launch(kv_prompt_kernel<D>, dim3((unsigned)blocks), PT_THREADS, (size_t)PtSmem<D>::TOTAL, st, a, pairs, debug_words());
   }
-  count_launch();
+  if (ok != QALORA_OK) return ok;
   if (a.splits > 1) {
     constexpr int ROWS = 256 / (D / 4);
     const int row_blocks = (int)((rows_max + ROWS - 1) / ROWS);
     if ((long long)row_blocks * sh.kv_heads > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
-    kv_prompt_join_kernel<D><<<dim3((unsigned)(row_blocks * sh.kv_heads), (unsigned)a.kb.batch), 256, 0, st>>>(a, row_blocks, debug_words());
-    count_launch();
+    ok = kv_launch(kv_prompt_join_kernel<D>, dim3((unsigned)(row_blocks * sh.kv_heads), (unsigned)a.kb.batch), 256, 0, st, a, row_blocks, debug_words());
+    if (ok != QALORA_OK) return ok;
   }
   if (a.at.score_out != nullptr && a.kb.max_len > 0) {
     ok = once_score.run([] {
@@ -771,10 +774,10 @@ int prompt(const PromptArgs& a, cudaStream_t st) {
     if (ok != QALORA_OK) return ok;
     const int tiles = (a.kb.max_len + PT_TOK - 1) / PT_TOK;
     if ((long long)tiles * sh.kv_heads > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
-    kv_prompt_score_kernel<D><<<dim3((unsigned)(tiles * sh.kv_heads), (unsigned)a.kb.batch), 320, PsSmem<D>::TOTAL, st>>>(a, tiles, debug_words());
-    count_launch();
+    return kv_launch(kv_prompt_score_kernel<D>, dim3((unsigned)(tiles * sh.kv_heads), (unsigned)a.kb.batch), 320, (size_t)PsSmem<D>::TOTAL, st, a,
+                     tiles, debug_words());
   }
-  return cuda_status(cudaGetLastError());
+  return QALORA_OK;
 }
 
 }  // namespace
