@@ -103,10 +103,7 @@ __device__ __forceinline__ int kv_block(const int32_t* table, int max_blocks, in
   return (id >= 0 && id < num_blocks) ? id : -1;
 }
 
-// Code of v under scale s > 0: clamp(rint(v / s), -127, 127) with the IEEE quotient.  v * (1/s) is
-// within 4e-5 of it for |v / s| <= 128 (two roundings of 2^-24 each), so that the division is
-// needed only where that product lies nearer than 1e-4 to a half-integer, where alone the two
-// could round apart.  `fast`: 1/s is neither zero nor infinite nor a subnormal.
+// Code of v under scale s > 0: clamp(rint(v / s), -127, 127) with the IEEE quotient.
 __device__ __forceinline__ float kv_code_div(float v, float s) {
   const float t = __fdiv_rn(v, s);
   return fminf(fmaxf(rintf(t), -127.f), 127.f);
@@ -126,8 +123,8 @@ __device__ __forceinline__ void kv_floats4(uint32_t w, float2& a, float2& b) {
   b = ptx::fsub2(make_float2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7542)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7543))), k);
 }
 
-// Four codes by division, for elements near a tie, scales whose inverse is not an ordinary number and elements that
-// may not be finite.  A call, not inlined: unrolled into every pass it made the kernels wait for instructions.
+// Four codes by division, for scales whose inverse is not an ordinary number and elements that may not be finite.  A
+// call, not inlined: unrolled into every pass it made the kernels wait for instructions.
 static __device__ __noinline__ uint32_t kv_codes4_any(float v0, float v1, float v2, float v3, float s) {
   const float v[4] = {v0, v1, v2, v3};
   uint32_t c[4];
@@ -135,16 +132,49 @@ static __device__ __noinline__ uint32_t kv_codes4_any(float v0, float v1, float 
   for (int i = 0; i < 4; ++i) c[i] = (s > 0.f && v[i] == v[i]) ? (uint32_t)(int)kv_code_div(v[i], s) : 0u;
   return kv_pack4(c[0], c[1], c[2], c[3]);
 }
-// Four codes; `inv` = 1 / s, or 0 where every element goes through the division.  The low byte of x / s + 1.5 * 2^23
-// is the rounded quotient in two's complement, so no float-to-integer conversion is needed.
-__device__ __forceinline__ uint32_t kv_codes4(float2 a, float2 b, float s, float inv) {
-  const float2 ii = make_float2(inv, inv), up = make_float2(12582912.f, 12582912.f), down = make_float2(-12582912.f, -12582912.f);
-  const float2 t0 = ptx::fmul2(a, ii), t1 = ptx::fmul2(b, ii);
-  const float2 u0 = ptx::fadd2(t0, up), u1 = ptx::fadd2(t1, up);
-  const float2 d0 = ptx::fsub2(t0, ptx::fadd2(u0, down)), d1 = ptx::fsub2(t1, ptx::fadd2(u1, down));
-  const float far = fmaxf(fmaxf(fabsf(d0.x), fabsf(d0.y)), fmaxf(fabsf(d1.x), fabsf(d1.y)));
-  if (!(far <= 0.4999f) || inv == 0.f) return kv_codes4_any(a.x, a.y, b.x, b.y, s);
-  return kv_pack4(__float_as_uint(u0.x), __float_as_uint(u0.y), __float_as_uint(u1.x), __float_as_uint(u1.y));
+// Eight elements under scale s, 1 / s correctly rounded in inv, to their codes.  The quotient is q = x * inv with two
+// corrections q += (x - q * s) * inv: the first brings q within a unit of its last place, and from there one
+// correction yields the correctly rounded quotient (P. Markstein, "Computation of elementary functions on the IBM
+// RISC System/6000 processor", 1990: the residual is exact, and inv is the correctly rounded reciprocal).  A check
+// whether x * inv lies near a tie, with a division where it does, took a third of the kernels' instructions: elements of
+// 8 significant bits over a scale of their own meet exact ties every few hundred elements.  The low byte of
+// q + 1.5 * 2^23 is the rounded quotient in two's complement: no float-to-integer conversion.
+__device__ __forceinline__ uint2 kv_codes8(const float2 (&x)[4], float s, float inv) {
+  const float2 ii = make_float2(inv, inv), ms = make_float2(-s, -s), up = make_float2(12582912.f, 12582912.f);
+  float2 u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float2 q = ptx::fmul2(x[i], ii);
+    q = ptx::ffma2(ptx::ffma2(q, ms, x[i]), ii, q);
+    q = ptx::ffma2(ptx::ffma2(q, ms, x[i]), ii, q);
+    u[i] = ptx::fadd2(q, up);
+  }
+  return make_uint2(kv_pack4(__float_as_uint(u[0].x), __float_as_uint(u[0].y), __float_as_uint(u[1].x), __float_as_uint(u[1].y)),
+                    kv_pack4(__float_as_uint(u[2].x), __float_as_uint(u[2].y), __float_as_uint(u[3].x), __float_as_uint(u[3].y)));
+}
+
+// Packed 16-bit maxima and minima in one instruction each.
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t max_s16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.s16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t min_s16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("min.s16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// Bytes 2 p and 2 p + 1 of w as signed 16-bit numbers (prmt's selector bit 3 repeats a byte's sign).
+template <int P>
+__device__ __forceinline__ uint32_t signed_pair(uint32_t w) {
+  uint32_t d;
+  asm("prmt.b32 %0, %1, 0, %2;" : "=r"(d) : "r"(w), "n"(P == 0 ? 0x9180 : 0xb3a2));
+  return d;
 }
 #endif
 

@@ -11,13 +11,13 @@ constexpr int KV_THREADS = 256;            // 128 threads for keys, 128 for valu
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ uint32_t max_abs2(uint32_t m, uint32_t w) { return __vmaxu2(m, w & 0x7fff7fffu); }
+__device__ __forceinline__ uint32_t max_abs2(uint32_t m, uint32_t w) { return max_u16x2(m, w & 0x7fff7fffu); }
 
 // One thread block per (block of tokens that new rows enter, kv head, sequence): the new rows of
 // that block stay in registers between the maximum and the rounding, so each element is read once.
 // PASSES rows of D elements per 128 / (D / 8) rows in flight: PASSES * 128 * 8 = block * D elements.
 template <int D, int PASSES>
-__global__ void __launch_bounds__(KV_THREADS)
+__global__ void __launch_bounds__(KV_THREADS, PASSES <= 8 ? 4 : 2)
 kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, long long k_stride,
                  const __nv_bfloat16* __restrict__ v, long long v_stride, int8_t* __restrict__ codes, float* __restrict__ scales,
                  float* __restrict__ score, int32_t* __restrict__ dev_status, int* dbg) {
@@ -37,17 +37,16 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
   const __nv_bfloat16* src = which == 0 ? k : v;
   const long long stride = which == 0 ? k_stride : v_stride;
 
+  const __nv_bfloat16* from = src + ((long long)s.row0 + (base + row - s.first)) * stride + (long long)h * D + chunk * 8;
+  const long long step = ROWS * stride;
   uint4 x[PASSES];
   uint32_t mx = 0;
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const int slot = p * ROWS + row;
     x[p] = make_uint4(0, 0, 0, 0);
-    if (slot >= s0 && slot < s1) {
-      const long long r = (long long)s.row0 + (base + slot - s.first);
-      if (QALORA_CHECK(dbg, r, kb.m))
-        x[p] = __ldcs(reinterpret_cast<const uint4*>(src + r * stride + (long long)h * D + chunk * 8));
-    }
+    if ((uint32_t)(slot - s0) < (uint32_t)(s1 - s0) && QALORA_CHECK(dbg, (long long)s.row0 + (base + slot - s.first), kb.m))
+      x[p] = __ldcs(reinterpret_cast<const uint4*>(from + p * step));
   }
   const int id = raw >= 0 && raw < sh.num_blocks ? raw : -1;      // (looked up while the rows are on their way)
   if (id < 0) return;
@@ -103,14 +102,19 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
       if (QALORA_CHECK(dbg, i, sh.block * (D / 16))) reinterpret_cast<uint4*>(dst)[i] = c;
     }
   }
-  const float inv = !odd && kv_fast_scale(scale) ? __fdiv_rn(1.f, scale) : 0.f;
+  const bool exact = odd || !kv_fast_scale(scale);
+  const float inv = exact ? 0.f : __fdiv_rn(1.f, scale);
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const int slot = p * ROWS + row;
-    if (slot < s0 || slot >= s1 || !QALORA_CHECK(dbg, slot, sh.block)) continue;
-    uint2 out;
-    out.x = kv_codes4(make_float2(bf16_lo(x[p].x), bf16_hi(x[p].x)), make_float2(bf16_lo(x[p].y), bf16_hi(x[p].y)), scale, inv);
-    out.y = kv_codes4(make_float2(bf16_lo(x[p].z), bf16_hi(x[p].z)), make_float2(bf16_lo(x[p].w), bf16_hi(x[p].w)), scale, inv);
+    if ((uint32_t)(slot - s0) >= (uint32_t)(s1 - s0) || !QALORA_CHECK(dbg, slot, sh.block)) continue;
+    const float2 e[4] = {make_float2(bf16_lo(x[p].x), bf16_hi(x[p].x)), make_float2(bf16_lo(x[p].y), bf16_hi(x[p].y)),
+                         make_float2(bf16_lo(x[p].z), bf16_hi(x[p].z)), make_float2(bf16_lo(x[p].w), bf16_hi(x[p].w))};
+    uint2 out = kv_codes8(e, scale, inv);
+    if (exact) {
+      out.x = kv_codes4_any(e[0].x, e[0].y, e[1].x, e[1].y, scale);
+      out.y = kv_codes4_any(e[2].x, e[2].y, e[3].x, e[3].y, scale);
+    }
     *reinterpret_cast<uint2*>(dst + slot * D + chunk * 8) = out;
   }
   if (score != nullptr)

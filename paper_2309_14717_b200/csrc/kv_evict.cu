@@ -188,16 +188,17 @@ kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__
   }
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
+    // largest magnitude of 16 codes, two at a time as signed 16-bit numbers
     const uint32_t w[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
-    float m = 0.f;
+    uint32_t hi = 0, lo = 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      float2 f0, f1;
-      kv_floats4(w[q], f0, f1);
-      m = fmaxf(fmaxf(m, fmaxf(fabsf(f0.x), fabsf(f0.y))), fmaxf(fabsf(f1.x), fabsf(f1.y)));
+      const uint32_t a = signed_pair<0>(w[q]), c = signed_pair<1>(w[q]);
+      hi = max_s16x2(max_s16x2(hi, a), c);
+      lo = min_s16x2(min_s16x2(lo, a), c);
     }
-    // (the codes are converted again below: kept as floats they would cost four times the registers)
-    asm volatile("" : "+r"(x[p].x), "+r"(x[p].y), "+r"(x[p].z), "+r"(x[p].w));
+    const int top = max((int)(int16_t)(hi & 0xffffu), (int)(int16_t)(hi >> 16)), low = min((int)(int16_t)(lo & 0xffffu), (int)(int16_t)(lo >> 16));
+    const float m = (float)max(top, -low);
     mx = fmaxf(mx, __fmul_rn(m, s[p]));                 // (the rounded product grows with the code)
   }
 #pragma unroll
@@ -208,7 +209,8 @@ kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__
   const float scale = __fdiv_rn(mx, 127.f);
   const long long plane = ((long long)dst_id * 2 + which) * sh.kv_heads + h;
   if (t == 0 && QALORA_CHECK(dbg, plane, (long long)sh.num_blocks * 2 * sh.kv_heads)) scales[plane] = scale;
-  const float inv = kv_fast_scale(scale) ? __fdiv_rn(1.f, scale) : 0.f;
+  const bool exact = !kv_fast_scale(scale);
+  const float inv = exact ? 0.f : __fdiv_rn(1.f, scale);
   int8_t* dst = codes + plane * sh.block * D;
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
@@ -216,14 +218,21 @@ kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__
     if (slot >= n || !QALORA_CHECK(dbg, slot, sh.block)) continue;
     const uint32_t w[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
     const float2 ss = make_float2(s[p], s[p]);
-    uint32_t o[4];
+    uint2 o[2];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      float2 f0, f1;
-      kv_floats4(w[q], f0, f1);
-      o[q] = kv_codes4(ptx::fmul2(f0, ss), ptx::fmul2(f1, ss), scale, inv);
+    for (int q = 0; q < 2; ++q) {
+      float2 f[4];
+      kv_floats4(w[2 * q], f[0], f[1]);
+      kv_floats4(w[2 * q + 1], f[2], f[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = ptx::fmul2(f[e], ss);
+      o[q] = kv_codes8(f, scale, inv);
+      if (exact) {
+        o[q].x = kv_codes4_any(f[0].x, f[0].y, f[1].x, f[1].y, scale);
+        o[q].y = kv_codes4_any(f[2].x, f[2].y, f[3].x, f[3].y, scale);
+      }
     }
-    *reinterpret_cast<uint4*>(dst + slot * D + chunk * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+    *reinterpret_cast<uint4*>(dst + slot * D + chunk * 16) = make_uint4(o[0].x, o[0].y, o[1].x, o[1].y);
   }
   for (int slot = threadIdx.x; slot < n; slot += 256) {
     const int pos = from[slot];
