@@ -13,6 +13,7 @@ namespace {
 
 constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
 constexpr int SEL_BINS = 2048;                  // 11 bits of the key per pass: 11 + 11 + 10
+constexpr int SEL_COARSE = SEL_BINS / 32;
 constexpr int SEL_MAX_CLUSTER = 8;
 constexpr int SEL_CACHED_KEYS = 49152;          // keys of one thread block that fit its shared memory (192 KiB)
 
@@ -27,7 +28,8 @@ struct SelectArgs {
   const float* score;
   int32_t* dst_lens;
   int32_t* kept;
-  int budget, recent, cached;
+  int budget, recent;
+  int cached;                                   // keys of a thread block that its shared memory holds, 0: they are read again
 };
 
 // One cluster per (sequence, kv head); its thread blocks share the candidates (all tokens but the
@@ -38,10 +40,10 @@ struct SelectArgs {
 // offsets, and the places come out in order.
 __global__ void __launch_bounds__(SEL_THREADS)
 kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
-  extern __shared__ uint32_t keys[];            // [per] when cached
+  extern __shared__ __align__(16) uint32_t keys[];   // [cached] when the keys fit
   __shared__ uint32_t hist[SEL_BINS];
-  __shared__ uint32_t warp_part[SEL_WARPS], warp_gt[SEL_WARPS], warp_eq[SEL_WARPS];
-  __shared__ uint32_t found[3];                 // bin, keys above it, keys in it
+  __shared__ uint32_t coarse[SEL_COARSE], warp_gt[SEL_WARPS], warp_eq[SEL_WARPS];
+  __shared__ uint32_t found[2];                 // bin, keys above it
   __shared__ uint32_t share[2];                 // this block's keys above / at the threshold, read by its cluster
   kv_begin();
   cg::cluster_group cluster = cg::this_cluster();
@@ -62,14 +64,20 @@ kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
   for (int i = rank * SEL_THREADS + tid; i < a.recent; i += C * SEL_THREADS)
     if (QALORA_CHECK(dbg, want + i, a.budget)) kept[want + i] = cand + i;
   if (want == 0) return;
-  const int per = (cand + C - 1) / C, begin = rank * per, end = begin + per < cand ? begin + per : cand;
+  const int per = ((cand + C - 1) / C + 3) & ~3, begin = rank * per, end = begin + per < cand ? begin + per : cand;
+  auto meet = [&] { if (C == 1) __syncthreads(); else cluster.sync(); };
   auto fetch = [&](int t) -> uint32_t {
     const int id = kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, t >> sh.log_block);
     return id < 0 ? 0u : score_key(a.score[((long long)id * sh.kv_heads + h) * sh.block + (t & (sh.block - 1))]);
   };
-  if (a.cached) {
+  if (a.cached) {                               // four neighbouring tokens, which lie in one block, at a time
 #pragma unroll 4
-    for (int t = begin + tid; t < end; t += SEL_THREADS) keys[t - begin] = fetch(t);
+    for (int t = begin + tid * 4; t < end; t += SEL_THREADS * 4) {
+      const int id = kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, t >> sh.log_block);
+      const float4 x = *reinterpret_cast<const float4*>(a.score + ((long long)(id < 0 ? 0 : id) * sh.kv_heads + h) * sh.block + (t & (sh.block - 1)));
+      const uint4 k = make_uint4(score_key(x.x), score_key(x.y), score_key(x.z), score_key(x.w));
+      if (QALORA_CHECK(dbg, t - begin + 3, a.cached)) *reinterpret_cast<uint4*>(keys + (t - begin)) = id < 0 ? make_uint4(0, 0, 0, 0) : k;
+    }
     __syncthreads();
   }
   auto key_at = [&](int t) -> uint32_t { return a.cached ? keys[t - begin] : fetch(t); };
@@ -85,28 +93,43 @@ kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
       const uint32_t key = key_at(t);
       if ((key & mask) == prefix) atomicAdd(&hist[(key >> SHIFT[p]) & digit_mask], 1u);
     }
-    cluster.sync();
-    // thread i owns the bins 2047 - 2i and 2046 - 2i: an inclusive scan over threads counts from the largest key down
-    uint32_t n0 = 0, n1 = 0;
-    const int hi = SEL_BINS - 1 - 2 * tid;
-    for (int r = 0; r < C; ++r) {
-      const uint32_t* other = cluster.map_shared_rank(hist, r);
-      n0 += other[hi];
-      n1 += other[hi - 1];
-    }
-    uint32_t sum = n0 + n1;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += up;
-    }
-    if (lane == 31) warp_part[warp] = sum;
     __syncthreads();
-    const uint32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? warp_part[lane] : 0u);
-    const uint32_t above = before + sum - n0 - n1;                      // keys in larger bins than this thread's
-    if (above < left && left <= above + n0) { found[0] = hi; found[1] = above; found[2] = n0; }
-    else if (above + n0 < left && left <= above + n0 + n1) { found[0] = hi - 1; found[1] = above + n0; found[2] = n1; }
-    cluster.sync();                                                     // (also: nobody reads this histogram any more)
+    // sums of 32 neighbouring bins, so that the cluster reads few words of each other's: 64 sums, then the 32 bins of one
+    for (int i = warp; i < SEL_COARSE; i += SEL_WARPS) {
+      const uint32_t n = __reduce_add_sync(0xffffffffu, hist[i * 32 + lane]);
+      if (lane == 0) coarse[i] = n;
+    }
+    meet();
+    if (warp == 0) {
+      // from the largest key down: the lane's bins are hi and hi - 1 of the sums, then one of the 32
+      auto total = [&](uint32_t* mine, int at) {
+        uint32_t part[SEL_MAX_CLUSTER], n = 0;                          // (all loads first: each takes some hundred cycles)
+#pragma unroll
+        for (int r = 0; r < SEL_MAX_CLUSTER; ++r) part[r] = r < C ? cluster.map_shared_rank(mine, r)[at] : 0u;
+#pragma unroll
+        for (int r = 0; r < SEL_MAX_CLUSTER; ++r) n += part[r];
+        return n;
+      };
+      auto inclusive = [&](uint32_t n) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t up = __shfl_up_sync(0xffffffffu, n, o);
+          if (lane >= o) n += up;
+        }
+        return n;
+      };
+      const int hi = SEL_COARSE - 1 - 2 * lane;
+      const uint32_t n0 = total(coarse, hi), n1 = total(coarse, hi - 1), above = inclusive(n0 + n1) - n0 - n1;
+      const bool first = above < left && left <= above + n0, second = above + n0 < left && left <= above + n0 + n1;
+      const uint32_t who = __ballot_sync(0xffffffffu, first || second);       // one lane: `left` keys at least match the prefix
+      const int from = __ffs(who) - 1;
+      const int group = __shfl_sync(0xffffffffu, first ? hi : hi - 1, from);
+      const uint32_t before = __shfl_sync(0xffffffffu, first ? above : above + n0, from);
+      const int bin = group * 32 + 31 - lane;
+      const uint32_t n = total(hist, bin), over = before + inclusive(n) - n;
+      if (over < left && left <= over + n) { found[0] = bin; found[1] = over; }
+    }
+    meet();                                                             // (also: nobody reads this histogram any more)
     prefix |= found[0] << SHIFT[p];
     mask |= digit_mask << SHIFT[p];
     left -= found[1];
@@ -127,7 +150,7 @@ kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
   uint32_t gt0 = __reduce_add_sync(0xffffffffu, lane < warp ? warp_gt[lane] : 0u);
   uint32_t eq0 = __reduce_add_sync(0xffffffffu, lane < warp ? warp_eq[lane] : 0u);
   if (warp == SEL_WARPS - 1 && lane == 0) { share[0] = gt0 + gt; share[1] = eq0 + eq; }
-  cluster.sync();
+  meet();
   for (int r = 0; r < rank; ++r) {
     const uint32_t* other = cluster.map_shared_rank(share, r);
     gt0 += other[0];
@@ -146,7 +169,7 @@ kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
     gt0 += __popc(bg);
     eq0 += __popc(be);
   }
-  cluster.sync();                               // a block's shared memory is read by its cluster until here
+  meet();                                       // a block's shared memory is read by its cluster until here
 }
 
 // One thread block per (destination block, kv head, sequence): 128 threads move the keys and 128 the
@@ -268,9 +291,9 @@ int launch_kv_evict(const KvShape& sh, const KvBatch& b, int budget, int recent,
   while (C < SEL_MAX_CLUSTER && ((b.max_len + C - 1) / C > SEL_CACHED_KEYS / 2 ||
                                  (pairs * C * 2 <= device_sm_count() && b.max_len / C >= 4096)))
     C *= 2;
-  const int per = (b.max_len + C - 1) / C;
+  const int per = ((b.max_len + C - 1) / C + 3) & ~3;
   if (pairs * C > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
-  SelectArgs a{score, dst_lens, kept, budget, recent, per <= SEL_CACHED_KEYS ? 1 : 0};
+  SelectArgs a{score, dst_lens, kept, budget, recent, per <= SEL_CACHED_KEYS ? per : 0};
   static PerDeviceOnce once;
   const int ok = once.run([] {
     return cudaFuncSetAttribute(kv_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_CACHED_KEYS * 4);
@@ -279,7 +302,7 @@ int launch_kv_evict(const KvShape& sh, const KvBatch& b, int budget, int recent,
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(pairs * C));
   cfg.blockDim = dim3(SEL_THREADS);
-  cfg.dynamicSmemBytes = a.cached ? (size_t)per * 4 : 0;
+  cfg.dynamicSmemBytes = (size_t)a.cached * 4;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
