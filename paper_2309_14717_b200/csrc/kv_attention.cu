@@ -13,7 +13,8 @@ namespace {
 
 constexpr int AT_WARPS = 4;                       // consumer warps; one more warp brings the tiles in
 constexpr int AT_THREADS = (AT_WARPS + 1) * 32;
-constexpr int AT_MAX_BATCH = 1024;                // sequences of one launch (the plan lies in shared memory)
+constexpr int AT_MAX_BATCH = 512;                 // sequences of one launch (their rows, lengths and units lie in shared memory)
+constexpr int JOIN_TOKENS = 512;                  // whose gathered weights a block of the second kernel adds up
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoMax = -1e30f;                  // running maximum of a row that has met no token
 constexpr float kGrow = 6.f;                      // a row is rescaled when its maximum has grown by 2^6 or more
@@ -34,34 +35,29 @@ struct AttnArgs {
   int units_grid;        // thread blocks of the first kernel
 };
 
-// Work is cut into units of TOK tokens of one (sequence, kv head, tile of ROWS rows), in this order;
-// every thread block takes the same number of consecutive units, whatever the sequences' lengths.
-template <int TOK, int ROWS>
-__device__ __forceinline__ void seq_units(const KvBatch& kb, const KvShape& sh, const KvSeq& s, int* row_tiles, int* tiles) {
-  *row_tiles = (s.n * sh.group + ROWS - 1) / ROWS;
-  *tiles = s.len > 0 ? (s.len + TOK - 1) / TOK : 1;           // (no tokens: one empty unit writes the zero rows)
+// Work is cut into units of TOK tokens of one (sequence, kv head), in this order; every thread block takes the same number
+// of consecutive units, whatever the sequences' lengths.
+template <int TOK>
+__device__ __forceinline__ int seq_tiles(const KvSeq& s) {
+  return s.n == 0 ? 0 : (s.len > 0 ? (s.len + TOK - 1) / TOK : 1);       // (rows without tokens: one empty unit writes zeros)
 }
 
 struct UnitPlace {
-  int b, h, rt, tile, tiles;
+  int b, h, tile, tiles;
 };
-template <int TOK, int ROWS>
-__device__ __forceinline__ UnitPlace find_unit(const AttnArgs& a, const uint32_t* prefix, uint32_t u) {
-  int lo = 0, hi = a.kb.batch;                                 // last b with prefix[b] <= u (its successor's is larger)
+template <int TOK>
+__device__ __forceinline__ UnitPlace find_unit(const uint32_t* prefix, const KvSeq* seqs, int batch, uint32_t u) {
+  int lo = 0, hi = batch;                                      // last b with prefix[b] <= u (its successor's is larger)
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (prefix[mid] <= u) lo = mid; else hi = mid;
   }
   UnitPlace p;
   p.b = lo;
-  const KvSeq s = kv_seq(a.kb, lo);
-  int row_tiles;
-  seq_units<TOK, ROWS>(a.kb, a.sh, s, &row_tiles, &p.tiles);
-  const uint32_t r = u - prefix[lo], per_head = (uint32_t)row_tiles * p.tiles;
-  p.h = (int)(r / per_head);
-  const uint32_t q = r % per_head;
-  p.rt = (int)(q / p.tiles);
-  p.tile = (int)(q % p.tiles);
+  p.tiles = seq_tiles<TOK>(seqs[lo]);
+  const uint32_t r = u - prefix[lo];
+  p.h = (int)(r / p.tiles);
+  p.tile = (int)(r % p.tiles);
   return p;
 }
 
@@ -77,8 +73,8 @@ struct AtSmem {
   static constexpr int OFF_ML = OFF_SCALES + STAGES * 2 * SUBS * 4;           // [AT_WARPS][ROWS][2]
   static constexpr int OFF_BARS = OFF_ML + AT_WARPS * ROWS * 2 * 4;
   static constexpr int OFF_FLAG = OFF_BARS + STAGES * 2 * 8;
-  static constexpr int OFF_PLAN = OFF_FLAG + 16;
-  static int total(int batch) { return OFF_PLAN + (batch + 2) * 4 + 1024; }   // (the window starts on a 1 KiB boundary)
+  static constexpr int OFF_SEQS = OFF_FLAG + 16;                              // [batch] KvSeq, then the plan
+  static int total(int batch) { return OFF_SEQS + batch * (int)sizeof(KvSeq) + (batch + 2) * 4 + 1024; }   // (the window starts on a 1 KiB boundary)
 };
 
 // Partial result `slot` = 2 * block + (0: the rows' units began in an earlier block, 1: they began here):
@@ -110,7 +106,8 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
   float* ml = reinterpret_cast<float*>(smem + S::OFF_ML);
   float* merge = reinterpret_cast<float*>(smem + S::OFF_MERGE);
   volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_FLAG);
-  uint32_t* prefix = reinterpret_cast<uint32_t*>(smem + S::OFF_PLAN);
+  KvSeq* seqs = reinterpret_cast<KvSeq*>(smem + S::OFF_SEQS);
+  uint32_t* prefix = reinterpret_cast<uint32_t*>(seqs + a.kb.batch);
   const uint32_t bars = sbase + S::OFF_BARS;
   auto full = [&](int s) { return bars + s * 16; };
   auto empty = [&](int s) { return bars + s * 16 + 8; };
@@ -132,9 +129,8 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       uint32_t n = 0;
       if (b0 + lane < a.kb.batch) {
         const KvSeq s = kv_seq(a.kb, b0 + lane);
-        int rt, tiles;
-        seq_units<TOK, ROWS>(a.kb, sh, s, &rt, &tiles);
-        n = (uint32_t)sh.kv_heads * rt * tiles;
+        seqs[b0 + lane] = s;
+        n = (uint32_t)sh.kv_heads * seq_tiles<TOK>(s);
       }
       uint32_t sum = n;
 #pragma unroll
@@ -164,10 +160,9 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     auto look = [&](uint32_t u) {
       Look l{-1, -1, 0.f, 0.f};
       if (u >= u1) return l;
-      const UnitPlace p = find_unit<TOK, ROWS>(a, prefix, u);
-      const KvSeq s = kv_seq(a.kb, p.b);
+      const UnitPlace p = find_unit<TOK>(prefix, seqs, a.kb.batch, u);
       const int t = p.tile * TOK + sub * 16;
-      if (t >= s.len) return l;
+      if (t >= seqs[p.b].len) return l;
       const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, p.b, t >> sh.log_block);
       if (id < 0) return l;
       const long long k_plane = ((long long)id * 2) * sh.kv_heads + p.h, v_plane = k_plane + sh.kv_heads;
@@ -186,18 +181,18 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         const int st = it % STAGES;
         if (it >= STAGES) ok = __all_sync(0xffffffffu, ptx::mbar_wait(empty(st), ((it / STAGES) - 1) & 1, flag));
         if (!ok) break;
-        const bool mine = lane / SUBS == i;
-        if (mine) { scale_ring[st * 2 * SUBS + sub] = cur.ks; scale_ring[st * 2 * SUBS + SUBS + sub] = cur.vs; }
-        const bool issues = mine && cur.k_row >= 0 && (sub * 16) % box == 0;
+        // the copies first: they need only the block, the scales may still be on their way
+        const bool mine = lane / SUBS == i, issues = mine && cur.k_row >= 0 && (sub * 16) % box == 0;
         const int boxes = __popc(__ballot_sync(0xffffffffu, issues));
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive_expect_tx(full(st), (uint32_t)(boxes * 2 * box * D));
-        __syncwarp();
         if (issues) {
           const uint32_t at = sbase + st * 2 * S::TILE + sub * 16 * D;
           ptx::tma_load_2d(at, &map, 0, cur.k_row, full(st));
           ptx::tma_load_2d(at + S::TILE, &map, 0, cur.v_row, full(st));
         }
+        if (mine) { scale_ring[st * 2 * SUBS + sub] = cur.ks; scale_ring[st * 2 * SUBS + SUBS + sub] = cur.vs; }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_expect_tx(full(st), (uint32_t)(boxes * 2 * box * D));
+        __syncwarp();
       }
       cur = next;
     }
@@ -212,20 +207,18 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     UnitPlace p{};
     KvSeq s{};
     bool fresh = true, ok = true;
-    int rows = 0, limit_lo = 0;
+    int rows = 0;
     for (uint32_t u = u0, it = 0; u < u1; ++u, ++it) {
       if (fresh) {
-        p = find_unit<TOK, ROWS>(a, prefix, u);
-        s = kv_seq(a.kb, p.b);
-        rows = s.n * sh.group - p.rt * ROWS;
-        if (rows > ROWS) rows = ROWS;
-        limit_lo = s.first + (p.rt * ROWS) / sh.group;                 // the earliest row's
+        p = find_unit<TOK>(prefix, seqs, a.kb.batch, u);
+        s = seqs[p.b];
+        rows = s.n * sh.group;
         ref = inv_ref = 0.f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           // this lane's part of row g8 of the tile, as the B operand
-          const int mine = nt * 8 + g8, r = p.rt * ROWS + mine, i = r / sh.group, g = r % sh.group;
-          const bool load = mine < rows && QALORA_CHECK(dbg, s.row0 + i, a.kb.m);
+          const int r = nt * 8 + g8, i = r / sh.group, g = r % sh.group;
+          const bool load = r < rows && QALORA_CHECK(dbg, s.row0 + i, a.kb.m);
           const __nv_bfloat16* src = a.at.q + (long long)(s.row0 + i) * a.at.q_stride + (long long)(p.h * sh.group + g) * D;
           uint2 w[KSTEPS];
           uint32_t mx = 0;
@@ -250,13 +243,13 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           // and what belongs to the rows 2 q4, 2 q4 + 1 whose scores this lane holds
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            const int own = nt * 8 + q4 * 2 + c, ro = p.rt * ROWS + own, io = ro / sh.group;
+            const int own = nt * 8 + q4 * 2 + c, io = own / sh.group;
             q_scale[nt][c] = __shfl_sync(0xffffffffu, back, (q4 * 2 + c) * 4);
             limit[nt][c] = own < rows ? s.first + io : -1;
             mrow[nt][c] = kNoMax;
             lrow[nt][c] = 0.f;
             logit_row[nt][c] = a.logits != nullptr && own < rows
-                                   ? a.logits + ((long long)((a.batch0 + p.b) * a.kb.n_hi + io) * sh.heads + p.h * sh.group + ro % sh.group) *
+                                   ? a.logits + ((long long)((a.batch0 + p.b) * a.kb.n_hi + io) * sh.heads + p.h * sh.group + own % sh.group) *
                                                     a.logit_stride
                                    : nullptr;
           }
@@ -297,7 +290,7 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           }
         }
         // scaled scores in powers of two, masked
-        const bool edge = t0 + 15 > limit_lo || rows < ROWS;
+        const bool edge = t0 + 15 > s.first || rows < ROWS;             // (the first row sees the least)
         bool grow = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -373,10 +366,10 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       if (lane == 0) ptx::mbar_arrive(empty(st));
 
       if (++p.tile == p.tiles || u + 1 == u1) {
-        // ---- the row tile ends here, or goes on in the next block: the warps' shares are added up
-        const uint32_t row_tile_first = u + 1 - p.tile;          // unit of its tile 0
-        const bool whole = row_tile_first >= u0 && p.tile == p.tiles;
-        const int slot = 2 * (int)blockIdx.x + (row_tile_first < u0 ? 0 : 1);
+        // ---- the rows' tokens end here, or go on in the next block: the warps' shares are added up
+        const uint32_t first_unit = u + 1 - p.tile;          // their unit of tile 0
+        const bool whole = first_unit >= u0 && p.tile == p.tiles;
+        const int slot = 2 * (int)blockIdx.x + (first_unit < u0 ? 0 : 1);
         float* part = a.parts + slot * part_floats<D, ROWS>();
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -408,7 +401,7 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
             x.x = fmaf(by, y.x, x.x); x.y = fmaf(by, y.y, x.y); x.z = fmaf(by, y.z, x.z); x.w = fmaf(by, y.w, x.w);
           }
           if (whole) {
-            const int rr = p.rt * ROWS + r, i_new = rr / sh.group, head = p.h * sh.group + rr % sh.group;
+            const int i_new = r / sh.group, head = p.h * sh.group + r % sh.group;
             const long long at = (long long)(s.row0 + i_new) * sh.heads + head;
             if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) continue;
             kvp::store_row4(a.at.out + at * D + d, x, l);
@@ -429,93 +422,111 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
   if (*flag != 0 && lane == 0) *a.status = 1;
 }
 
-// Joins the partial results of row tiles that several blocks shared (first blocks of the grid), and
-// adds up the gathered weights from the stored scores (the other blocks).
+// Joins the partial results of rows that several blocks shared (first blocks of the grid, one per row: the tokens of a
+// long sequence lie in up to some hundred parts), and adds up the gathered weights from the stored scores (the
+// other blocks, JOIN_TOKENS tokens of one kv head each).
 template <int D, int ROWS, int TOK>
 __global__ void __launch_bounds__(128)
-kv_join_kernel(const __grid_constant__ AttnArgs a, int join_blocks, int row_tiles_max, int* dbg) {
-  __shared__ float row_lse[1024];
+kv_join_kernel(const __grid_constant__ AttnArgs a, int row_blocks, int* dbg) {
+  __shared__ float row_lse[ROWS];
+  __shared__ float4 share[4][32];
   kv_begin();
   const KvShape& sh = a.sh;
-  const int b = blockIdx.y, tid = threadIdx.x;
+  const int b = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const bool scores = (int)blockIdx.x >= row_blocks;
+  const int x = scores ? (int)blockIdx.x - row_blocks : (int)blockIdx.x, h = x % sh.kv_heads;
+  const int t0 = scores ? x / sh.kv_heads * JOIN_TOKENS : 0, row = scores ? 0 : x / sh.kv_heads;
   const KvSeq s = kv_seq(a.kb, b);
-  if (s.n == 0) return;
-  const uint32_t per_block = a.plan[a.kb.batch + 1], first = a.plan[b];
-  int row_tiles, tiles;
-  seq_units<TOK, ROWS>(a.kb, sh, s, &row_tiles, &tiles);
-  if ((int)blockIdx.x < join_blocks) {
-    const int h = blockIdx.x / row_tiles_max, rt = blockIdx.x % row_tiles_max;
-    if (rt >= row_tiles) return;
-    const uint32_t f = first + ((uint32_t)h * row_tiles + rt) * tiles;
-    const uint32_t c0 = f / per_block, c1 = (f + tiles - 1) / per_block;
-    if (c0 == c1) return;                                       // one block had all of it
-    const int rows = s.n * sh.group - rt * ROWS < ROWS ? s.n * sh.group - rt * ROWS : ROWS;
-    for (int i = tid; i < rows * (D / 4); i += 128) {
-      const int r = i / (D / 4), d = (i % (D / 4)) * 4;
-      float mx = kNoMax, l = 0.f;
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (uint32_t c = c0; c <= c1; ++c) {                     // in the order of the tokens
-        const float* part = a.parts + (2ll * c + (f < c * per_block ? 0 : 1)) * part_floats<D, ROWS>();
-        const float2 v = *reinterpret_cast<const float2*>(part + 2 * r);
-        const float4 y = *reinterpret_cast<const float4*>(part + 2 * ROWS + r * D + d);
-        const float top = fmaxf(mx, v.x), b0 = exp2f(mx - top), b1 = exp2f(v.x - top);
-        l = l * b0 + v.y * b1;
-        x.x = x.x * b0 + y.x * b1; x.y = x.y * b0 + y.y * b1; x.z = x.z * b0 + y.z * b1; x.w = x.w * b0 + y.w * b1;
-        mx = top;
-      }
-      const int rr = rt * ROWS + r, tok = s.row0 + rr / sh.group, head = h * sh.group + rr % sh.group;
-      const long long at = (long long)tok * sh.heads + head;
-      if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) continue;
-      kvp::store_row4(a.at.out + at * D + d, x, l);
-      if (d == 0) kvp::store_lse(a.at.lse, at, nullptr, 0, mx, l, kLift);
+  const int rows = s.n * sh.group;
+  if (row >= rows) return;                                      // (also: no rows)
+  const uint32_t per_block = a.plan[a.kb.batch + 1];
+  const int tiles = seq_tiles<TOK>(s);
+  const uint32_t f = a.plan[b] + (uint32_t)h * tiles, c0 = f / per_block, c1 = (f + tiles - 1) / per_block;
+  if (scores ? t0 >= s.len : c0 == c1) return;                  // (c0 == c1: one block had all of it)
+  auto part_of = [&](uint32_t c) { return a.parts + (2ll * c + (f < c * per_block ? 0 : 1)) * part_floats<D, ROWS>(); };
+  // maximum and sum of row r over the parts, by one warp
+  auto stats = [&](int r, float& mx, float& l) {
+    mx = kNoMax;
+    l = 0.f;
+    for (uint32_t c = c0 + lane; c <= c1; c += 32) {
+      const float2 v = *reinterpret_cast<const float2*>(part_of(c) + 2 * r);
+      const float top = fmaxf(mx, v.x);
+      l = l * exp2f(mx - top) + v.y * exp2f(v.x - top);
+      mx = top;
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float m2 = __shfl_xor_sync(0xffffffffu, mx, o), l2 = __shfl_xor_sync(0xffffffffu, l, o), top = fmaxf(mx, m2);
+      l = l * exp2f(mx - top) + l2 * exp2f(m2 - top);
+      mx = top;
+    }
+  };
+  if (!scores) {
+    constexpr int LANES = D / 4, SHARES = 128 / LANES;          // lanes of a row's output; shares of its parts
+    float mx, l;
+    stats(row, mx, l);
+    const int who = tid / LANES, d = (tid % LANES) * 4;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (uint32_t c = c0 + who; c <= c1; c += SHARES) {
+      const float* part = part_of(c);
+      const float by = exp2f(part[2 * row] - mx);
+      const float4 v = *reinterpret_cast<const float4*>(part + 2 * ROWS + row * D + d);
+      y.x = fmaf(v.x, by, y.x); y.y = fmaf(v.y, by, y.y); y.z = fmaf(v.z, by, y.z); y.w = fmaf(v.w, by, y.w);
+    }
+    share[warp][lane] = y;
+    __syncthreads();
+    if (tid >= LANES) return;
+    y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < SHARES; ++i) {
+      const float4 v = (&share[0][0])[i * LANES + tid];
+      y.x += v.x; y.y += v.y; y.z += v.z; y.w += v.w;
+    }
+    const long long at = (long long)(s.row0 + row / sh.group) * sh.heads + h * sh.group + row % sh.group;
+    if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) return;
+    kvp::store_row4(a.at.out + at * D + d, y, l);
+    if (d == 0) kvp::store_lse(a.at.lse, at, nullptr, 0, mx, l, kLift);
     return;
   }
-  // gathered weights: 512 tokens of one kv head, four per thread
-  const int idx = (int)blockIdx.x - join_blocks, h = idx % sh.kv_heads, t0 = (idx / sh.kv_heads) * 512;
-  if (t0 >= s.len) return;
-  const int rows = s.n * sh.group, t = t0 + tid * 4;
-  float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int r0 = 0; r0 < rows; r0 += 1024) {
-    __syncthreads();
-    for (int r = r0 + tid; r < rows && r < r0 + 1024; r += 128) {
-      const int rt = r / ROWS;
-      const uint32_t f = first + ((uint32_t)h * row_tiles + rt) * tiles;
-      const uint32_t c0 = f / per_block, c1 = (f + tiles - 1) / per_block;
-      float v = 0.f;
-      if (c0 == c1) v = a.lse2[(long long)((a.batch0 + b) * a.kb.n_hi + r / sh.group) * sh.heads + h * sh.group + r % sh.group];
-      else {
-        float mx = kNoMax, l = 0.f;
-        for (uint32_t c = c0; c <= c1; ++c) {
-          const float* part = a.parts + (2ll * c + (f < c * per_block ? 0 : 1)) * part_floats<D, ROWS>();
-          const float2 q = *reinterpret_cast<const float2*>(part + 2 * (r % ROWS));
-          const float top = fmaxf(mx, q.x);
-          l = l * exp2f(mx - top) + q.y * exp2f(q.x - top);
-          mx = top;
-        }
-        v = l > 0.f ? mx - kLift + log2f(l) : INFINITY;
-      }
-      row_lse[r - r0] = v;
+  if (c0 != c1) {
+    for (int r = warp; r < rows; r += 4) {
+      float mx, l;
+      stats(r, mx, l);
+      if (lane == 0) row_lse[r] = l > 0.f ? mx - kLift + log2f(l) : INFINITY;
     }
-    __syncthreads();
-    if (t < s.len) {
-      const int stop = rows - r0 < 1024 ? rows - r0 : 1024;
-      for (int r = 0; r < stop; ++r) {
-        const long long at = (long long)((a.batch0 + b) * a.kb.n_hi + (r0 + r) / sh.group) * sh.heads + h * sh.group + (r0 + r) % sh.group;
-        const float4 x = __ldcs(reinterpret_cast<const float4*>(a.logits + at * a.logit_stride + t));
-        const float n = row_lse[r];
-        w.x += kvp::exp2_fast(x.x - n); w.y += kvp::exp2_fast(x.y - n);
-        w.z += kvp::exp2_fast(x.z - n); w.w += kvp::exp2_fast(x.w - n);
-      }
-    }
+  } else if (tid < rows) {
+    row_lse[tid] = a.lse2[(long long)((a.batch0 + b) * a.kb.n_hi + tid / sh.group) * sh.heads + h * sh.group + tid % sh.group];
   }
+  __syncthreads();
+  const float* logits = a.logits + ((long long)(a.batch0 + b) * a.kb.n_hi * sh.heads + h * sh.group) * a.logit_stride;
+  const long long skip = (long long)(sh.heads - sh.group) * a.logit_stride;      // from one new token's last head to the next one's first
+  const int t = t0 + tid * 4;                                   // four tokens per thread
   if (t >= s.len) return;
   const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t >> sh.log_block);
+  const float* at_row = logits + t;
+  float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0, r = 0; i < s.n; ++i, at_row += skip) {
+#pragma unroll 8
+    for (int g = 0; g < sh.group; ++g, ++r, at_row += a.logit_stride) {
+      const float4 v = __ldcs(reinterpret_cast<const float4*>(at_row));
+      const float n = row_lse[r];
+      w.x += kvp::exp2_fast(v.x - n); w.y += kvp::exp2_fast(v.y - n);
+      w.z += kvp::exp2_fast(v.z - n); w.w += kvp::exp2_fast(v.w - n);
+    }
+  }
   if (id < 0) return;
   const long long at = ((long long)id * sh.kv_heads + h) * sh.block + (t & (sh.block - 1));
-  const float got[4] = {w.x, w.y, w.z, w.w};
-  for (int c = 0; c < 4 && t + c < s.len; ++c)
-    a.at.score_out[at + c] = (a.at.score_in != nullptr ? a.at.score_in[at + c] : 0.f) + got[c];
+  if (t + 4 <= s.len) {
+    if (a.at.score_in != nullptr) {
+      const float4 v = *reinterpret_cast<const float4*>(a.at.score_in + at);
+      w.x += v.x; w.y += v.y; w.z += v.z; w.w += v.w;
+    }
+    *reinterpret_cast<float4*>(a.at.score_out + at) = w;
+  } else {                                                      // the sequence ends inside
+    const float got[4] = {w.x, w.y, w.z, w.w};
+    for (int c = 0; t + c < s.len; ++c) a.at.score_out[at + c] = (a.at.score_in != nullptr ? a.at.score_in[at + c] : 0.f) + got[c];
+  }
 }
 
 // keys and values as one matrix of rows of `dim` bytes; a box is the part of a block that a unit takes
@@ -547,10 +558,10 @@ int attend(const AttnArgs& a, cudaStream_t st) {
     r = kv_launch(kv_attend_kernel<D, NT, SUB>, dim3((unsigned)a.units_grid), AT_THREADS, (size_t)S::total(a.kb.batch), st, map, a, debug_words());
   }
   if (r != QALORA_OK) return r;
-  const int row_tiles = (a.kb.max_new * a.sh.group + S::ROWS - 1) / S::ROWS, join = a.sh.kv_heads * row_tiles;
-  const int score_blocks = a.logits != nullptr ? a.sh.kv_heads * ((a.kb.max_len + 511) / 512) : 0;
-  return kv_launch(kv_join_kernel<D, S::ROWS, S::TOK>, dim3((unsigned)(join + score_blocks), (unsigned)a.kb.batch), 128, 0, st, a, join,
-                   row_tiles, debug_words());
+  const int row_blocks = a.sh.kv_heads * a.kb.max_new * a.sh.group;
+  const int score_blocks = a.logits != nullptr ? a.sh.kv_heads * ((a.kb.max_len + JOIN_TOKENS - 1) / JOIN_TOKENS) : 0;
+  return kv_launch(kv_join_kernel<D, S::ROWS, S::TOK>, dim3((unsigned)(row_blocks + score_blocks), (unsigned)a.kb.batch), 128, 0, st, a,
+                   row_blocks, debug_words());
 }
 
 struct AttnLayout {
@@ -611,7 +622,7 @@ int launch_few(const KvShape& sh, const KvBatch& b, const KvAttention& at, const
   a.logit_stride = (long long)round_up((size_t)max_len, 128);
   const int nt = column_tiles(sh, L.few), tok = sh.dim == 128 ? 64 : 128;
   const long long tiles = b.max_len > 0 ? (b.max_len + tok - 1) / tok : 1;
-  const long long per_seq = tiles * sh.kv_heads * ((L.few * (long long)sh.group + 8 * nt - 1) / (8 * nt));
+  const long long per_seq = tiles * sh.kv_heads;
   if (per_seq > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
   // sequences of one launch: their plan fits shared memory and their units 31 bits
   const long long fit = 0x7fffffffll / per_seq;
