@@ -157,28 +157,25 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     constexpr int AHEAD = 32 / SUBS;
     const int sub = lane % SUBS, box = sh.block < TOK ? sh.block : TOK;
     struct Look { int k_row, v_row; float ks, vs; };
+    // (no branch hangs on what is loaded: nothing waits here)
     auto look = [&](uint32_t u) {
-      Look l{-1, -1, 0.f, 0.f};
-      if (u >= u1) return l;
-      const UnitPlace p = find_unit<TOK>(prefix, seqs, a.kb.batch, u);
+      const UnitPlace p = find_unit<TOK>(prefix, seqs, a.kb.batch, u < u1 ? u : u1 - 1);
       const int t = p.tile * TOK + sub * 16;
-      if (t >= seqs[p.b].len) return l;
-      const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, p.b, t >> sh.log_block);
-      if (id < 0) return l;
-      const long long k_plane = ((long long)id * 2) * sh.kv_heads + p.h, v_plane = k_plane + sh.kv_heads;
-      l.ks = a.at.scales[k_plane];
-      l.vs = a.at.scales[v_plane];
-      l.k_row = (int)(k_plane * sh.block + (t & (sh.block - 1)));
-      l.v_row = (int)(v_plane * sh.block + (t & (sh.block - 1)));
-      return l;
+      const bool in = u < u1 && t < seqs[p.b].len;
+      const int entry = in ? a.kb.table[(size_t)p.b * a.kb.max_blocks + (t >> sh.log_block)] : -1;
+      const bool valid = entry >= 0 && entry < sh.num_blocks;
+      const long long k_plane = ((long long)(valid ? entry : 0) * 2) * sh.kv_heads + p.h, v_plane = k_plane + sh.kv_heads;
+      const float ks = a.at.scales[k_plane], vs = a.at.scales[v_plane];
+      const int at = t & (sh.block - 1);
+      return Look{valid ? (int)(k_plane * sh.block + at) : -1, (int)(v_plane * sh.block + at), valid ? ks : 0.f, valid ? vs : 0.f};
     };
-    Look cur = look(u0 + lane / SUBS);
+    Look cur = look(u0 + lane / SUBS), next = cur;
     uint32_t it = 0;
     bool ok = true;
     for (uint32_t base = u0; base < u1 && ok; base += AHEAD) {
-      const Look next = look(base + AHEAD + lane / SUBS);
       for (int i = 0; i < AHEAD && base + i < u1; ++i, ++it) {
         const int st = it % STAGES;
+        if (i == (STAGES < AHEAD ? STAGES : AHEAD) - 1) next = look(base + AHEAD + lane / SUBS);   // (not before the first copies are out)
         if (it >= STAGES) ok = __all_sync(0xffffffffu, ptx::mbar_wait(empty(st), ((it / STAGES) - 1) & 1, flag));
         if (!ok) break;
         // the copies first: they need only the block, the scales may still be on their way
@@ -264,64 +261,75 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       ok = ok && ptx::mbar_wait(full(st), (it / STAGES) & 1, flag);
       ok = __all_sync(0xffffffffu, ok);
       const uint32_t k_base = sbase + st * 2 * S::TILE, v_base = k_base + S::TILE;
-#pragma unroll 1
-      for (int sb = 0; sb < SUB; ++sb) {
-        const int sub = sb * AT_WARPS + warp, t0 = p.tile * TOK + sub * 16;
-        if (t0 >= s.len || !ok) break;
-        const float ks = scale_ring[st * 2 * SUBS + sub], vs = scale_ring[st * 2 * SUBS + SUBS + sub];
-        // scores of 16 tokens: rows of the product are tokens g8 and g8 + 8
-        float sc[NT][4];
+      const int sub0 = warp * SUB, t0 = p.tile * TOK + sub0 * 16;        // this warp's SUB * 16 tokens of the unit
+      if (t0 < s.len && ok) {
+        float ks[SUB], vs[SUB], sc[SUB][NT][4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int g = 0; g < SUB; ++g) {                // (a group behind the sequence's end has scales of 0 and is masked)
+          ks[g] = scale_ring[st * 2 * SUBS + sub0 + g];
+          vs[g] = scale_ring[st * 2 * SUBS + SUBS + sub0 + g];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) sc[nt][c] = 0.f;
-        const int tok = sub * 16 + (lane & 15);        // ldmatrix: lanes 0-15 the tokens of one chunk, 16-31 of the next
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int c2 = 0; c2 < D / 32; ++c2) {
-          uint32_t r[4];
-          kvp::ldmatrix_x4(r, k_base + kvp::swizzled<D>(tok, c2 * 2 + (lane >> 4)));
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            uint32_t f[4];                             // {token g8, +8} x {channels 0-1, 2-3 of the lane's four}
-            kvp::codes_to_half(r[2 * x], f[0], f[2]);
-            kvp::codes_to_half(r[2 * x + 1], f[1], f[3]);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) kvp::mma16816(sc[nt], f, qf[nt][c2 * 2 + x][0], qf[nt][c2 * 2 + x][1]);
-          }
+            for (int c = 0; c < 4; ++c) sc[g][nt][c] = 0.f;
         }
+        // scores: rows of the product are tokens g8 and g8 + 8 of a group
+        const int tok = sub0 * 16 + (lane & 15);       // ldmatrix: lanes 0-15 the tokens of one chunk, 16-31 of the next
+#pragma unroll
+        for (int c2 = 0; c2 < D / 32; ++c2)
+#pragma unroll
+          for (int g = 0; g < SUB; ++g) {
+            uint32_t r[4];
+            kvp::ldmatrix_x4(r, k_base + kvp::swizzled<D>(tok + g * 16, c2 * 2 + (lane >> 4)));
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              uint32_t f[4];                           // {token g8, +8} x {channels 0-1, 2-3 of the lane's four}
+              kvp::codes_to_half(r[2 * x], f[0], f[2]);
+              kvp::codes_to_half(r[2 * x + 1], f[1], f[3]);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) kvp::mma16816(sc[g][nt], f, qf[nt][c2 * 2 + x][0], qf[nt][c2 * 2 + x][1]);
+            }
+          }
         // scaled scores in powers of two, masked
-        const bool edge = t0 + 15 > s.first || rows < ROWS;             // (the first row sees the least)
+        const bool edge = t0 + SUB * 16 - 1 > s.first || rows < ROWS;    // (the first row sees the least)
         bool grow = false;
+        float v_top = vs[0];
+#pragma unroll
+        for (int g = 1; g < SUB; ++g) v_top = fmaxf(v_top, vs[g]);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const float f = q_scale[nt][c] * ks;
-            float &x0 = sc[nt][c], &x1 = sc[nt][2 + c];
-            x0 *= f;
-            x1 *= f;
-            if (edge) {
-              if (t0 + g8 > limit[nt][c]) x0 = -INFINITY;
-              if (t0 + g8 + 8 > limit[nt][c]) x1 = -INFINITY;
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int g = 0; g < SUB; ++g) {
+              const float f = q_scale[nt][c] * ks[g];
+              const int t = t0 + g * 16 + g8;
+              float &x0 = sc[g][nt][c], &x1 = sc[g][nt][2 + c];
+              x0 *= f;
+              x1 *= f;
+              if (edge) {
+                if (t > limit[nt][c]) x0 = -INFINITY;
+                if (t + 8 > limit[nt][c]) x1 = -INFINITY;
+              }
+              grow |= fmaxf(x0, x1) > mrow[nt][c] + kGrow;
+              if (logit_row[nt][c] != nullptr && QALORA_CHECK(dbg, t + 8, a.logit_stride)) {
+                logit_row[nt][c][t] = x0;
+                logit_row[nt][c][t + 8] = x1;
+              }
             }
-            grow |= fmaxf(x0, x1) > mrow[nt][c] + kGrow;
-            if (logit_row[nt][c] != nullptr && QALORA_CHECK(dbg, t0 + g8 + 8, a.logit_stride)) {
-              logit_row[nt][c][t0 + g8] = x0;
-              logit_row[nt][c][t0 + g8 + 8] = x1;
-            }
-          }
-        if (__any_sync(0xffffffffu, grow) || vs > ref) {
+        if (__any_sync(0xffffffffu, grow) || v_top > ref) {
           // rare: bring the rows to their new maximum, and the outputs to the new largest value scale
-          const float ref_new = vs > ref ? vs : ref, ref_ratio = ref_new > 0.f ? ref / ref_new : 0.f;
+          const float ref_new = fmaxf(v_top, ref), ref_ratio = ref_new > 0.f ? ref / ref_new : 0.f;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             float by[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              float mx = fmaxf(sc[nt][c], sc[nt][2 + c]);
+              float mx = mrow[nt][c];
+#pragma unroll
+              for (int g = 0; g < SUB; ++g) mx = fmaxf(mx, fmaxf(sc[g][nt][c], sc[g][nt][2 + c]));
 #pragma unroll
               for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-              mx = fmaxf(mx, mrow[nt][c]);
               by[c] = exp2f(mrow[nt][c] - mx);
               mrow[nt][c] = mx;
               lrow[nt][c] *= by[c];
@@ -336,31 +344,36 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           ref = ref_new;
           inv_ref = ref > 0.f ? 1.f / ref : 0.f;
         }
-        const float v_rel = vs * inv_ref;
-        uint32_t pf[NT][2];                            // P^T as the B operand: tokens 0-7 and 8-15
+        uint32_t pf[SUB][NT][2];                       // P^T as the B operand: tokens 0-7 and 8-15 of a group
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float e[4];
+        for (int g = 0; g < SUB; ++g) {
+          const float v_rel = vs[g] * inv_ref;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) e[c] = kvp::exp2_fast(sc[nt][c] - (mrow[nt][c & 1] - kLift));
-          lrow[nt][0] += e[0] + e[2];
-          lrow[nt][1] += e[1] + e[3];
-          pf[nt][0] = kvp::movmatrix(kvp::pack_half2(e[0] * v_rel, e[1] * v_rel));
-          pf[nt][1] = kvp::movmatrix(kvp::pack_half2(e[2] * v_rel, e[3] * v_rel));
-        }
+          for (int nt = 0; nt < NT; ++nt) {
+            float e[4];
 #pragma unroll
-        for (int c2 = 0; c2 < D / 32; ++c2) {
-          uint32_t r[4];
-          kvp::ldmatrix_x4_trans(r, v_base + kvp::swizzled<D>(tok, c2 * 2 + (lane >> 4)));
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            uint32_t f[4];                             // {even, odd channels} x {tokens 0-7, 8-15}
-            kvp::pairs_to_half(r[2 * x], f[0], f[1]);
-            kvp::pairs_to_half(r[2 * x + 1], f[2], f[3]);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) kvp::mma16816(o[nt][c2 * 2 + x], f, pf[nt][0], pf[nt][1]);
+            for (int c = 0; c < 4; ++c) e[c] = kvp::exp2_fast(sc[g][nt][c] - (mrow[nt][c & 1] - kLift));
+            lrow[nt][0] += e[0] + e[2];
+            lrow[nt][1] += e[1] + e[3];
+            pf[g][nt][0] = kvp::movmatrix(kvp::pack_half2(e[0] * v_rel, e[1] * v_rel));
+            pf[g][nt][1] = kvp::movmatrix(kvp::pack_half2(e[2] * v_rel, e[3] * v_rel));
           }
         }
+#pragma unroll
+        for (int g = 0; g < SUB; ++g)
+#pragma unroll
+          for (int c2 = 0; c2 < D / 32; ++c2) {
+            uint32_t r[4];
+            kvp::ldmatrix_x4_trans(r, v_base + kvp::swizzled<D>(tok + g * 16, c2 * 2 + (lane >> 4)));
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              uint32_t f[4];                           // {even, odd channels} x {tokens 0-7, 8-15}
+              kvp::pairs_to_half(r[2 * x], f[0], f[1]);
+              kvp::pairs_to_half(r[2 * x + 1], f[2], f[3]);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) kvp::mma16816(o[nt][c2 * 2 + x], f, pf[g][nt][0], pf[g][nt][1]);
+            }
+          }
       }
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(empty(st));
