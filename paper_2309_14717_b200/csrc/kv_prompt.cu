@@ -44,9 +44,11 @@ struct PtSmem {
   static constexpr int TILE = 128 * D * 2;                    // bytes of an fp16 tile
   static constexpr int OFF_Q = 0;                             // two row tiles
   static constexpr int OFF_K = 2 * TILE, OFF_V = 4 * TILE;    // two stages each
-  static constexpr int OFF_RING = 6 * TILE;
+  static constexpr int STAGED = 128 * D;                      // bytes of a tile of codes
+  static constexpr int OFF_STAGED = 6 * TILE;                 // keys, values
+  static constexpr int OFF_RING = OFF_STAGED + 2 * STAGED;
   static constexpr int OFF_BARS = OFF_RING + PT_RING * PT_RING_FLOATS * 4;
-  static constexpr int NBARS = 1 + 4 * 2 + 4 * 2 + 2 * PT_RING;
+  static constexpr int NBARS = 1 + 4 * 2 + 4 * 2 + PT_RING + 4;
   static constexpr int OFF_SLOT = OFF_BARS + NBARS * 8 + 8;
   static constexpr int TOTAL = OFF_SLOT + 16 + 1024;
 };
@@ -65,42 +67,30 @@ __device__ __forceinline__ void store_codes(uint8_t* tile, int row, int piece, c
   *reinterpret_cast<uint4*>(base + (((chunk + 1) ^ (row & 7)) << 4)) = hi;
 }
 
-// Which 16 codes of every pass over a tile thread t of `THREADS` takes: eight neighbouring lanes hold four pieces of
-// an even and of an odd row, whose swizzled chunks lie in different banks.
+// Which 16 codes of pass p over a tile thread t of `THREADS` takes.  Eight neighbouring lanes read the eight pieces of a
+// 128-byte row (or the four of two 64-byte rows): different banks.  With 128 channels the lanes of the second half take
+// the neighbouring row, so that the swizzled chunks that the eight of them store lie in different banks too.
 template <int D, int THREADS>
 struct TileMap {
   static constexpr int PIECES = D / 16, ROWS = THREADS / PIECES, PASSES = 128 / ROWS;
   int piece, row0;
-  __device__ __forceinline__ explicit TileMap(int t)
-      : piece(D == 128 ? (t & 3) | ((t >> 3) & 1) << 2 : t & 3), row0(D == 128 ? ((t >> 2) & 1) | (t >> 4) << 1 : t >> 2) {}
+  __device__ __forceinline__ explicit TileMap(int t) : piece(t % PIECES), row0(D == 128 ? (t / PIECES) ^ ((t >> 2) & 1) : t / PIECES) {}
 };
 
-// The codes of one 128-token tile on their way from memory.
+// A staged tile of codes, rows of D bytes, to an fp16 tile.  Unless all of it is there, rows from `rows` on and those of
+// blocks that are not there (`ids`: the blocks of the tile's groups of 16 tokens) become zeros.
 template <int D>
-struct TileCodes {
+__device__ __forceinline__ void convert_tile(const uint8_t* staged, uint8_t* tile, bool all, const int* ids, int rows, int t) {
   using Map = TileMap<D, PT_CONV * 32>;
-  uint4 c[Map::PASSES];
-  // `src`: this head's keys (or values) of block 0, at this thread's piece; `ids`: the blocks of the tile's groups of
-  // 16 tokens.  Blocks that are not there are read at block 0: a load under a condition, or a select behind
-  // it, would make the thread wait for it here.
-  __device__ __forceinline__ void load(const int8_t* src, long long block_bytes, int block, const int* ids, const Map& map) {
+  const Map map(t);
 #pragma unroll
-    for (int p = 0; p < Map::PASSES; ++p) {
-      const int row = p * Map::ROWS + map.row0, id = ids[row >> 4];
-      c[p] = *reinterpret_cast<const uint4*>(src + (id < 0 ? 0 : id) * block_bytes + (row & (block - 1)) * D);
-    }
+  for (int p = 0; p < Map::PASSES; ++p) {
+    const int row = p * Map::ROWS + map.row0;
+    uint4 c = *reinterpret_cast<const uint4*>(staged + row * D + map.piece * 16);
+    if (!all && (row >= rows || ids[row >> 4] < 0)) c = make_uint4(0, 0, 0, 0);
+    store_codes(tile, row, map.piece, c);
   }
-  // unless all of the tile is there, rows from `rows` on and those of blocks that are not there become zeros
-  __device__ __forceinline__ void store(uint8_t* tile, bool all, const int* ids, int rows, const Map& map) const {
-#pragma unroll
-    for (int p = 0; p < Map::PASSES; ++p) {
-      const int row = p * Map::ROWS + map.row0;
-      uint4 v = c[p];
-      if (!all && (row >= rows || ids[row >> 4] < 0)) v = make_uint4(0, 0, 0, 0);
-      store_codes(tile, row, map.piece, v);
-    }
-  }
-};
+}
 
 // A softmax thread's row.
 struct SoftmaxRow {
@@ -109,38 +99,28 @@ struct SoftmaxRow {
   float ref;               // value scale that the outputs are relative to
 };
 
-struct TileScales {
-  float c[8], off[8], inv[8];    // of 16 tokens each: factor of a score, log2 of the relative value scale, its inverse
-};
-
-// First look at a tile of S (t_s: 128 columns of this thread's lane): whether a row's maximum has grown by 2^kGrow or
-// more, or the values' reference has changed (rare; and always on the first tile); the maximum and the outputs are
-// then brought up to date.  EDGE: columns beyond `seen` are masked.
-template <int D, bool EDGE>
-__device__ __forceinline__ void softmax_settle(SoftmaxRow& w, const TileScales& sc, float ref_ratio, uint32_t t_s, uint32_t t_o, int seen, bool first) {
-  float top = kNoMax;
-  float x[2][32];
-  ptx::tmem_ld32(t_s, reinterpret_cast<uint32_t*>(x[0]));
+// A tile of S in a thread's registers: the columns (tokens) beyond `seen` masked, and whether the row's maximum has grown
+// by 2^kGrow or more, or the values' reference has changed (rare; and always on the first tile); the maximum and the
+// outputs are then brought up to date.  rg: the tile's scales, of 16 tokens each.
+template <int D>
+__device__ __forceinline__ void softmax_settle(SoftmaxRow& w, float (&x)[128], const float* rg, uint32_t t_o, bool edge, int seen, bool first) {
+  if (edge) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    ptx::tmem_wait_ld();
-    if (q < 3) ptx::tmem_ld32(t_s + 32 * (q + 1), reinterpret_cast<uint32_t*>(x[(q + 1) & 1]));
-    float* v = x[q & 1];
-    if (EDGE) {
-#pragma unroll
-      for (int t = 0; t < 32; ++t) if (32 * q + t > seen) v[t] = -INFINITY;
-    }
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      float a = fmaxf(v[16 * g], v[16 * g + 1]), b = fmaxf(v[16 * g + 2], v[16 * g + 3]);
-#pragma unroll
-      for (int t = 4; t < 16; t += 4) {
-        a = kvp::max3(a, v[16 * g + t], v[16 * g + t + 1]);
-        b = kvp::max3(b, v[16 * g + t + 2], v[16 * g + t + 3]);
-      }
-      top = fmaxf(top, fmaf(fmaxf(a, b), sc.c[2 * q + g], sc.off[2 * q + g]));
-    }
+    for (int t = 0; t < 128; ++t) if (t > seen) x[t] = -INFINITY;
   }
+  float top = kNoMax;
+#pragma unroll
+  for (int g = 0; g < 8; ++g) {
+    const float* v = x + 16 * g;
+    float a = fmaxf(v[0], v[1]), b = fmaxf(v[2], v[3]);
+#pragma unroll
+    for (int t = 4; t < 16; t += 4) {
+      a = kvp::max3(a, v[t], v[t + 1]);
+      b = kvp::max3(b, v[t + 2], v[t + 3]);
+    }
+    top = fmaxf(top, fmaf(fmaxf(a, b), fmaxf(w.factor * rg[g], kTiny), rg[8 + g]));
+  }
+  const float ref_ratio = rg[24];
   if (!__any_sync(0xffffffffu, top > w.m + kGrow) && ref_ratio == 1.f) return;
   top = fmaxf(top, w.m);
   const float by = exp2f(w.m - top), scale = by * ref_ratio;
@@ -158,39 +138,30 @@ __device__ __forceinline__ void softmax_settle(SoftmaxRow& w, const TileScales& 
   }
 }
 
-// S to P, over columns of S that have been read: 32 columns at a time with the next 32 on their way.
-template <bool EDGE>
-__device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const TileScales& sc, uint32_t t_s, int seen) {
+// The tile's weights to P, over its own columns of S; `turn` is passed on before the last quarter.
+__device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[128], const float* rg, uint32_t t_s, uint32_t turn) {
   const float base = kLift - w.m;
-  float x[2][32];
-  ptx::tmem_ld32(t_s, reinterpret_cast<uint32_t*>(x[0]));
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    ptx::tmem_wait_ld();
-    if (q < 3) ptx::tmem_ld32(t_s + 32 * (q + 1), reinterpret_cast<uint32_t*>(x[(q + 1) & 1]));
-    const float* v = x[q & 1];
     uint32_t pk[16];
 #pragma unroll
     for (int g2 = 0; g2 < 2; ++g2) {
       const int g = 2 * q + g2;
-      const float off = sc.off[g] + base;
-      const float2 cc = make_float2(sc.c[g], sc.c[g]), oo = make_float2(off, off);
+      const float c = fmaxf(w.factor * rg[g], kTiny), off = rg[8 + g] + base;
+      const float2 cc = make_float2(c, c), oo = make_float2(off, off);
       float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        float2 y = ptx::ffma2(make_float2(v[16 * g2 + 2 * t], v[16 * g2 + 2 * t + 1]), cc, oo);
-        if (EDGE) {
-          if (16 * g + 2 * t > seen) y.x = -INFINITY;
-          if (16 * g + 2 * t + 1 > seen) y.y = -INFINITY;
-        }
+        float2 y = ptx::ffma2(make_float2(x[16 * g + 2 * t], x[16 * g + 2 * t + 1]), cc, oo);
         y.x = kvp::exp2_fast(y.x);
         y.y = kvp::exp2_fast(y.y);
         sum = ptx::fadd2(sum, y);
         pk[8 * g2 + t] = kvp::pack_half2(y.x, y.y);
       }
-      w.l = fmaf(sum.x + sum.y, sc.inv[g], w.l);
+      w.l = fmaf(sum.x + sum.y, rg[16 + g], w.l);
     }
     ptx::tmem_st16(t_s + 16 * q, pk);
+    if (q == 2 && (threadIdx.x & 31) == 0) ptx::mbar_arrive(turn);
   }
 }
 
@@ -220,8 +191,9 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
   auto p_full = [&](int i) { return bars + 88 + 8 * i; };
   auto o_full = [&](int i) { return bars + 104 + 8 * i; };
   auto turn = [&](int i) { return bars + 120 + 8 * i; };
-  auto r_full = [&](int x) { return bars + 136 + 8 * x; };              // blocks and scales of a tile are there
-  auto r_used = [&](int x) { return bars + 136 + 8 * (PT_RING + x); };  // its codes have been converted
+  auto r_used = [&](int x) { return bars + 136 + 8 * x; };              // the codes of a tile have been converted
+  auto c_full = [&](int w) { return bars + 136 + 8 * (PT_RING + w); };  // codes of keys (0) or values (1) are staged
+  auto c_empty = [&](int w) { return bars + 136 + 8 * (PT_RING + 2 + w); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::OFF_SLOT);
   volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_SLOT + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -261,7 +233,8 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       ptx::mbar_init(o_full(x), 1);
       ptx::mbar_init(turn(x), 4);
     }
-    for (int x = 0; x < PT_RING; ++x) { ptx::mbar_init(r_full(x), 1); ptx::mbar_init(r_used(x), PT_CONV); }
+    for (int x = 0; x < PT_RING; ++x) ptx::mbar_init(r_used(x), PT_CONV);
+    for (int x = 0; x < 2; ++x) { ptx::mbar_init(c_full(x), 1); ptx::mbar_init(c_empty(x), PT_CONV); }
     ptx::fence_mbar_init();
   }
   if (warp == PT_ISSUE) {
@@ -277,7 +250,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
 
   if (warp < 8) {
     // ------------------------------------------------------------------------------ softmax ----
-    kvp::more_registers<152>();
+    kvp::more_registers<176>();
     const int i = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
     const int r = (pair * 2 + i) * PT_ROWS + row;
     const bool there = r < rows;
@@ -332,27 +305,18 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       const int step = j - first, others = end[1 - i] - first;
       if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(s_full(i), step & 1, flag)))) break;
       ptx::tc_fence_after();
-      const float4* rg = reinterpret_cast<const float4*>(ring + (step % PT_RING) * PT_RING_FLOATS);
-      TileScales sc;
+      float x[128];
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const float4 k = rg[g], o = rg[2 + g], v = rg[4 + g];
-        sc.c[4 * g] = fmaxf(factor * k.x, kTiny); sc.c[4 * g + 1] = fmaxf(factor * k.y, kTiny);
-        sc.c[4 * g + 2] = fmaxf(factor * k.z, kTiny); sc.c[4 * g + 3] = fmaxf(factor * k.w, kTiny);
-        sc.off[4 * g] = o.x; sc.off[4 * g + 1] = o.y; sc.off[4 * g + 2] = o.z; sc.off[4 * g + 3] = o.w;
-        sc.inv[4 * g] = v.x; sc.inv[4 * g + 1] = v.y; sc.inv[4 * g + 2] = v.z; sc.inv[4 * g + 3] = v.w;
-      }
-      const float4 rr = rg[6];                                    // {reference before / now, reference now}
-      w.ref = rr.y;
-      if (j < whole) softmax_settle<D, false>(w, sc, rr.x, t_s, t_o, 0, step == 0);
-      else softmax_settle<D, true>(w, sc, rr.x, t_s, t_o, limit - j * PT_TOK, step == 0);
+      for (int q = 0; q < 4; ++q) ptx::tmem_ld32(t_s + 32 * q, reinterpret_cast<uint32_t*>(x + 32 * q));
+      const float* rg = ring + (step % PT_RING) * PT_RING_FLOATS;
+      w.ref = rg[25];
+      ptx::tmem_wait_ld();
+      softmax_settle<D>(w, x, rg, t_o, j >= whole, limit - j * PT_TOK, step == 0);
       // The two row tiles' exponentials take turns: side by side they would share the exponential unit and then the
       // tensor core, each idle while the other works.  (Waits only for a step that the other tile has.)
       if (i == 0 ? step >= 1 && step - 1 < others : step < others)
         if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(turn(i), (i == 0 ? step - 1 : step) & 1, flag)))) break;
-      if (j < whole) softmax_exp<false>(w, sc, t_s, 0);
-      else softmax_exp<true>(w, sc, t_s, limit - j * PT_TOK);
-      if (lane == 0) ptx::mbar_arrive(turn(1 - i));
+      softmax_exp(w, x, rg, t_s, turn(1 - i));
       ptx::tmem_wait_st();
       ptx::tc_fence_before();
       __syncwarp();
@@ -408,39 +372,31 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
     if (!partial && there) kvp::store_lse(a.at.lse, at, nullptr, 0, m, l, kLift);
   } else if (warp < PT_ISSUE) {
     // --------------------------------------------------------------------------- conversion ----
-    kvp::fewer_registers<64>();
-    const TileMap<D, PT_CONV * 32> map(threadIdx.x - 256);
-    const long long block_bytes = 2ll * sh.kv_heads * sh.block * D;
-    const int8_t* k_src = a.at.codes + (long long)h * sh.block * D + map.piece * 16;
-    const int8_t* v_src = k_src + (long long)sh.kv_heads * sh.block * D;
-    auto ring_ids = [&](int it) { return reinterpret_cast<const int*>(ring + (it % PT_RING) * PT_RING_FLOATS) + 32; };
-    auto known = [&](int it) { return __all_sync(0xffffffffu, ptx::mbar_wait(r_full(it % PT_RING), (it / PT_RING) & 1, flag)); };
-    TileCodes<D> kc, vc;
-    bool ok = count == 0 || known(0);
-    if (count > 0 && ok) kc.load(k_src, block_bytes, sh.block, ring_ids(0), map);
+    kvp::fewer_registers<40>();
+    const int t = threadIdx.x - 256;
+    auto wait = [&](uint32_t bar, int phase) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, phase & 1, flag)); };
+    bool ok = true;
+#pragma unroll 1
     for (int it = 0; it < count && ok; ++it) {
       const int st = it & 1, rows_here = s.len - (first + it) * PT_TOK;
-      const int* ids = ring_ids(it);
-      const bool all = ids[-6] != 0;
-      vc.load(v_src, block_bytes, sh.block, ids + 8, map);
-      if (it >= 2 && !__all_sync(0xffffffffu, ptx::mbar_wait(k_empty(st), ((it >> 1) - 1) & 1, flag))) break;
-      kc.store(smem + S::OFF_K + st * S::TILE, all, ids, rows_here, map);
-      ptx::fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(k_full(st));
-      if (it + 1 < count) {
-        if (!(ok = known(it + 1))) break;
-        kc.load(k_src, block_bytes, sh.block, ring_ids(it + 1), map);
+      const int* ids = reinterpret_cast<const int*>(ring + (it % PT_RING) * PT_RING_FLOATS) + 32;
+#pragma unroll 1
+      for (int w = 0; w < 2; ++w) {                              // keys, values
+        if (!(ok = wait(c_full(w), it))) break;
+        if (it >= 2 && !(ok = wait(w == 0 ? k_empty(st) : v_empty(st), (it >> 1) - 1))) break;
+        convert_tile<D>(smem + S::OFF_STAGED + w * S::STAGED, smem + (w == 0 ? S::OFF_K : S::OFF_V) + st * S::TILE, ids[-6] != 0, ids + 8 * w, rows_here, t);
+        ptx::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          ptx::mbar_arrive(c_empty(w));
+          ptx::mbar_arrive(w == 0 ? k_full(st) : v_full(st));
+          if (w == 1) ptx::mbar_arrive(r_used(it % PT_RING));
+        }
       }
-      if (it >= 2 && !__all_sync(0xffffffffu, ptx::mbar_wait(v_empty(st), ((it >> 1) - 1) & 1, flag))) break;
-      vc.store(smem + S::OFF_V + st * S::TILE, all, ids + 8, rows_here, map);
-      ptx::fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) { ptx::mbar_arrive(v_full(st)); ptx::mbar_arrive(r_used(it % PT_RING)); }
     }
   } else {
     // --------------------------------------------------------------------------- MMA issuers ----
-    kvp::fewer_registers<48>();
+    kvp::fewer_registers<40>();
     const int i = __shfl_sync(0xffffffffu, warp, 0) - PT_ISSUE;
     if (i < 2) {
       const uint32_t leader = kvp::elect_one();
@@ -527,7 +483,24 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
         }
         if (lane == 8) { rg[24] = ratio; rg[25] = ref; reinterpret_cast<int*>(rg)[26] = all ? 1 : 0; }
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(r_full(it % PT_RING));
+        // the codes of the blocks that are there, one copy each (a copy starts on a 16-byte boundary: blocks are multiples
+        // of 1 KiB); lane 16-token group l stands for the block that begins with it
+        const int groups = sh.block >> 4;
+        const bool begins = lane < 8 && lane % groups == 0;
+        bool ok = true;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const int id = w == 0 ? cur.id : v_id;
+          const bool copies = begins && id >= 0;
+          const int n = __popc(__ballot_sync(0xffffffffu, copies));
+          if (it >= 1 && !(ok = __all_sync(0xffffffffu, ptx::mbar_wait(c_empty(w), (it - 1) & 1, flag)))) break;
+          if (lane == 0) ptx::mbar_arrive_expect_tx(c_full(w), (uint32_t)(n * sh.block * D));
+          __syncwarp();
+          if (copies)
+            ptx::bulk_load(sbase + S::OFF_STAGED + w * S::STAGED + lane * 16 * D,
+                           a.at.codes + (((long long)id * 2 + w) * sh.kv_heads + h) * sh.block * D, (uint32_t)(sh.block * D), c_full(w));
+        }
+        if (!ok) break;
       }
     }
     __syncwarp();
