@@ -48,7 +48,7 @@ struct PtSmem {
   static constexpr int OFF_STAGED = 6 * TILE;                 // keys, values
   static constexpr int OFF_RING = OFF_STAGED + 2 * STAGED;
   static constexpr int OFF_BARS = OFF_RING + PT_RING * PT_RING_FLOATS * 4;
-  static constexpr int NBARS = 1 + 4 * 2 + 4 * 2 + PT_RING + 4;
+  static constexpr int NBARS = 1 + 4 * 2 + 4 * 2 + PT_RING + 6;
   static constexpr int OFF_SLOT = OFF_BARS + NBARS * 8 + 8;
   static constexpr int TOTAL = OFF_SLOT + 16 + 1024;
 };
@@ -101,9 +101,10 @@ struct SoftmaxRow {
 
 // A tile of S in a thread's registers: the columns (tokens) beyond `seen` masked, and whether the row's maximum has grown
 // by 2^kGrow or more, or the values' reference has changed (rare; and always on the first tile); the maximum and the
-// outputs are then brought up to date.  rg: the tile's scales, of 16 tokens each.
+// outputs are then brought up to date.  c, off: the factor of a score and log2 of the value scale, of 16 tokens each.
 template <int D>
-__device__ __forceinline__ void softmax_settle(SoftmaxRow& w, float (&x)[128], const float* rg, uint32_t t_o, bool edge, int seen, bool first) {
+__device__ __forceinline__ void softmax_settle(SoftmaxRow& w, float (&x)[128], const float (&c)[8], const float (&off)[8], float ref_ratio,
+                                               uint32_t t_o, bool edge, int seen, bool first) {
   if (edge) {
 #pragma unroll
     for (int t = 0; t < 128; ++t) if (t > seen) x[t] = -INFINITY;
@@ -118,9 +119,8 @@ __device__ __forceinline__ void softmax_settle(SoftmaxRow& w, float (&x)[128], c
       a = kvp::max3(a, v[t], v[t + 1]);
       b = kvp::max3(b, v[t + 2], v[t + 3]);
     }
-    top = fmaxf(top, fmaf(fmaxf(a, b), fmaxf(w.factor * rg[g], kTiny), rg[8 + g]));
+    top = fmaxf(top, fmaf(fmaxf(a, b), c[g], off[g]));
   }
-  const float ref_ratio = rg[24];
   if (!__any_sync(0xffffffffu, top > w.m + kGrow) && ref_ratio == 1.f) return;
   top = fmaxf(top, w.m);
   const float by = exp2f(w.m - top), scale = by * ref_ratio;
@@ -138,16 +138,21 @@ __device__ __forceinline__ void softmax_settle(SoftmaxRow& w, float (&x)[128], c
   }
 }
 
-// The tile's weights to P, over its own columns of S; `turn` is passed on before the last quarter.
-__device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[128], const float* rg, uint32_t t_s, uint32_t turn) {
+// The tile's weights to P, over its own columns of S.  `half` is told when the first half of them is there, `turn` is passed
+// on before the last quarter.  rg: the tile's scales; they are asked for a quarter ahead (beside the tensor
+// core's own reads a shared-memory load takes some hundred cycles).
+__device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[128], const float* rg, uint32_t t_s, uint32_t half, uint32_t turn) {
   const float base = kLift - w.m;
+  float2 k = *reinterpret_cast<const float2*>(rg), o = *reinterpret_cast<const float2*>(rg + 8), v = *reinterpret_cast<const float2*>(rg + 16);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     uint32_t pk[16];
+    const float2 kn = *reinterpret_cast<const float2*>(rg + 2 * (q + 1 & 3)), on = *reinterpret_cast<const float2*>(rg + 8 + 2 * (q + 1 & 3));
+    const float2 vn = *reinterpret_cast<const float2*>(rg + 16 + 2 * (q + 1 & 3));
 #pragma unroll
     for (int g2 = 0; g2 < 2; ++g2) {
       const int g = 2 * q + g2;
-      const float c = fmaxf(w.factor * rg[g], kTiny), off = rg[8 + g] + base;
+      const float c = fmaxf(w.factor * (g2 == 0 ? k.x : k.y), kTiny), off = (g2 == 0 ? o.x : o.y) + base;
       const float2 cc = make_float2(c, c), oo = make_float2(off, off);
       float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
@@ -158,9 +163,16 @@ __device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[128]
         sum = ptx::fadd2(sum, y);
         pk[8 * g2 + t] = kvp::pack_half2(y.x, y.y);
       }
-      w.l = fmaf(sum.x + sum.y, rg[16 + g], w.l);
+      w.l = fmaf(sum.x + sum.y, g2 == 0 ? v.x : v.y, w.l);
     }
+    k = kn; o = on; v = vn;
     ptx::tmem_st16(t_s + 16 * q, pk);
+    if (q == 1) {
+      ptx::tmem_wait_st();
+      ptx::tc_fence_before();
+      __syncwarp();
+      if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(half);
+    }
     if (q == 2 && (threadIdx.x & 31) == 0) ptx::mbar_arrive(turn);
   }
 }
@@ -194,6 +206,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
   auto r_used = [&](int x) { return bars + 136 + 8 * x; };              // the codes of a tile have been converted
   auto c_full = [&](int w) { return bars + 136 + 8 * (PT_RING + w); };  // codes of keys (0) or values (1) are staged
   auto c_empty = [&](int w) { return bars + 136 + 8 * (PT_RING + 2 + w); };
+  auto p_half = [&](int i) { return bars + 136 + 8 * (PT_RING + 4 + i); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::OFF_SLOT);
   volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_SLOT + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -230,6 +243,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       ptx::mbar_init(v_empty(x), 2);
       ptx::mbar_init(s_full(x), 1);
       ptx::mbar_init(p_full(x), 4);
+      ptx::mbar_init(p_half(x), 4);
       ptx::mbar_init(o_full(x), 1);
       ptx::mbar_init(turn(x), 4);
     }
@@ -309,14 +323,22 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
 #pragma unroll
       for (int q = 0; q < 4; ++q) ptx::tmem_ld32(t_s + 32 * q, reinterpret_cast<uint32_t*>(x + 32 * q));
       const float* rg = ring + (step % PT_RING) * PT_RING_FLOATS;
-      w.ref = rg[25];
+      float c[8], off[8];
+#pragma unroll
+      for (int g = 0; g < 8; g += 4) {
+        const float4 k = *reinterpret_cast<const float4*>(rg + g), o = *reinterpret_cast<const float4*>(rg + 8 + g);
+        c[g] = fmaxf(factor * k.x, kTiny); c[g + 1] = fmaxf(factor * k.y, kTiny); c[g + 2] = fmaxf(factor * k.z, kTiny); c[g + 3] = fmaxf(factor * k.w, kTiny);
+        off[g] = o.x; off[g + 1] = o.y; off[g + 2] = o.z; off[g + 3] = o.w;
+      }
+      const float2 refs = *reinterpret_cast<const float2*>(rg + 24);      // {reference before / now, now}
+      w.ref = refs.y;
       ptx::tmem_wait_ld();
-      softmax_settle<D>(w, x, rg, t_o, j >= whole, limit - j * PT_TOK, step == 0);
+      softmax_settle<D>(w, x, c, off, refs.x, t_o, j >= whole, limit - j * PT_TOK, step == 0);
       // The two row tiles' exponentials take turns: side by side they would share the exponential unit and then the
       // tensor core, each idle while the other works.  (Waits only for a step that the other tile has.)
       if (i == 0 ? step >= 1 && step - 1 < others : step < others)
         if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(turn(i), (i == 0 ? step - 1 : step) & 1, flag)))) break;
-      softmax_exp(w, x, rg, t_s, turn(1 - i));
+      softmax_exp(w, x, rg, t_s, p_half(i), turn(1 - i));
       ptx::tmem_wait_st();
       ptx::tc_fence_before();
       __syncwarp();
@@ -423,14 +445,19 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
           ptx::mbar_arrive(k_empty(st));
         }
         __syncwarp();
-        if (mine && !(ok = wait(p_full(i), it & 1))) break;
         if (!(ok = wait(v_full(st), ph))) break;
         if (mine) {
-          ptx::tc_fence_after();
           const uint64_t v_desc = ptx::smem_desc(sbase + S::OFF_V + st * S::TILE, 16384, 1024);
+          if (!(ok = wait(p_half(i), it & 1))) break;            // the first 64 tokens' weights, then the others'
+          ptx::tc_fence_after();
 #pragma unroll
-          for (int k = 0; k < PT_TOK / 16; ++k)
+          for (int k = 0; k < PT_TOK / 32; ++k)
             kvp::mma_ts(leader, t_o, t_s + 8 * k, v_desc + (uint64_t)(k * 128), IDESC_O, it > 0 || k > 0 ? 1u : 0u);
+          if (!(ok = wait(p_full(i), it & 1))) break;
+          ptx::tc_fence_after();
+#pragma unroll
+          for (int k = PT_TOK / 32; k < PT_TOK / 16; ++k)
+            kvp::mma_ts(leader, t_o, t_s + 8 * k, v_desc + (uint64_t)(k * 128), IDESC_O, 1u);
           kvp::mma_commit(leader, v_empty(st));
           if (first + it + 1 == end[i]) kvp::mma_commit(leader, o_full(i));
         } else if (leader) {
