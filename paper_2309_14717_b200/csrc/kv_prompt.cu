@@ -12,6 +12,7 @@ constexpr int PT_CONV = 8;                     // conversion warps
 constexpr int PT_THREADS = 256 + PT_CONV * 32 + 128;   // 2 x 128 softmax, conversion, 2 issuing warps (and 2 idle ones)
 constexpr int PT_ISSUE = 8 + PT_CONV;          // first issuing warp
 constexpr int PT_TOK = 128, PT_ROWS = 128;    // a tile: tokens x rows (new tokens x heads of a group)
+constexpr int PT_HALF = 64;                   // tokens of a step: half a tile
 constexpr int PT_RING = 8;                    // tiles whose blocks and scales are kept
 constexpr int PT_RING_FLOATS = 48;            // ks[8], log2 of vs / ref [8], ref / vs [8], {ref_before / ref, ref, all there}, blocks of
                                               // keys [8] at 32 and of values [8] at 40
@@ -48,7 +49,7 @@ struct PtSmem {
   static constexpr int OFF_STAGED = 6 * TILE;                 // keys, values
   static constexpr int OFF_RING = OFF_STAGED + 2 * STAGED;
   static constexpr int OFF_BARS = OFF_RING + PT_RING * PT_RING_FLOATS * 4;
-  static constexpr int NBARS = 1 + 4 * 2 + 4 * 2 + PT_RING + 6;
+  static constexpr int NBARS = 1 + 4 * 2 + 6 * 2 + PT_RING + 4;
   static constexpr int OFF_SLOT = OFF_BARS + NBARS * 8 + 8;
   static constexpr int TOTAL = OFF_SLOT + 16 + 1024;
 };
@@ -99,19 +100,18 @@ struct SoftmaxRow {
   float ref;               // value scale that the outputs are relative to
 };
 
-// A tile of S in a thread's registers: the columns (tokens) beyond `seen` masked, and whether the row's maximum has grown
-// by 2^kGrow or more, or the values' reference has changed (rare; and always on the first tile); the maximum and the
-// outputs are then brought up to date.  c, off: the factor of a score and log2 of the value scale, of 16 tokens each.
-template <int D>
-__device__ __forceinline__ void softmax_settle(SoftmaxRow& w, float (&x)[128], const float (&c)[8], const float (&off)[8], float ref_ratio,
-                                               uint32_t t_o, bool edge, int seen, bool first) {
+// A step's scores in a thread's registers: the columns (tokens) beyond `seen` masked, and whether the row's maximum has grown
+// by 2^kGrow or more (rare; and always on the first step).  c, off: the factor of a score and log2 of the value scale,
+// of 16 tokens each.  Returns the row's maximum, the running one included.
+__device__ __forceinline__ float softmax_top(const SoftmaxRow& w, float (&x)[PT_HALF], const float4 c, const float4 off, bool edge, int seen) {
   if (edge) {
 #pragma unroll
-    for (int t = 0; t < 128; ++t) if (t > seen) x[t] = -INFINITY;
+    for (int t = 0; t < PT_HALF; ++t) if (t > seen) x[t] = -INFINITY;
   }
-  float top = kNoMax;
+  const float cs[4] = {c.x, c.y, c.z, c.w}, os[4] = {off.x, off.y, off.z, off.w};
+  float top = w.m;
 #pragma unroll
-  for (int g = 0; g < 8; ++g) {
+  for (int g = 0; g < 4; ++g) {
     const float* v = x + 16 * g;
     float a = fmaxf(v[0], v[1]), b = fmaxf(v[2], v[3]);
 #pragma unroll
@@ -119,41 +119,22 @@ __device__ __forceinline__ void softmax_settle(SoftmaxRow& w, float (&x)[128], c
       a = kvp::max3(a, v[t], v[t + 1]);
       b = kvp::max3(b, v[t + 2], v[t + 3]);
     }
-    top = fmaxf(top, fmaf(fmaxf(a, b), c[g], off[g]));
+    top = fmaxf(top, fmaf(fmaxf(a, b), cs[g], os[g]));
   }
-  if (!__any_sync(0xffffffffu, top > w.m + kGrow) && ref_ratio == 1.f) return;
-  top = fmaxf(top, w.m);
-  const float by = exp2f(w.m - top), scale = by * ref_ratio;
-  w.m = top;
-  w.l *= by;
-  if (first) return;
-#pragma unroll 1
-  for (int q = 0; q < D / 16; ++q) {
-    uint32_t o[16];
-    kvp::tmem_ld16(t_o + 16 * q, o);
-    ptx::tmem_wait_ld();
-#pragma unroll
-    for (int t = 0; t < 16; ++t) o[t] = __float_as_uint(__uint_as_float(o[t]) * scale);
-    ptx::tmem_st16(t_o + 16 * q, o);
-  }
+  return top;
 }
 
-// The tile's weights to P, over its own columns of S.  `half` is told when the first half of them is there, `turn` is passed
-// on before the last quarter.  rg: the tile's scales; they are asked for a quarter ahead (beside the tensor
-// core's own reads a shared-memory load takes some hundred cycles).
-__device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[128], const float* rg, uint32_t t_s, uint32_t half, uint32_t turn) {
+// The step's weights to P, over its own columns of S; inv: the inverse of the relative value scale.
+__device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[PT_HALF], const float4 c, const float4 off, const float4 inv, uint32_t t_s) {
+  const float cs[4] = {c.x, c.y, c.z, c.w}, os[4] = {off.x, off.y, off.z, off.w}, is[4] = {inv.x, inv.y, inv.z, inv.w};
   const float base = kLift - w.m;
-  float2 k = *reinterpret_cast<const float2*>(rg), o = *reinterpret_cast<const float2*>(rg + 8), v = *reinterpret_cast<const float2*>(rg + 16);
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < 2; ++q) {
     uint32_t pk[16];
-    const float2 kn = *reinterpret_cast<const float2*>(rg + 2 * (q + 1 & 3)), on = *reinterpret_cast<const float2*>(rg + 8 + 2 * (q + 1 & 3));
-    const float2 vn = *reinterpret_cast<const float2*>(rg + 16 + 2 * (q + 1 & 3));
 #pragma unroll
     for (int g2 = 0; g2 < 2; ++g2) {
       const int g = 2 * q + g2;
-      const float c = fmaxf(w.factor * (g2 == 0 ? k.x : k.y), kTiny), off = (g2 == 0 ? o.x : o.y) + base;
-      const float2 cc = make_float2(c, c), oo = make_float2(off, off);
+      const float2 cc = make_float2(cs[g], cs[g]), oo = make_float2(os[g] + base, os[g] + base);
       float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
@@ -163,29 +144,23 @@ __device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[128]
         sum = ptx::fadd2(sum, y);
         pk[8 * g2 + t] = kvp::pack_half2(y.x, y.y);
       }
-      w.l = fmaf(sum.x + sum.y, g2 == 0 ? v.x : v.y, w.l);
+      w.l = fmaf(sum.x + sum.y, is[g], w.l);
     }
-    k = kn; o = on; v = vn;
     ptx::tmem_st16(t_s + 16 * q, pk);
-    if (q == 1) {
-      ptx::tmem_wait_st();
-      ptx::tc_fence_before();
-      __syncwarp();
-      if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(half);
-    }
-    if (q == 2 && (threadIdx.x & 31) == 0) ptx::mbar_arrive(turn);
   }
 }
 
-// Two tiles of 128 rows of one kv head against a range of its sequence's tokens, 128 at a time:
+// Two tiles of 128 rows of one kv head against a range of its sequence's tokens, in tiles of 128 and steps of 64:
+//   look-up warp      blocks and scales of a tile, bulk copies of its codes;
 //   conversion warps  codes of a tile -> fp16 keys (K-major) and values (MN-major) in shared memory;
-//   issuing threads   one per row tile: S = Q K^T into tensor memory, then O += P V with P in tensor memory
-//                     (a thread issues an instruction per ~110 cycles, an N = 128 step takes 64: one
-//                     thread could not keep the tensor pipe busy, two can);
-//   softmax threads   one per row: S from tensor memory, P back over S's columns.
-// While one row tile's softmax runs, the other tile's products do.  P V of a step is issued before the next
-// S of the same tile by the same thread, so S may overwrite P; and an S that has arrived means that
-// the P V before it is done, so a softmax thread may rescale O whenever it holds a new S.
+//   issuing warps     one per row tile: S = Q K^T of a step into one of two places in tensor memory, O += P V with P in
+//                     tensor memory;
+//   softmax threads   one per row: S from tensor memory, P back over its columns.
+// S of the next step is there while a step's softmax runs: the exponentials, which bound the kernel together with the
+// products (64 x 128 x 128 of either take the exponential unit and the tensor core the same time), never wait
+// for a product.  (Steps of 128 tokens, for whose S there is one place only, left softmax and products of a row
+// tile to alternate: 189 us for a 4096-token prompt of 32 heads against NNN.)  P V of a step is issued before S of the
+// next but one by the same thread, so that S may overwrite P.
 template <int D>
 __global__ void __launch_bounds__(PT_THREADS, 1)
 kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) {
@@ -199,14 +174,14 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
   auto k_empty = [&](int s) { return bars + 24 + 8 * s; };
   auto v_full = [&](int s) { return bars + 40 + 8 * s; };
   auto v_empty = [&](int s) { return bars + 56 + 8 * s; };
-  auto s_full = [&](int i) { return bars + 72 + 8 * i; };
-  auto p_full = [&](int i) { return bars + 88 + 8 * i; };
-  auto o_full = [&](int i) { return bars + 104 + 8 * i; };
-  auto turn = [&](int i) { return bars + 120 + 8 * i; };
-  auto r_used = [&](int x) { return bars + 136 + 8 * x; };              // the codes of a tile have been converted
-  auto c_full = [&](int w) { return bars + 136 + 8 * (PT_RING + w); };  // codes of keys (0) or values (1) are staged
-  auto c_empty = [&](int w) { return bars + 136 + 8 * (PT_RING + 2 + w); };
-  auto p_half = [&](int i) { return bars + 136 + 8 * (PT_RING + 4 + i); };
+  auto s_full = [&](int i, int step) { return bars + 72 + 16 * i + 8 * (step & 1); };
+  auto p_full = [&](int i, int step) { return bars + 104 + 16 * i + 8 * (step & 1); };
+  // P V of a step is done.  (Two: a wait tells a barrier's phase from the next but not from the next but one, and a softmax
+  // thread that holds S of a step knows only that P V of the step two before is done.)
+  auto o_done = [&](int i, int step) { return bars + 136 + 16 * i + 8 * (step & 1); };
+  auto r_used = [&](int x) { return bars + 168 + 8 * x; };              // the codes of a tile have been converted
+  auto c_full = [&](int w) { return bars + 168 + 8 * (PT_RING + w); };  // codes of keys (0) or values (1) are staged
+  auto c_empty = [&](int w) { return bars + 168 + 8 * (PT_RING + 2 + w); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::OFF_SLOT);
   volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_SLOT + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -220,18 +195,20 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
   const KvSeq s = kv_seq(a.kb, b);
   const int rows = s.n * sh.group;                               // of this kv head
   if (pair * 2 * PT_ROWS >= rows) return;
-  int tiles[2], first, most;                                      // token tiles that the rows of each row tile can see
+  int steps[2];                                                   // steps that the rows of each row tile can see
   for (int i = 0; i < 2; ++i) {
     const int r0 = (pair * 2 + i) * PT_ROWS, last = (r0 + PT_ROWS < rows ? r0 + PT_ROWS : rows) - 1;
     const int lim = r0 < rows ? s.first + last / sh.group : -1;
-    tiles[i] = lim < 0 ? 0 : lim / PT_TOK + 1;
+    steps[i] = lim < 0 ? 0 : lim / PT_HALF + 1;
   }
-  most = tiles[0] > tiles[1] ? tiles[0] : tiles[1];
-  const int per_split = (most + a.splits - 1) / a.splits;
-  first = split * per_split;
-  int end[2];
-  for (int i = 0; i < 2; ++i) end[i] = tiles[i] < first + per_split ? tiles[i] : first + per_split;
-  const int stop = end[0] > end[1] ? end[0] : end[1], count = stop > first ? stop - first : 0;
+  const int most = ((steps[0] > steps[1] ? steps[0] : steps[1]) + 1) >> 1, per_split = (most + a.splits - 1) / a.splits;
+  const int first = split * per_split;                            // tiles first ... of this part
+  const int stop = first + per_split < most ? first + per_split : most, count = stop > first ? stop - first : 0;
+  int mine_of[2];                                                 // its steps that each row tile sees
+  for (int i = 0; i < 2; ++i) {
+    const int n = (steps[i] < 2 * stop ? steps[i] : 2 * stop) - 2 * first;
+    mine_of[i] = count > 0 && n > 0 ? n : 0;
+  }
 
   if (threadIdx.x == 0) {
     *flag = 0;
@@ -241,11 +218,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       ptx::mbar_init(k_empty(x), 2);
       ptx::mbar_init(v_full(x), PT_CONV);
       ptx::mbar_init(v_empty(x), 2);
-      ptx::mbar_init(s_full(x), 1);
-      ptx::mbar_init(p_full(x), 4);
-      ptx::mbar_init(p_half(x), 4);
-      ptx::mbar_init(o_full(x), 1);
-      ptx::mbar_init(turn(x), 4);
+      for (int y = 0; y < 2; ++y) { ptx::mbar_init(s_full(x, y), 1); ptx::mbar_init(p_full(x, y), 4); ptx::mbar_init(o_done(x, y), 1); }
     }
     for (int x = 0; x < PT_RING; ++x) ptx::mbar_init(r_used(x), PT_CONV);
     for (int x = 0; x < 2; ++x) { ptx::mbar_init(c_full(x), 1); ptx::mbar_init(c_empty(x), PT_CONV); }
@@ -260,7 +233,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  constexpr uint32_t COL_O = 256;                                // S (and P) of tile i at column 128 i, O at 256 + 128 i
+  constexpr uint32_t COL_O = 256;                                // S (and P) of row tile i at columns 128 i and 128 i + 64, O at 256 + 128 i
 
   if (warp < 8) {
     // ------------------------------------------------------------------------------ softmax ----
@@ -312,41 +285,52 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
     }
     SoftmaxRow w{factor, kNoMax, 0.f, 0.f};
     bool ok = true;
-    // whole tiles first, then the ones that some row of the warp does not see all of
-    const int whole = (limit_lo + 1) / PT_TOK < end[i] ? (limit_lo + 1) / PT_TOK : end[i];
+    const int n_steps = mine_of[i];
 #pragma unroll 1
-    for (int j = first; j < end[i]; ++j) {
-      const int step = j - first, others = end[1 - i] - first;
-      if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(s_full(i), step & 1, flag)))) break;
+    for (int step = 0; step < n_steps; ++step) {
+      if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(s_full(i, step), (step >> 1) & 1, flag)))) break;
       ptx::tc_fence_after();
-      float x[128];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) ptx::tmem_ld32(t_s + 32 * q, reinterpret_cast<uint32_t*>(x + 32 * q));
-      const float* rg = ring + (step % PT_RING) * PT_RING_FLOATS;
-      float c[8], off[8];
-#pragma unroll
-      for (int g = 0; g < 8; g += 4) {
-        const float4 k = *reinterpret_cast<const float4*>(rg + g), o = *reinterpret_cast<const float4*>(rg + 8 + g);
-        c[g] = fmaxf(factor * k.x, kTiny); c[g + 1] = fmaxf(factor * k.y, kTiny); c[g + 2] = fmaxf(factor * k.z, kTiny); c[g + 3] = fmaxf(factor * k.w, kTiny);
-        off[g] = o.x; off[g + 1] = o.y; off[g + 2] = o.z; off[g + 3] = o.w;
-      }
-      const float2 refs = *reinterpret_cast<const float2*>(rg + 24);      // {reference before / now, now}
+      const uint32_t t_mine = t_s + PT_HALF * (step & 1);
+      float x[PT_HALF];
+      ptx::tmem_ld32(t_mine, reinterpret_cast<uint32_t*>(x));
+      ptx::tmem_ld32(t_mine + 32, reinterpret_cast<uint32_t*>(x + 32));
+      const float4* rg = reinterpret_cast<const float4*>(ring + ((step >> 1) % PT_RING) * PT_RING_FLOATS) + (step & 1);
+      const float4 k = rg[0], off = rg[2], inv = rg[4];
+      const float4 c = make_float4(fmaxf(factor * k.x, kTiny), fmaxf(factor * k.y, kTiny), fmaxf(factor * k.z, kTiny), fmaxf(factor * k.w, kTiny));
+      const float2 refs = *reinterpret_cast<const float2*>(rg - (step & 1) + 6);      // {reference before the tile / in it, in it}
+      const float ref_ratio = (step & 1) == 0 ? refs.x : 1.f;
       w.ref = refs.y;
+      const int t0 = (2 * first + step) * PT_HALF;
       ptx::tmem_wait_ld();
-      softmax_settle<D>(w, x, c, off, refs.x, t_o, j >= whole, limit - j * PT_TOK, step == 0);
-      // The two row tiles' exponentials take turns: side by side they would share the exponential unit and then the
-      // tensor core, each idle while the other works.  (Waits only for a step that the other tile has.)
-      if (i == 0 ? step >= 1 && step - 1 < others : step < others)
-        if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(turn(i), (i == 0 ? step - 1 : step) & 1, flag)))) break;
-      softmax_exp(w, x, rg, t_s, p_half(i), turn(1 - i));
+      const float top = softmax_top(w, x, c, off, t0 + PT_HALF - 1 > limit_lo, limit - t0);
+      if (__any_sync(0xffffffffu, top > w.m + kGrow) || ref_ratio != 1.f) {
+        // rare: the maximum and the outputs are brought up to date
+        const float by = exp2f(w.m - top), scale = by * ref_ratio;
+        w.m = top;
+        w.l *= by;
+        if (step > 0) {
+          if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(o_done(i, step - 1), ((step - 1) >> 1) & 1, flag)))) break;
+          ptx::tc_fence_after();
+#pragma unroll 1
+          for (int q = 0; q < D / 16; ++q) {
+            uint32_t o[16];
+            kvp::tmem_ld16(t_o + 16 * q, o);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int t = 0; t < 16; ++t) o[t] = __float_as_uint(__uint_as_float(o[t]) * scale);
+            ptx::tmem_st16(t_o + 16 * q, o);
+          }
+        }
+      }
+      softmax_exp(w, x, c, off, inv, t_mine);
       ptx::tmem_wait_st();
       ptx::tc_fence_before();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(p_full(i));
+      if (lane == 0) ptx::mbar_arrive(p_full(i, step));
     }
     const float m = w.m, l = w.l, ref = w.ref;
-    const bool some = end[i] > first;
-    if (some && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(o_full(i), 0, flag));
+    const bool some = n_steps > 0;
+    if (some && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(o_done(i, n_steps - 1), ((n_steps - 1) >> 1) & 1, flag));
     ptx::tc_fence_after();
     const bool partial = a.splits > 1;
     const long long prow = slot * PT_ROWS + row;
@@ -422,48 +406,51 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
     const int i = __shfl_sync(0xffffffffu, warp, 0) - PT_ISSUE;
     if (i < 2) {
       const uint32_t leader = kvp::elect_one();
-      constexpr uint32_t IDESC_S = kvp::idesc_f16(128, 128, false, false), IDESC_O = kvp::idesc_f16(128, D, false, true);
+      constexpr uint32_t IDESC_S = kvp::idesc_f16(128, PT_HALF, false, false), IDESC_O = kvp::idesc_f16(128, D, false, true);
       const uint32_t t_s = tmem + 128 * i, t_o = tmem + COL_O + 128 * i;
       const uint64_t q_desc = ptx::smem_desc(sbase + S::OFF_Q + i * S::TILE, 16, 1024);
       auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, flag)); };
       bool ok = count == 0 || wait(q_full, 0);
-      for (int it = 0; it < count && ok; ++it) {
-        const int st = it & 1, ph = (it >> 1) & 1;
-        const bool mine = first + it < end[i];
-        if (!(ok = wait(k_full(st), ph))) break;
-        if (mine) {
+      const int n_steps = mine_of[i];
+      auto scores = [&](int step) {                              // S of a step
+        const int it = step >> 1, st = it & 1;
+        if ((step & 1) == 0 && !wait(k_full(st), (it >> 1) & 1)) return false;
+        if (step < n_steps) {
           ptx::tc_fence_after();
-          const uint64_t k_desc = ptx::smem_desc(sbase + S::OFF_K + st * S::TILE, 16, 1024);
+          const uint64_t k_desc = ptx::smem_desc(sbase + S::OFF_K + st * S::TILE, 16, 1024) + (uint64_t)((step & 1) * 512);
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
-            const uint64_t step = (uint64_t)((k >> 2) * 1024 + (k & 3) * 2);    // 16 channels; 64 to a block of 16 KiB
-            kvp::mma_ss(leader, t_s, q_desc + step, k_desc + step, IDESC_S, k > 0 ? 1u : 0u);
+            const uint64_t at = (uint64_t)((k >> 2) * 1024 + (k & 3) * 2);      // 16 channels; 64 to a block of 16 KiB
+            kvp::mma_ss(leader, t_s + PT_HALF * (step & 1), q_desc + at, k_desc + at, IDESC_S, k > 0 ? 1u : 0u);
           }
-          kvp::mma_commit(leader, s_full(i));
-          kvp::mma_commit(leader, k_empty(st));
-        } else if (leader) {
-          ptx::mbar_arrive(k_empty(st));
+          kvp::mma_commit(leader, s_full(i, step));
+        }
+        if ((step & 1) == 1) {                                   // the keys of the tile are done with
+          if (step - 1 < n_steps) kvp::mma_commit(leader, k_empty(st));
+          else if (leader) ptx::mbar_arrive(k_empty(st));
         }
         __syncwarp();
-        if (!(ok = wait(v_full(st), ph))) break;
-        if (mine) {
-          const uint64_t v_desc = ptx::smem_desc(sbase + S::OFF_V + st * S::TILE, 16384, 1024);
-          if (!(ok = wait(p_half(i), it & 1))) break;            // the first 64 tokens' weights, then the others'
+        return true;
+      };
+      ok = ok && (count == 0 || (scores(0) && scores(1)));
+      for (int step = 0; step < 2 * count && ok; ++step) {
+        const int it = step >> 1, st = it & 1;
+        if ((step & 1) == 0 && !(ok = wait(v_full(st), (it >> 1) & 1))) break;
+        if (step < n_steps) {
+          if (!(ok = wait(p_full(i, step), it & 1))) break;
           ptx::tc_fence_after();
+          const uint64_t v_desc = ptx::smem_desc(sbase + S::OFF_V + st * S::TILE, 16384, 1024) + (uint64_t)((step & 1) * 512);
 #pragma unroll
-          for (int k = 0; k < PT_TOK / 32; ++k)
-            kvp::mma_ts(leader, t_o, t_s + 8 * k, v_desc + (uint64_t)(k * 128), IDESC_O, it > 0 || k > 0 ? 1u : 0u);
-          if (!(ok = wait(p_full(i), it & 1))) break;
-          ptx::tc_fence_after();
-#pragma unroll
-          for (int k = PT_TOK / 32; k < PT_TOK / 16; ++k)
-            kvp::mma_ts(leader, t_o, t_s + 8 * k, v_desc + (uint64_t)(k * 128), IDESC_O, 1u);
-          kvp::mma_commit(leader, v_empty(st));
-          if (first + it + 1 == end[i]) kvp::mma_commit(leader, o_full(i));
-        } else if (leader) {
-          ptx::mbar_arrive(v_empty(st));
+          for (int k = 0; k < PT_HALF / 16; ++k)
+            kvp::mma_ts(leader, t_o, t_s + PT_HALF * (step & 1) + 8 * k, v_desc + (uint64_t)(k * 128), IDESC_O, step > 0 || k > 0 ? 1u : 0u);
+          kvp::mma_commit(leader, o_done(i, step));
+        }
+        if ((step & 1) == 1) {                                   // and its values
+          if (step - 1 < n_steps) kvp::mma_commit(leader, v_empty(st));
+          else if (leader) ptx::mbar_arrive(v_empty(st));
         }
         __syncwarp();
+        if (step + 2 < 2 * count) ok = scores(step + 2);
       }
     } else if (i == 2) {
       // ------------------------------------------------------------------------- look-ups ----
