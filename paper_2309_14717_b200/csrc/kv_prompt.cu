@@ -125,11 +125,11 @@ __device__ __forceinline__ float softmax_top(const SoftmaxRow& w, float (&x)[PT_
 }
 
 // The step's weights to P, over its own columns of S; inv: the inverse of the relative value scale.
+template <int q>
 __device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[PT_HALF], const float4 c, const float4 off, const float4 inv, uint32_t t_s) {
   const float cs[4] = {c.x, c.y, c.z, c.w}, os[4] = {off.x, off.y, off.z, off.w}, is[4] = {inv.x, inv.y, inv.z, inv.w};
   const float base = kLift - w.m;
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
+  {
     uint32_t pk[16];
 #pragma unroll
     for (int g2 = 0; g2 < 2; ++g2) {
@@ -248,37 +248,50 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
     const uint32_t t_s = tmem + lane_base + 128 * i, t_o = tmem + lane_base + COL_O + 128 * i;
     const long long slot = ((long long)h * a.slots + first_slot(sh, s, b) + pair * 2 + i);
     const bool tile_there = (pair * 2 + i) * PT_ROWS < rows;
+    // A warp moves its 32 rows of Q and of the output LANES lanes to a row, so that an access covers whole rows: a thread
+    // to a row would touch 32 lines at a time, 64 times the 256-byte rows' share of the load unit.
+    constexpr int LANES = D / 8, AT_ONCE = 32 / LANES, MOVES = 32 / AT_ONCE;
+    const int part = lane / LANES, piece = lane % LANES;
+    const long long out_row = there ? (long long)tok * sh.heads + head : -1;
     float factor;                                                // softmax_scale * log2(e) / (the row's power of two)
     {
-      // the row's largest element is brought to 2^14 .. 2^15: exact in fp16 down to 2^-28 of it
-      uint32_t mx = 0;
-      const uint4* src = reinterpret_cast<const uint4*>(a.at.q + (long long)tok * a.at.q_stride + (long long)head * D);
-      const bool load = there && QALORA_CHECK(dbg, tok, a.kb.m);
-      uint4 w[D / 8];
+      const long long q_row = there && QALORA_CHECK(dbg, tok, a.kb.m) ? (long long)tok * a.at.q_stride + (long long)head * D : -1;
+      uint4 w[MOVES];
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c) {
-        w[c] = load ? src[c] : make_uint4(0, 0, 0, 0);
-        mx = __vmaxu2(mx, w[c].x & 0x7fff7fffu); mx = __vmaxu2(mx, w[c].y & 0x7fff7fffu);
-        mx = __vmaxu2(mx, w[c].z & 0x7fff7fffu); mx = __vmaxu2(mx, w[c].w & 0x7fff7fffu);
+      for (int x = 0; x < MOVES; ++x) {
+        const long long from = __shfl_sync(0xffffffffu, q_row, x * AT_ONCE + part);
+        w[x] = from >= 0 ? *(reinterpret_cast<const uint4*>(a.at.q + from) + piece) : make_uint4(0, 0, 0, 0);
       }
-      mx = max(mx & 0xffffu, mx >> 16);
-      int e = 268 - (int)(mx >> 7);
-      e = e > 254 ? 254 : (e < 1 ? 1 : e);
-      const float f = __uint_as_float((uint32_t)e << 23);
-      factor = a.at.softmax_scale * kLog2e * (e == 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23));
-      uint8_t* image = a.q_image != nullptr && tile_there && split == 0 ? a.q_image + slot * S::TILE : nullptr;
+      // each row's largest element is brought to 2^14 .. 2^15: exact in fp16 down to 2^-28 of it
+      auto exponent = [](uint32_t mx) {
+        const int e = 268 - (int)(mx >> 7);
+        return e > 254 ? 254 : (e < 1 ? 1 : e);
+      };
+      uint8_t* image = a.q_image != nullptr && tile_there && split == 0 && QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)
+                           ? a.q_image + slot * S::TILE : nullptr;
+      uint32_t mine = 0;
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c) {
-        const uint32_t in[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
-        uint32_t out[4];
+      for (int x = 0; x < MOVES; ++x) {
+        uint32_t mx = __vmaxu2(__vmaxu2(w[x].x & 0x7fff7fffu, w[x].y & 0x7fff7fffu), __vmaxu2(w[x].z & 0x7fff7fffu, w[x].w & 0x7fff7fffu));
+        mx = max(mx & 0xffffu, mx >> 16);
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          out[x] = kvp::pack_half2(__uint_as_float(in[x] << 16) * f, __uint_as_float(in[x] & 0xffff0000u) * f);
-        const int at = (c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4);
-        const uint4 v = make_uint4(out[0], out[1], out[2], out[3]);
+        for (int o = LANES / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const uint32_t of_row = __shfl_sync(0xffffffffu, mx, (lane % AT_ONCE) * LANES);
+        if (lane / AT_ONCE == x) mine = of_row;
+        const float f = __uint_as_float((uint32_t)exponent(mx) << 23);
+        const uint32_t in[4] = {w[x].x, w[x].y, w[x].z, w[x].w};
+        uint32_t to[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          to[y] = kvp::pack_half2(__uint_as_float(in[y] << 16) * f, __uint_as_float(in[y] & 0xffff0000u) * f);
+        const int tile_row = quarter * 32 + x * AT_ONCE + part;
+        const int at = (piece >> 3) * 16384 + tile_row * 128 + (((piece & 7) ^ (tile_row & 7)) << 4);
+        const uint4 v = make_uint4(to[0], to[1], to[2], to[3]);
         *reinterpret_cast<uint4*>(smem + S::OFF_Q + i * S::TILE + at) = v;
-        if (image != nullptr && QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) *reinterpret_cast<uint4*>(image + at) = v;
+        if (image != nullptr) *reinterpret_cast<uint4*>(image + at) = v;
       }
+      const int e = exponent(mine);
+      factor = a.at.softmax_scale * kLog2e * (e == 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23));
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(q_full);
@@ -286,14 +299,19 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
     SoftmaxRow w{factor, kNoMax, 0.f, 0.f};
     bool ok = true;
     const int n_steps = mine_of[i];
-#pragma unroll 1
-    for (int step = 0; step < n_steps; ++step) {
-      if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(s_full(i, step), (step >> 1) & 1, flag)))) break;
+    const bool some = n_steps > 0;
+    // S of a step, asked for while the one before is worked on
+    float x[PT_HALF];
+    auto ask = [&](int step) {
+      if (step >= n_steps) return true;
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(s_full(i, step), (step >> 1) & 1, flag))) return false;
       ptx::tc_fence_after();
+      ptx::tmem_ld32(t_s + PT_HALF * (step & 1), reinterpret_cast<uint32_t*>(x));
+      return true;
+    };
+    auto ask_rest = [&](int step) { if (step < n_steps) ptx::tmem_ld32(t_s + PT_HALF * (step & 1) + 32, reinterpret_cast<uint32_t*>(x + 32)); };
+    auto work = [&](int step) {
       const uint32_t t_mine = t_s + PT_HALF * (step & 1);
-      float x[PT_HALF];
-      ptx::tmem_ld32(t_mine, reinterpret_cast<uint32_t*>(x));
-      ptx::tmem_ld32(t_mine + 32, reinterpret_cast<uint32_t*>(x + 32));
       const float4* rg = reinterpret_cast<const float4*>(ring + ((step >> 1) % PT_RING) * PT_RING_FLOATS) + (step & 1);
       const float4 k = rg[0], off = rg[2], inv = rg[4];
       const float4 c = make_float4(fmaxf(factor * k.x, kTiny), fmaxf(factor * k.y, kTiny), fmaxf(factor * k.z, kTiny), fmaxf(factor * k.w, kTiny));
@@ -309,7 +327,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
         w.m = top;
         w.l *= by;
         if (step > 0) {
-          if (!(ok = __all_sync(0xffffffffu, ptx::mbar_wait(o_done(i, step - 1), ((step - 1) >> 1) & 1, flag)))) break;
+          if (!__all_sync(0xffffffffu, ptx::mbar_wait(o_done(i, step - 1), ((step - 1) >> 1) & 1, flag))) return false;
           ptx::tc_fence_after();
 #pragma unroll 1
           for (int q = 0; q < D / 16; ++q) {
@@ -322,16 +340,23 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
           }
         }
       }
-      softmax_exp(w, x, c, off, inv, t_mine);
+      softmax_exp<0>(w, x, c, off, inv, t_mine);
+      softmax_exp<1>(w, x, c, off, inv, t_mine);
       ptx::tmem_wait_st();
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(p_full(i, step));
-    }
-    const float m = w.m, l = w.l, ref = w.ref;
-    const bool some = n_steps > 0;
+      if (!ask(step + 1)) return false;
+      ask_rest(step + 1);
+      return true;
+    };
+    ok = ask(0);
+    ask_rest(0);
+#pragma unroll 1
+    for (int step = 0; step < n_steps && ok; ++step) ok = work(step);
     if (some && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(o_done(i, n_steps - 1), ((n_steps - 1) >> 1) & 1, flag));
     ptx::tc_fence_after();
+    const float m = w.m, l = w.l, ref = w.ref;
     const bool partial = a.splits > 1;
     const long long prow = slot * PT_ROWS + row;
     if (a.rows != nullptr && tile_there && !partial && QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads))
@@ -342,7 +367,9 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       if (QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) a.part_ml[at] = make_float2(m, l);
     }
     const float inv = partial ? ref : (l == 0.f ? 0.f : ref / l);
-    const long long at = (long long)tok * sh.heads + head;
+    // through the warp's quarter of its tile of Q, which the products are done with; 16-byte pieces of a row in an order
+    // that keeps both sides free of bank conflicts
+    uint8_t* stage = smem + S::OFF_Q + i * S::TILE + quarter * (S::TILE / 4);
 #pragma unroll 1
     for (int q = 0; q < D / 32; ++q) {
       uint32_t o[32];
@@ -357,12 +384,20 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
 #pragma unroll
       for (int t = 0; t < 32; ++t) f[t] = l == 0.f ? 0.f : __uint_as_float(o[t]) * inv;
       if (partial) {
-        if (!tile_there || !QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) continue;
-        float4* dst = reinterpret_cast<float4*>(a.part_o + ((long long)split * a.slots * sh.kv_heads * PT_ROWS + prow) * D + 32 * q);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) dst[t] = make_float4(f[4 * t], f[4 * t + 1], f[4 * t + 2], f[4 * t + 3]);
-      } else if (there && QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) {
-        uint4* dst = reinterpret_cast<uint4*>(a.at.out + at * D + 32 * q);
+        for (int t = 0; t < 8; ++t)
+          *reinterpret_cast<float4*>(stage + lane * 128 + ((t ^ (lane & 7)) << 4)) = make_float4(f[4 * t], f[4 * t + 1], f[4 * t + 2], f[4 * t + 3]);
+        __syncwarp();
+        if (tile_there && QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) {
+          float* dst = a.part_o + ((long long)split * a.slots * sh.kv_heads * PT_ROWS + slot * PT_ROWS + quarter * 32) * D + 32 * q + 4 * (lane & 7);
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const int from = 4 * x + (lane >> 3);
+            *reinterpret_cast<float4*>(dst + from * D) = *reinterpret_cast<const float4*>(stage + from * 128 + (((lane ^ from) & 7) << 4));
+          }
+        }
+        __syncwarp();
+      } else {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           uint32_t w[4];
@@ -371,11 +406,21 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
             const __nv_bfloat162 two = __floats2bfloat162_rn(f[8 * t + 2 * y], f[8 * t + 2 * y + 1]);
             w[y] = *reinterpret_cast<const uint32_t*>(&two);
           }
-          dst[t] = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(stage + lane * (2 * D) + (((4 * q + t) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
         }
       }
     }
-    if (!partial && there) kvp::store_lse(a.at.lse, at, nullptr, 0, m, l, kLift);
+    if (!partial) {
+      __syncwarp();
+#pragma unroll
+      for (int x = 0; x < MOVES; ++x) {
+        const int from = x * AT_ONCE + part;
+        const long long to = __shfl_sync(0xffffffffu, out_row, from);
+        if (to >= 0 && QALORA_CHECK(dbg, to, (long long)a.kb.m * sh.heads))
+          *(reinterpret_cast<uint4*>(a.at.out + to * D) + piece) = *reinterpret_cast<const uint4*>(stage + from * (2 * D) + ((piece ^ (from & 7)) << 4));
+      }
+      if (there) kvp::store_lse(a.at.lse, out_row, nullptr, 0, m, l, kLift);
+    }
   } else if (warp < PT_ISSUE) {
     // --------------------------------------------------------------------------- conversion ----
     kvp::fewer_registers<40>();
