@@ -51,7 +51,7 @@ struct KvPromptScratch {
 };
 KvPromptScratch kv_prompt_scratch(const KvShape& sh, int batch, int64_t m, int max_len, bool with_score);
 int launch_kv_prompt(const KvShape& sh, const KvBatch& b, const KvAttention& a, const KvPromptScratch& s, float2* part_ml,
-                     float* part_o, uint8_t* q_image, float2* rows, int* status, cudaStream_t st);
+                     float* part_o, uint8_t* q_image, float* rows, int* status, cudaStream_t st);
 
 int launch_kv_evict(const KvShape& sh, const KvBatch& b, int budget, int recent, int8_t* codes, float* scales, float* score,
                     const int32_t* dst_table, int dst_max_blocks, int32_t* dst_lens, int32_t* kept, cudaStream_t st);

@@ -671,7 +671,7 @@ int launch_kv_attention(const KvShape& sh, const KvBatch& b, const KvAttention& 
   KvBatch many = b;
   many.n_lo = L.few + 1;
   return launch_kv_prompt(sh, many, at, L.prompt, reinterpret_cast<float2*>(base + L.pr_ml), reinterpret_cast<float*>(base + L.pr_o),
-                          reinterpret_cast<uint8_t*>(base + L.pr_q), reinterpret_cast<float2*>(base + L.pr_rows),
+                          reinterpret_cast<uint8_t*>(base + L.pr_q), reinterpret_cast<float*>(base + L.pr_rows),
                           reinterpret_cast<int*>(base + L.status), st);
 }
 
