@@ -256,45 +256,51 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
     float factor;                                                // softmax_scale * log2(e) / (the row's power of two)
     {
       const long long q_row = there && QALORA_CHECK(dbg, tok, a.kb.m) ? (long long)tok * a.at.q_stride + (long long)head * D : -1;
-      uint4 w[MOVES];
-#pragma unroll
+      uint8_t* tile = smem + S::OFF_Q + i * S::TILE;
+#pragma unroll 4
       for (int x = 0; x < MOVES; ++x) {
-        const long long from = __shfl_sync(0xffffffffu, q_row, x * AT_ONCE + part);
-        w[x] = from >= 0 ? *(reinterpret_cast<const uint4*>(a.at.q + from) + piece) : make_uint4(0, 0, 0, 0);
+        const int at_row = x * AT_ONCE + part, tile_row = quarter * 32 + at_row;
+        const long long from = __shfl_sync(0xffffffffu, q_row, at_row);
+        uint8_t* to = tile + (piece >> 3) * 16384 + tile_row * 128 + (((piece & 7) ^ (tile_row & 7)) << 4);
+        if (from >= 0) kvp::copy16_async(ptx::smem_u32(to), reinterpret_cast<const uint4*>(a.at.q + from) + piece);
+        else *reinterpret_cast<uint4*>(to) = make_uint4(0, 0, 0, 0);
       }
+      kvp::copies_done();
+      __syncwarp();
       // each row's largest element is brought to 2^14 .. 2^15: exact in fp16 down to 2^-28 of it
-      auto exponent = [](uint32_t mx) {
-        const int e = 268 - (int)(mx >> 7);
-        return e > 254 ? 254 : (e < 1 ? 1 : e);
-      };
-      uint8_t* image = a.q_image != nullptr && tile_there && split == 0 && QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)
-                           ? a.q_image + slot * S::TILE : nullptr;
-      uint32_t mine = 0;
-#pragma unroll
-      for (int x = 0; x < MOVES; ++x) {
-        uint32_t mx = __vmaxu2(__vmaxu2(w[x].x & 0x7fff7fffu, w[x].y & 0x7fff7fffu), __vmaxu2(w[x].z & 0x7fff7fffu, w[x].w & 0x7fff7fffu));
-        mx = max(mx & 0xffffu, mx >> 16);
-#pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const uint32_t of_row = __shfl_sync(0xffffffffu, mx, (lane % AT_ONCE) * LANES);
-        if (lane / AT_ONCE == x) mine = of_row;
-        const float f = __uint_as_float((uint32_t)exponent(mx) << 23);
-        const uint32_t in[4] = {w[x].x, w[x].y, w[x].z, w[x].w};
+      uint8_t* mine = tile + row * 128;
+      uint32_t mx = 0;
+#pragma unroll 4
+      for (int c = 0; c < D / 8; ++c) {
+        const uint4 v = *reinterpret_cast<const uint4*>(mine + (c >> 3) * 16384 + (((c & 7) ^ (row & 7)) << 4));
+        mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
+      }
+      mx = max(mx & 0xffffu, mx >> 16);
+      int e = 268 - (int)(mx >> 7);
+      e = e > 254 ? 254 : (e < 1 ? 1 : e);
+      const float f = __uint_as_float((uint32_t)e << 23);
+      factor = a.at.softmax_scale * kLog2e * (e == 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23));
+#pragma unroll 4
+      for (int c = 0; c < D / 8; ++c) {
+        uint4* at = reinterpret_cast<uint4*>(mine + (c >> 3) * 16384 + (((c & 7) ^ (row & 7)) << 4));
+        const uint4 v = *at;
+        const uint32_t in[4] = {v.x, v.y, v.z, v.w};
         uint32_t to[4];
 #pragma unroll
         for (int y = 0; y < 4; ++y)
           to[y] = kvp::pack_half2(__uint_as_float(in[y] << 16) * f, __uint_as_float(in[y] & 0xffff0000u) * f);
-        const int tile_row = quarter * 32 + x * AT_ONCE + part;
-        const int at = (piece >> 3) * 16384 + tile_row * 128 + (((piece & 7) ^ (tile_row & 7)) << 4);
-        const uint4 v = make_uint4(to[0], to[1], to[2], to[3]);
-        *reinterpret_cast<uint4*>(smem + S::OFF_Q + i * S::TILE + at) = v;
-        if (image != nullptr) *reinterpret_cast<uint4*>(image + at) = v;
+        *at = make_uint4(to[0], to[1], to[2], to[3]);
       }
-      const int e = exponent(mine);
-      factor = a.at.softmax_scale * kLog2e * (e == 254 ? 0x1p-127f : __uint_as_float((uint32_t)(254 - e) << 23));
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(q_full);
+      if (a.q_image != nullptr && tile_there && split == 0 && QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) {
+#pragma unroll 4
+        for (int x = 0; x < D / 8; ++x) {
+          const int of = (x >> 3) * 16384 + quarter * 4096 + (x & 7) * 512 + lane * 16;
+          *reinterpret_cast<uint4*>(a.q_image + slot * S::TILE + of) = *reinterpret_cast<const uint4*>(tile + of);
+        }
+      }
     }
     SoftmaxRow w{factor, kNoMax, 0.f, 0.f};
     bool ok = true;
@@ -368,60 +374,57 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       if (QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) a.part_ml[at] = make_float2(m, l);
     }
     const float inv = partial ? ref : (l == 0.f ? 0.f : ref / l);
-    // through the warp's quarter of its tile of Q, which the products are done with; 16-byte pieces of a row in an order
-    // that keeps both sides free of bank conflicts
+    // through the warp's quarter of its tile of Q, which the products are done with, CHUNKS pieces of 16 bytes of a row at a
+    // time in an order that keeps both sides free of bank conflicts
+    constexpr int CHUNKS = D / 8;
     uint8_t* stage = smem + S::OFF_Q + i * S::TILE + quarter * (S::TILE / 4);
+    auto place = [&](int of, int c) { return stage + of * (16 * CHUNKS) + ((c ^ (of & 7)) << 4); };
+    const int channels = partial ? 4 * CHUNKS : 8 * CHUNKS;      // of a pass
+    const bool store = tile_there && QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads);
+    const long long at = there && QALORA_CHECK(dbg, out_row, (long long)a.kb.m * sh.heads) ? out_row : -1;
 #pragma unroll 1
-    for (int q = 0; q < D / 32; ++q) {
-      uint32_t o[32];
-      if (some && ok) {
-        ptx::tmem_ld32(t_o + 32 * q, o);
-        ptx::tmem_wait_ld();
-      } else {
+    for (int q = 0; q < D; q += channels) {
+#pragma unroll 1
+      for (int c = 0; c < channels; c += 16) {
+        uint32_t o[16];
+        if (some && ok) {
+          kvp::tmem_ld16(t_o + q + c, o);
+          ptx::tmem_wait_ld();
+        }
+        float f[16];
 #pragma unroll
-        for (int t = 0; t < 32; ++t) o[t] = 0u;
-      }
-      float f[32];
+        for (int t = 0; t < 16; ++t) f[t] = !some || !ok || l == 0.f ? 0.f : __uint_as_float(o[t]) * inv;
+        if (partial) {
 #pragma unroll
-      for (int t = 0; t < 32; ++t) f[t] = l == 0.f ? 0.f : __uint_as_float(o[t]) * inv;
-      if (partial) {
+          for (int t = 0; t < 4; ++t) *reinterpret_cast<float4*>(place(lane, (c >> 2) + t)) = make_float4(f[4 * t], f[4 * t + 1], f[4 * t + 2], f[4 * t + 3]);
+        } else {
 #pragma unroll
-        for (int t = 0; t < 8; ++t)
-          *reinterpret_cast<float4*>(stage + lane * 128 + ((t ^ (lane & 7)) << 4)) = make_float4(f[4 * t], f[4 * t + 1], f[4 * t + 2], f[4 * t + 3]);
-        __syncwarp();
-        if (tile_there && QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) {
-          float* dst = a.part_o + ((long long)split * a.slots * sh.kv_heads * PT_ROWS + slot * PT_ROWS + quarter * 32) * D + 32 * q + 4 * (lane & 7);
+          for (int t = 0; t < 2; ++t) {
+            uint32_t v[4];
 #pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const int from = 4 * x + (lane >> 3);
-            *reinterpret_cast<float4*>(dst + from * D) = *reinterpret_cast<const float4*>(stage + from * 128 + (((lane ^ from) & 7) << 4));
+            for (int y = 0; y < 4; ++y) {
+              const __nv_bfloat162 two = __floats2bfloat162_rn(f[8 * t + 2 * y], f[8 * t + 2 * y + 1]);
+              v[y] = *reinterpret_cast<const uint32_t*>(&two);
+            }
+            *reinterpret_cast<uint4*>(place(lane, (c >> 3) + t)) = make_uint4(v[0], v[1], v[2], v[3]);
           }
         }
-        __syncwarp();
-      } else {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          uint32_t w[4];
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const __nv_bfloat162 two = __floats2bfloat162_rn(f[8 * t + 2 * y], f[8 * t + 2 * y + 1]);
-            w[y] = *reinterpret_cast<const uint32_t*>(&two);
-          }
-          *reinterpret_cast<uint4*>(stage + lane * (2 * D) + (((4 * q + t) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
       }
-    }
-    if (!partial) {
       __syncwarp();
-#pragma unroll
+#pragma unroll 4
       for (int x = 0; x < MOVES; ++x) {
         const int from = x * AT_ONCE + part;
-        const long long to = __shfl_sync(0xffffffffu, out_row, from);
-        if (to >= 0 && QALORA_CHECK(dbg, to, (long long)a.kb.m * sh.heads))
-          *(reinterpret_cast<uint4*>(a.at.out + to * D) + piece) = *reinterpret_cast<const uint4*>(stage + from * (2 * D) + ((piece ^ (from & 7)) << 4));
+        const uint4 v = *reinterpret_cast<const uint4*>(place(from, piece));
+        const long long to = __shfl_sync(0xffffffffu, at, from);
+        if (partial) {
+          if (store) *reinterpret_cast<uint4*>(a.part_o + ((long long)split * a.slots * sh.kv_heads * PT_ROWS + slot * PT_ROWS + quarter * 32 + from) * D + q + 4 * piece) = v;
+        } else if (to >= 0) {
+          *reinterpret_cast<uint4*>(a.at.out + to * D + 8 * piece) = v;
+        }
       }
-      if (there) kvp::store_lse(a.at.lse, out_row, nullptr, 0, m, l, kLift);
+      __syncwarp();
     }
+    if (!partial && there) kvp::store_lse(a.at.lse, out_row, nullptr, 0, m, l, kLift);
   } else if (warp < PT_ISSUE) {
     // --------------------------------------------------------------------------- conversion ----
     kvp::fewer_registers<40>();
