@@ -125,7 +125,7 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
 // One thread block per (block of tokens that is read from, kv head, sequence), half of it for keys and half for
 // values: one look-up and one scale each, 16 codes per thread and pass.
 template <int D, int PASSES, bool BF16>
-__global__ void __launch_bounds__(KV_THREADS)
+__global__ void __launch_bounds__(KV_THREADS, PASSES <= 4 ? 5 : 3)
 kv_read_kernel(KvShape sh, KvBatch kb, const int8_t* __restrict__ codes, const float* __restrict__ scales,
                void* __restrict__ k, void* __restrict__ v, int* dbg) {
   constexpr int CHUNKS = D / 16, ROWS = 128 / CHUNKS;

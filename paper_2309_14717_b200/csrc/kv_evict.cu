@@ -175,7 +175,7 @@ kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
 // One thread block per (destination block, kv head, sequence): 128 threads move the keys and 128 the
 // values.  The codes stay in registers between the maximum and the rounding.
 template <int D, int PASSES>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, PASSES <= 4 ? 6 : 3)
 kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__ kept, int8_t* codes, float* scales, float* score,
                  const int32_t* __restrict__ dst_table, int dst_max_blocks, int* dbg) {
   constexpr int CHUNKS = D / 16, ROWS = 128 / CHUNKS;
