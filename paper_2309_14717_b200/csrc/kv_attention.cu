@@ -33,6 +33,7 @@ struct AttnArgs {
   long long logit_stride;
   int batch0;            // first sequence of this launch
   int units_grid;        // thread blocks of the first kernel
+  int whole;             // each of them takes all units of one (sequence, kv head)
 };
 
 // Work is cut into units of TOK tokens of one (sequence, kv head), in this order; every thread block takes the same number
@@ -141,16 +142,24 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       if (b0 + lane < a.kb.batch) prefix[b0 + lane] = run + sum - n;
       run += __shfl_sync(0xffffffffu, sum, 31);
     }
-    const uint32_t per_block = (run + gridDim.x - 1) / gridDim.x;
+    const uint32_t per_block = a.whole ? (run > 0 ? run : 1u) : (run + gridDim.x - 1) / gridDim.x;
     if (lane == 0) { prefix[a.kb.batch] = run; prefix[a.kb.batch + 1] = per_block; }
     __syncwarp();
     if (blockIdx.x == 0)
       for (int i = lane; i < a.kb.batch + 2; i += 32) a.plan[i] = prefix[i];
   }
   __syncthreads();
-  const uint32_t total = prefix[a.kb.batch], per_block = prefix[a.kb.batch + 1];
-  const uint32_t u0 = blockIdx.x * per_block, u1 = u0 + per_block < total ? u0 + per_block : total;
-  if (u0 >= total) return;
+  uint32_t u0, u1;
+  if (a.whole) {
+    const int b = blockIdx.x / sh.kv_heads, tiles = seq_tiles<TOK>(seqs[b]);
+    u0 = prefix[b] + (uint32_t)(blockIdx.x % sh.kv_heads) * tiles;
+    u1 = u0 + tiles;
+  } else {
+    const uint32_t total = prefix[a.kb.batch], per_block = prefix[a.kb.batch + 1];
+    u0 = blockIdx.x * per_block;
+    u1 = u0 + per_block < total ? u0 + per_block : total;
+  }
+  if (u0 >= u1) return;
 
   if (warp == AT_WARPS) {
     // ---- producer: the lanes look up the blocks and scales of 32 / SUBS units ahead, then issue their copies
@@ -571,8 +580,9 @@ int attend(const AttnArgs& a, cudaStream_t st) {
     r = kv_launch(kv_attend_kernel<D, NT, SUB>, dim3((unsigned)a.units_grid), AT_THREADS, (size_t)S::total(a.kb.batch), st, map, a, debug_words());
   }
   if (r != QALORA_OK) return r;
-  const int row_blocks = a.sh.kv_heads * a.kb.max_new * a.sh.group;
+  const int row_blocks = a.whole ? 0 : a.sh.kv_heads * a.kb.max_new * a.sh.group;
   const int score_blocks = a.logits != nullptr ? a.sh.kv_heads * ((a.kb.max_len + JOIN_TOKENS - 1) / JOIN_TOKENS) : 0;
+  if (row_blocks + score_blocks == 0) return QALORA_OK;
   return kv_launch(kv_join_kernel<D, S::ROWS, S::TOK>, dim3((unsigned)(row_blocks + score_blocks), (unsigned)a.kb.batch), 128, 0, st, a,
                    row_blocks, debug_words());
 }
@@ -587,6 +597,19 @@ struct AttnLayout {
 // Rows (new tokens x heads of a group) of one kv head up to which a sequence is taken here; with more, its
 // products fill the tensor core's tiles of 128 rows.
 constexpr int kFewRows = 16;
+
+// Whether every thread block takes one whole (sequence, kv head): nothing is left to join, but the blocks are as uneven as
+// the sequences, and fewer than could run.  Even shares need the second kernel, about 3 us, and pairs / most of them
+// less units each; a unit takes about 0.6 us with one tile of rows, 1 us with two.  So `allowed` units are given up for the
+// second kernel, half of them where it runs anyway for the gathered weights.  Measured, 32 heads of 128, microseconds whole
+// / even shares: one conversation of 333 tokens 7.6 / 8.4, of 700 10.9 / 9.0; 12 of up to 1000 20.3 / 25.8; 32 of 1000
+// tokens with four new ones and 8 kv heads 28.8 / 40.0.  kWholeUnits bounds what uneven sequences cost: 12 of up to 2000
+// tokens 33.1 / 33.0, of 2000 each 36.9 / 42.7, 13 of up to 4000 62.9 / 52.1.
+constexpr int kWholeUnits = 16;
+bool whole_sequences(long long units, long long pairs, long long most, int nt, bool scores) {
+  const long long allowed = (nt == 1 ? 8 : 5) >> (scores ? 1 : 0);
+  return units <= kWholeUnits && pairs <= most && units * (most - pairs) <= allowed * most;
+}
 
 int column_tiles(const KvShape& sh, int max_new) { return max_new * sh.group <= 8 ? 1 : 2; }     // NT
 
@@ -648,6 +671,9 @@ int launch_few(const KvShape& sh, const KvBatch& b, const KvAttention& at, const
     a.kb.table = b.table + (size_t)b0 * b.max_blocks;
     const long long units = per_seq * a.kb.batch, most = (nt == 1 ? 3ll : 2ll) * device_sm_count();
     a.units_grid = (int)(units < most ? units : most);
+    const long long pairs = (long long)a.kb.batch * sh.kv_heads;
+    a.whole = whole_sequences(tiles, pairs, most, nt, at.score_out != nullptr);
+    if (a.whole) a.units_grid = (int)pairs;
     int r;
     if (sh.dim == 128) r = nt == 1 ? attend<128, 1, 1>(a, st) : attend<128, 2, 1>(a, st);
     else r = nt == 1 ? attend<64, 1, 2>(a, st) : attend<64, 2, 2>(a, st);
