@@ -7,22 +7,22 @@ namespace qalora {
 
 namespace {
 
-constexpr int KV_THREADS = 256;            // 128 threads for keys, 128 for values
-
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 __device__ __forceinline__ uint32_t max_abs2(uint32_t m, uint32_t w) { return max_u16x2(m, w & 0x7fff7fffu); }
 
 // One thread block per (block of tokens that new rows enter, kv head, sequence): the new rows of
 // that block stay in registers between the maximum and the rounding, so each element is read once.
-// PASSES rows of D elements per 128 / (D / 8) rows in flight: PASSES * 128 * 8 = block * D elements.
-template <int D, int PASSES>
-__global__ void __launch_bounds__(KV_THREADS, PASSES <= 8 ? 4 : 2)
+// T threads for keys and T for values, PASSES * T * 8 = block * D elements: T follows the block's size, so that its threads
+// are all busy, mostly with eight pieces each (three prompts of up to 4093 tokens, 32 heads: blocks of 16 x 128 elements 79 us with
+// T = 128, 52 with 32; of 16 x 64 57 and 35).
+template <int D, int PASSES, int T>
+__global__ void __launch_bounds__(2 * T, (PASSES <= 8 ? 512 : 256) / T)
 kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, long long k_stride,
                  const __nv_bfloat16* __restrict__ v, long long v_stride, int8_t* __restrict__ codes, float* __restrict__ scales,
                  float* __restrict__ score, int32_t* __restrict__ dev_status, int* dbg) {
-  constexpr int CHUNKS = D / 8, ROWS = 128 / CHUNKS;
-  __shared__ uint32_t warp_max[8];
+  constexpr int CHUNKS = D / 8, ROWS = T / CHUNKS, WARPS = T / 32;
+  __shared__ uint32_t warp_max[2 * WARPS];
   kv_begin();
   const int b = blockIdx.y, h = blockIdx.x % sh.kv_heads, j = blockIdx.x / sh.kv_heads;
   const KvSeq s = kv_seq(kb, b);
@@ -33,7 +33,7 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
   const int s0 = lo > base ? lo - base : 0;                                       // slots s0 .. s1 - 1 are new
   const int s1 = s.len - base < sh.block ? s.len - base : sh.block;
   const int raw = kb.table[(size_t)b * kb.max_blocks + jb];
-  const int which = threadIdx.x >> 7, t = threadIdx.x & 127, chunk = t % CHUNKS, row = t / CHUNKS;
+  const int which = threadIdx.x / T, t = threadIdx.x % T, chunk = t % CHUNKS, row = t / CHUNKS;
   const __nv_bfloat16* src = which == 0 ? k : v;
   const long long stride = which == 0 ? k_stride : v_stride;
 
@@ -58,8 +58,14 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
   mx = max(mx & 0xffffu, mx >> 16);
   mx = __reduce_max_sync(0xffffffffu, mx);
   if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = mx;
+  auto of_plane = [&] {
+    uint32_t most = warp_max[which * WARPS];
+#pragma unroll
+    for (int w = 1; w < WARPS; ++w) most = max(most, warp_max[which * WARPS + w]);
+    return most;
+  };
   __syncthreads();
-  mx = max(max(warp_max[which * 4], warp_max[which * 4 + 1]), max(warp_max[which * 4 + 2], warp_max[which * 4 + 3]));
+  mx = of_plane();
   const bool odd = mx >= 0x7f80u;                      // an infinity or a NaN among the new elements
   if (__syncthreads_or(odd)) {                         // (both halves take part in the barriers)
     uint32_t fin = 0;
@@ -76,7 +82,7 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
     fin = __reduce_max_sync(0xffffffffu, fin);
     if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = fin;
     __syncthreads();
-    mx = max(max(warp_max[which * 4], warp_max[which * 4 + 1]), max(warp_max[which * 4 + 2], warp_max[which * 4 + 3]));
+    mx = of_plane();
     if (odd && t == 0 && dev_status != nullptr) atomicOr(dev_status, 1);
   }
   const float need = __fdiv_rn(__uint_as_float(mx << 16), 127.f);
@@ -85,7 +91,7 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
 
   if (s0 > 0 && scale > before) {                      // the block's earlier codes under the larger scale
     const float ratio = __fdiv_rn(before, scale);
-    for (int i = t; i < s0 * (D / 16); i += 128) {
+    for (int i = t; i < s0 * (D / 16); i += T) {
       uint4 c = reinterpret_cast<uint4*>(dst)[i];
       uint32_t* w = reinterpret_cast<uint32_t*>(&c);
 #pragma unroll
@@ -118,17 +124,17 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
     *reinterpret_cast<uint2*>(dst + slot * D + chunk * 8) = out;
   }
   if (score != nullptr)
-    for (int slot = s0 + threadIdx.x; slot < s1; slot += KV_THREADS)
+    for (int slot = s0 + threadIdx.x; slot < s1; slot += 2 * T)
       score[((long long)id * sh.kv_heads + h) * sh.block + slot] = 0.f;
 }
 
 // One thread block per (block of tokens that is read from, kv head, sequence), half of it for keys and half for
 // values: one look-up and one scale each, 16 codes per thread and pass.
-template <int D, int PASSES, bool BF16>
-__global__ void __launch_bounds__(KV_THREADS, PASSES <= 4 ? 5 : 3)
+template <int D, int PASSES, int T, bool BF16>
+__global__ void __launch_bounds__(2 * T, (PASSES == 8 ? 384 : 640) / T)
 kv_read_kernel(KvShape sh, KvBatch kb, const int8_t* __restrict__ codes, const float* __restrict__ scales,
                void* __restrict__ k, void* __restrict__ v, int* dbg) {
-  constexpr int CHUNKS = D / 16, ROWS = 128 / CHUNKS;
+  constexpr int CHUNKS = D / 16, ROWS = T / CHUNKS;
   kv_begin();
   const int b = blockIdx.y, h = blockIdx.x % sh.kv_heads, j = blockIdx.x / sh.kv_heads;
   const int r0 = kb.starts[b], r1 = kb.starts[b + 1], first = kb.lens[b];         // (lens: position of the first token read)
@@ -138,7 +144,7 @@ kv_read_kernel(KvShape sh, KvBatch kb, const int8_t* __restrict__ codes, const f
   const int jb = (lo >> sh.log_block) + j, base = jb * sh.block;
   if (base >= hi) return;
   const int s0 = lo > base ? lo - base : 0, s1 = hi - base < sh.block ? hi - base : sh.block;
-  const int which = threadIdx.x >> 7, t = threadIdx.x & 127, chunk = t % CHUNKS, row = t / CHUNKS;
+  const int which = threadIdx.x / T, t = threadIdx.x % T, chunk = t % CHUNKS, row = t / CHUNKS;
   void* out = which == 0 ? k : v;
   const int id = kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, jb);
   if (id < 0 || out == nullptr) return;
@@ -187,11 +193,13 @@ kv_read_kernel(KvShape sh, KvBatch kb, const int8_t* __restrict__ codes, const f
 
 template <int D, bool BF16>
 int read_passes(const KvShape& sh, const KvBatch& b, dim3 grid, const int8_t* codes, const float* scales, void* k, void* v, cudaStream_t st) {
-  const int rows = 128 / (D / 16), passes = (sh.block + rows - 1) / rows;
-#define QALORA_KV_READ(P) \
-  case P: return kv_launch(kv_read_kernel<D, P, BF16>, grid, KV_THREADS, 0, st, sh, b, codes, scales, k, v, debug_words());
-  switch (passes) {
-    QALORA_KV_READ(1) QALORA_KV_READ(2) QALORA_KV_READ(4) QALORA_KV_READ(8)
+#define QALORA_KV_READ(P, T) return kv_launch(kv_read_kernel<D, P, T, BF16>, grid, 2 * T, 0, st, sh, b, codes, scales, k, v, debug_words());
+  switch (sh.block * (D / 16)) {                                 // pieces of 16 codes
+    case 64: QALORA_KV_READ(2, 32)
+    case 128: QALORA_KV_READ(2, 64)
+    case 256: QALORA_KV_READ(2, 128)
+    case 512: QALORA_KV_READ(4, 128)
+    case 1024: QALORA_KV_READ(8, 128)
     default: return QALORA_ERR_UNSUPPORTED_SHAPE;
   }
 #undef QALORA_KV_READ
@@ -200,13 +208,15 @@ int read_passes(const KvShape& sh, const KvBatch& b, dim3 grid, const int8_t* co
 template <int D>
 int append_passes(const KvShape& sh, const KvBatch& b, dim3 grid, const __nv_bfloat16* k, int64_t k_stride, const __nv_bfloat16* v,
                   int64_t v_stride, int8_t* codes, float* scales, float* score, int32_t* dev_status, cudaStream_t st) {
-  const int passes = sh.block * D / 1024;
-#define QALORA_KV_APPEND(P)                                                                                              \
-  case P:                                                                                                                \
-    return kv_launch(kv_append_kernel<D, P>, grid, KV_THREADS, 0, st, sh, b, k, (long long)k_stride, v, (long long)v_stride, codes, \
+#define QALORA_KV_APPEND(P, T)                                                                                             \
+    return kv_launch(kv_append_kernel<D, P, T>, grid, 2 * T, 0, st, sh, b, k, (long long)k_stride, v, (long long)v_stride, codes, \
                      scales, score, dev_status, debug_words());
-  switch (passes) {
-    QALORA_KV_APPEND(1) QALORA_KV_APPEND(2) QALORA_KV_APPEND(4) QALORA_KV_APPEND(8) QALORA_KV_APPEND(16)
+  switch (sh.block * (D / 8)) {                                  // pieces of 8 elements
+    case 128: QALORA_KV_APPEND(4, 32)
+    case 256: QALORA_KV_APPEND(8, 32)
+    case 512: QALORA_KV_APPEND(8, 64)
+    case 1024: QALORA_KV_APPEND(8, 128)
+    case 2048: QALORA_KV_APPEND(16, 128)
     default: return QALORA_ERR_UNSUPPORTED_SHAPE;
   }
 #undef QALORA_KV_APPEND

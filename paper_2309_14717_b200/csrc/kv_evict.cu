@@ -11,7 +11,6 @@ namespace qalora {
 
 namespace {
 
-constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
 constexpr int SEL_BINS = 2048;                  // 11 bits of the key per pass: 11 + 11 + 10
 constexpr int SEL_COARSE = SEL_BINS / 32;
 constexpr int SEL_MAX_CLUSTER = 8;
@@ -38,8 +37,10 @@ struct SelectArgs {
 // through distributed shared memory.  The keys stay in shared memory between the passes, so
 // the scores are read once.  Then every warp counts its range, one scan turns the counts into
 // offsets, and the places come out in order.
+template <int SEL_THREADS>
 __global__ void __launch_bounds__(SEL_THREADS)
 kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
+  constexpr int SEL_WARPS = SEL_THREADS / 32;
   extern __shared__ __align__(16) uint32_t keys[];   // [cached] when the keys fit
   __shared__ uint32_t hist[SEL_BINS];
   __shared__ uint32_t coarse[SEL_COARSE], warp_gt[SEL_WARPS], warp_eq[SEL_WARPS];
@@ -172,14 +173,18 @@ kv_select_kernel(KvShape sh, KvBatch kb, SelectArgs a, int* dbg) {
   meet();                                       // a block's shared memory is read by its cluster until here
 }
 
-// One thread block per (destination block, kv head, sequence): 128 threads move the keys and 128 the
-// values.  The codes stay in registers between the maximum and the rounding.
-template <int D, int PASSES>
-__global__ void __launch_bounds__(256, PASSES <= 4 ? 6 : 3)
+// One thread block per (destination block, kv head, sequence): T threads move the keys and T the values, up to four times 16
+// codes each, which stay in registers between the maximum and the rounding; T follows the block's size, so that
+// its threads are all busy, and 1536 threads a multiprocessor cover the look-ups (place -> block -> codes and scale):
+// 1024 leave it at 98 us for eight conversations of 2048 kept tokens, 32 heads of 128, against 87.  It is bound by the instructions
+// of the correctly rounded quotients more than by the 38 us of its bytes.  (Blocks of 16 x 64 elements with T = 128 took
+// 68 us where T = 32 takes 41.)
+template <int D, int PASSES, int T>
+__global__ void __launch_bounds__(2 * T, PASSES == 4 && T == 32 ? 20 : 768 / T)
 kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__ kept, int8_t* codes, float* scales, float* score,
                  const int32_t* __restrict__ dst_table, int dst_max_blocks, int* dbg) {
-  constexpr int CHUNKS = D / 16, ROWS = 128 / CHUNKS;
-  __shared__ float warp_max[8];
+  constexpr int CHUNKS = D / 16, ROWS = T / CHUNKS, WARPS = T / 32;
+  __shared__ float warp_max[2 * WARPS];
   kv_begin();
   const int b = blockIdx.y, h = blockIdx.x % sh.kv_heads, j = blockIdx.x / sh.kv_heads;
   int len = kb.lens[b];
@@ -191,7 +196,7 @@ kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__
   const int dst_id = kv_block(dst_table, dst_max_blocks, sh.num_blocks, b, j);
   if (dst_id < 0) return;
   const int32_t* from = kept + ((long long)b * sh.kv_heads + h) * budget + base;
-  const int which = threadIdx.x >> 7, t = threadIdx.x & 127, chunk = t % CHUNKS, row = t / CHUNKS;
+  const int which = threadIdx.x / T, t = threadIdx.x % T, chunk = t % CHUNKS, row = t / CHUNKS;
   uint4 x[PASSES];
   float s[PASSES], mx = 0.f;
 #pragma unroll
@@ -228,7 +233,9 @@ kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__
   for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = mx;
   __syncthreads();
-  mx = fmaxf(fmaxf(warp_max[which * 4], warp_max[which * 4 + 1]), fmaxf(warp_max[which * 4 + 2], warp_max[which * 4 + 3]));
+  mx = warp_max[which * WARPS];
+#pragma unroll
+  for (int y = 1; y < WARPS; ++y) mx = fmaxf(mx, warp_max[which * WARPS + y]);
   const float scale = __fdiv_rn(mx, 127.f);
   const long long plane = ((long long)dst_id * 2 + which) * sh.kv_heads + h;
   if (t == 0 && QALORA_CHECK(dbg, plane, (long long)sh.num_blocks * 2 * sh.kv_heads)) scales[plane] = scale;
@@ -257,7 +264,7 @@ kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__
     }
     *reinterpret_cast<uint4*>(dst + slot * D + chunk * 16) = make_uint4(o[0].x, o[0].y, o[1].x, o[1].y);
   }
-  for (int slot = threadIdx.x; slot < n; slot += 256) {
+  for (int slot = threadIdx.x; slot < n; slot += 2 * T) {
     const int pos = from[slot];
     const int id = QALORA_CHECK(dbg, pos, len) ? kv_block(kb.table, kb.max_blocks, sh.num_blocks, b, pos >> sh.log_block) : -1;
     const float moved = id < 0 ? 0.f : score[((long long)id * sh.kv_heads + h) * sh.block + (pos & (sh.block - 1))];
@@ -268,13 +275,18 @@ kv_gather_kernel(KvShape sh, KvBatch kb, int budget, const int32_t* __restrict__
 template <int D>
 int gather_passes(const KvShape& sh, const KvBatch& b, dim3 grid, int budget, const int32_t* kept, int8_t* codes, float* scales,
                   float* score, const int32_t* dst_table, int dst_max_blocks, cudaStream_t st) {
-  const int rows = 128 / (D / 16), passes = (sh.block + rows - 1) / rows;
-#define QALORA_KV_GATHER(P)                                                                                                  \
-  case P:                                                                                                                    \
-    return kv_launch(kv_gather_kernel<D, P>, grid, 256, 0, st, sh, b, budget, kept, codes, scales, score, dst_table,        \
+#define QALORA_KV_GATHER(P, T)                                                                                               \
+    return kv_launch(kv_gather_kernel<D, P, T>, grid, 2 * T, 0, st, sh, b, budget, kept, codes, scales, score, dst_table,    \
                      dst_max_blocks, debug_words());
-  switch (passes) {
-    QALORA_KV_GATHER(1) QALORA_KV_GATHER(2) QALORA_KV_GATHER(4) QALORA_KV_GATHER(8)
+  // (twice the threads where all blocks run at once all the same: seven sequences of 411 tokens, 40 heads of 64,
+  // cut to 149 in 14.6 us against 17.5)
+  const bool wide = (long long)grid.x * grid.y * sh.block * (D / 16) <= 2ll * 768 * device_sm_count();
+  switch (sh.block * (D / 16)) {                                 // pieces of 16 codes
+    case 64: QALORA_KV_GATHER(2, 32)
+    case 128: if (wide) QALORA_KV_GATHER(2, 64) QALORA_KV_GATHER(4, 32)
+    case 256: if (wide) QALORA_KV_GATHER(2, 128) QALORA_KV_GATHER(4, 64)
+    case 512: if (wide) QALORA_KV_GATHER(2, 256) QALORA_KV_GATHER(4, 128)
+    case 1024: if (wide) QALORA_KV_GATHER(2, 512) QALORA_KV_GATHER(4, 256)
     default: return QALORA_ERR_UNSUPPORTED_SHAPE;
   }
 #undef QALORA_KV_GATHER
@@ -294,14 +306,20 @@ int launch_kv_evict(const KvShape& sh, const KvBatch& b, int budget, int recent,
   const int per = ((b.max_len + C - 1) / C + 3) & ~3;
   if (pairs * C > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
   SelectArgs a{score, dst_lens, kept, budget, recent, per <= SEL_CACHED_KEYS ? per : 0};
+  // Few keys to a block: eight blocks of 256 threads to a multiprocessor instead of two, and cheaper meetings (480 pairs of
+  // 337 tokens 38.9 -> 29.8 us with their move; 256 of 8000 107 -> 104).  With fewer pairs than multiprocessors
+  // the many threads of one block read faster (128 pairs of 8000: 57 us against 64).
+  const int threads = per <= (pairs * C > device_sm_count() ? 8192 : 2048) ? 256 : 1024;
+  const auto kernel = threads == 256 ? kv_select_kernel<256> : kv_select_kernel<1024>;
   static PerDeviceOnce once;
   const int ok = once.run([] {
-    return cudaFuncSetAttribute(kv_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_CACHED_KEYS * 4);
+    const cudaError_t e = cudaFuncSetAttribute(kv_select_kernel<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_CACHED_KEYS * 4);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(kv_select_kernel<1024>, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_CACHED_KEYS * 4);
   });
   if (ok != QALORA_OK) return ok;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(pairs * C));
-  cfg.blockDim = dim3(SEL_THREADS);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = (size_t)a.cached * 4;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -312,7 +330,7 @@ int launch_kv_evict(const KvShape& sh, const KvBatch& b, int budget, int recent,
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  if (cudaLaunchKernelEx(&cfg, kv_select_kernel, sh, b, a, debug_words()) != cudaSuccess) return QALORA_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, kernel, sh, b, a, debug_words()) != cudaSuccess) return QALORA_ERR_CUDA;
   count_launch();
   const int most = b.max_len < budget ? b.max_len : budget, blocks = (most + sh.block - 1) / sh.block;
   if (blocks == 0) return cuda_status(cudaGetLastError());
