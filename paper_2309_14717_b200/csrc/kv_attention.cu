@@ -90,7 +90,7 @@ __host__ __device__ constexpr long long part_floats() { return (long long)ROWS *
 //   O^T = V^T P^T the transposing ldmatrix, whose 16-bit elements are pairs of channels, gives the even and the odd
 //                 channels as rows 0-7 and 8-15 of A; P^T is S^T's result through movmatrix.
 // (With the query rows as the 16 rows of the product, most of them padding, the same work took twice the products and
-// 450 instead of 250 instructions per 16 tokens: 32 conversations of up to 4096 tokens 181 us, now NNN us.)
+// 450 instead of 250 instructions per 16 tokens: 32 conversations of up to 4096 tokens 181 us, against 115: 5.2 TB/s.)
 // Codes turn into fp16 exactly (1024 + 128 + c by byte permutation, minus 1152), the query is fp16 after a
 // power-of-two scaling per row (bf16 has fewer bits), so the scores are sums of exact products in float32.
 // Every warp keeps maximum, sum and output of its own tokens; the warps meet only at the end of a row tile.

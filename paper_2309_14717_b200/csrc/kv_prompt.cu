@@ -9,7 +9,7 @@ namespace qalora {
 namespace {
 
 constexpr int PT_CONV = 8;                     // conversion warps
-constexpr int PT_THREADS = 256 + PT_CONV * 32 + 128;   // 2 x 128 softmax, conversion, 2 issuing warps (and 2 idle ones)
+constexpr int PT_THREADS = 256 + PT_CONV * 32 + 128;   // 2 x 128 softmax, conversion, 2 issuing warps, the look-ups (and one idle warp)
 constexpr int PT_ISSUE = 8 + PT_CONV;          // first issuing warp
 constexpr int PT_TOK = 128, PT_ROWS = 128;    // a tile: tokens x rows (new tokens x heads of a group)
 constexpr int PT_HALF = 64;                   // tokens of a step: half a tile
@@ -156,11 +156,19 @@ __device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[PT_H
 //   issuing warps     one per row tile: S = Q K^T of a step into one of two places in tensor memory, O += P V with P in
 //                     tensor memory;
 //   softmax threads   one per row: S from tensor memory, P back over its columns.
-// S of the next step is there while a step's softmax runs: the exponentials, which bound the kernel together with the
-// products (64 x 128 x 128 of either take the exponential unit and the tensor core the same time), never wait
-// for a product.  (Steps of 128 tokens, for whose S there is one place only, left softmax and products of a row
-// tile to alternate: 189 us for a 4096-token prompt of 32 heads against NNN.)  P V of a step is issued before S of the
-// next but one by the same thread, so that S may overwrite P.
+// S of the next step is there while a step's softmax runs: a row tile's softmax never waits for its products.  (Steps of
+// 128 tokens, for whose S there is one place only, left softmax and products of a row tile to alternate: 189 us for a
+// 4096-token prompt of 32 heads of 128, against 185.)  P V of a step is issued before S of the next but one by the same
+// thread, so that S may overwrite P.
+// What bounds it: the softmax warps.  A step takes about 2200 cycles, of which the exponential unit is busy for 1024 (64 x 128
+// exponentials of either row tile at 16 a cycle), the tensor core for 1024 to 1280 (S with 64 columns reads Q again for
+// every half tile) and the four issue slots for about 1150; the two softmax warps of a scheduler run in step, so that the
+// unit rests while both look for their maxima.  Taking turns (by mbarriers, by named barriers), half a step's offset at the start,
+// S fetched in the middle of the step before, a share of the exponentials on the FMA pipe and two places of registers
+// for S were each measured and none was faster.  A block's beginning and end cost another 15 000 cycles, most of them
+// waits for instructions that no block has run for a while: hence the rolled loops there, 172 us against 176.  (One block to
+// a multiprocessor that takes over the work of blocks not yet started, with rows and tiles of the next piece brought in
+// during the last: 175 against 176.)
 template <int D>
 __global__ void __launch_bounds__(PT_THREADS, 1)
 kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) {
@@ -621,12 +629,30 @@ struct PsSmem {
   static constexpr int TOTAL = OFF_SLOT + 16 + 1024;
 };
 
+// 2^y of two values on the FMA pipe: y = n + r with |r| <= 1/2 by adding 1.5 * 2^23, 2^r by its minimax polynomial
+// of degree 4 (relative error 2.7e-6, 2^-18.5), n added to the exponent.  y <= 126; below -125 the result is 2^-125.
+__device__ __forceinline__ float2 exp2_fma(float2 y) {
+  y.x = fmaxf(y.x, -125.f);
+  y.y = fmaxf(y.y, -125.f);
+  const float2 n = ptx::fadd2(y, make_float2(12582912.f, 12582912.f));
+  const float2 r = ptx::ffma2(ptx::fadd2(n, make_float2(-12582912.f, -12582912.f)), make_float2(-1.f, -1.f), y);
+  float2 p = make_float2(0.0095701022f, 0.0095701022f);
+  p = ptx::ffma2(p, r, make_float2(0.055917859f, 0.055917859f));
+  p = ptx::ffma2(p, r, make_float2(0.24024744f, 0.24024744f));
+  p = ptx::ffma2(p, r, make_float2(0.69312179f, 0.69312179f));
+  p = ptx::ffma2(p, r, make_float2(0.99999928f, 0.99999928f));
+  p.x = __uint_as_float(__float_as_uint(p.x) + (__float_as_uint(n.x) << 23));
+  p.y = __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(n.y) << 23));
+  return p;
+}
+
 // The weights that 128 tokens of one kv head gather: S^T = K Q^T with the tokens as the rows of the product, so
 // that a thread owns a token and adds up exp2(S * factor - lse) over the rows without any exchange.
 // The row tiles come as the images that kv_prompt_kernel left.  Two groups of 128 threads, each with its accumulator,
 // take the row tiles in turn, and two blocks share a multiprocessor, so that one's tile of keys is fetched and its products
-// run while the other's exponentials do.  (One block of four accumulators: 180 us for two pieces of up to 700 tokens
-// against 12345 cached ones with 32 heads, against 132 us; 8 x 134 million exponentials take 57 us.)
+// run while the other's exponentials do.  Those bound it: two pieces of up to 700 tokens, 32 heads of 64, against up to 12345
+// cached ones 180 us with one block of four accumulators, 138 with two blocks (the exponential unit busy for 71 % of the
+// time), 128 with a quarter of the exponentials on the FMA pipe (an eighth 133, three eighths 135, half 145).
 template <int D>
 __global__ void __launch_bounds__(320, 2)
 kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, int* dbg) {
@@ -720,7 +746,12 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, in
           float2 e0 = ptx::ffma2(ptx::fmul2(make_float2(v[4 * x], v[4 * x + 1]), kk), make_float2(f.x, f.y), make_float2(g.x, g.y));
           float2 e1 = ptx::ffma2(ptx::fmul2(make_float2(v[4 * x + 2], v[4 * x + 3]), kk), make_float2(f.z, f.w), make_float2(g.z, g.w));
           e0.x = kvp::exp2_fast(e0.x); e0.y = kvp::exp2_fast(e0.y);
-          e1.x = kvp::exp2_fast(e1.x); e1.y = kvp::exp2_fast(e1.y);
+          if (x % 2 == 1) {                                      // a quarter of them
+            e1 = exp2_fma(e1);
+          } else {
+            e1.x = kvp::exp2_fast(e1.x);
+            e1.y = kvp::exp2_fast(e1.y);
+          }
           part[0] = ptx::fadd2(part[0], e0);
           part[1] = ptx::fadd2(part[1], e1);
         }
