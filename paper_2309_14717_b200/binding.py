@@ -368,9 +368,38 @@ def alloc_kv_cache(d: KvDesc, device="cuda"):
     return codes, scales, score
 
 
-# The cache calls are made once per layer and generated token, beside kernels of a few microseconds: their checks take
-# a fast path that only compares, pointers go to ctypes as plain integers, and the current stream is asked for as its
-# handle (constructing torch.cuda.current_stream() alone takes 3 us).
+# The cache calls are made once per layer and generated token, beside kernels of a few microseconds.  So each first asks
+# for the pointers of dense device tensors of the right types and shapes, one comparison after the other (_kv_at and
+# what uses it: None where something does not fit), and only then names what is wrong, or takes rows that lie apart.  Pointers
+# go to ctypes as plain integers, and the current stream is asked for as its handle (torch.cuda.current_stream() alone
+# takes 3 us).
+_I8, _I32, _F32, _BF16 = torch.int8, torch.int32, torch.float32, torch.bfloat16
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _kv_at(t, dtype, shape):
+    """Pointer of a dense device tensor of this type and shape; None when it is something else."""
+    return t.data_ptr() if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous() else None
+
+
+def _kv_batch_at(starts, lens, table):
+    """(batch, max_blocks, pointers of starts, lens and table), or None."""
+    shape = table.shape
+    if len(shape) != 2:
+        return None
+    batch, max_blocks = shape
+    p_lens, p_table = _kv_at(lens, _I32, (batch,)), _kv_at(table, _I32, shape)
+    p_starts = _kv_at(starts, _I32, (batch + 1,)) if starts is not None else 0
+    return None if p_lens is None or p_table is None or p_starts is None else (batch, max_blocks, p_starts, p_lens, p_table)
+
+
+def _kv_cache_at(d, codes, scales):
+    """(pointers of codes and scales), or None."""
+    n, h = d.num_blocks, d.kv_heads
+    p_codes, p_scales = _kv_at(codes, _I8, (n, 2, h, d.block_tokens, d.head_dim)), _kv_at(scales, _F32, (n, 2, h))
+    return None if p_codes is None or p_scales is None else (p_codes, p_scales)
+
+
 def _kv_want(name, t, dtype, shape):
     if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
@@ -378,12 +407,10 @@ def _kv_want(name, t, dtype, shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, wanted {shape}")
 
 
-def _kv_cache_want(d, codes, scales, score=None):
-    n, h, b = d.num_blocks, d.kv_heads, d.block_tokens
-    _kv_want("codes", codes, torch.int8, (n, 2, h, b, d.head_dim))
+def _kv_cache_want(d, codes, scales):
+    n, h = d.num_blocks, d.kv_heads
+    _kv_want("codes", codes, torch.int8, (n, 2, h, d.block_tokens, d.head_dim))
     _kv_want("scales", scales, torch.float32, (n, 2, h))
-    if score is not None:
-        _kv_want("score", score, torch.float32, (n, h, b))
 
 
 def _kv_batch(starts, lens, table):
@@ -399,11 +426,11 @@ def _kv_batch(starts, lens, table):
 
 def _kv_rows(name, t, heads, dim):
     """Row stride of bf16 rows [m, heads, dim] whose rows may lie apart, checked."""
+    if t.dtype is _BF16 and t.shape[1:] == (heads, dim) and t.is_cuda and t.is_contiguous():
+        return heads * dim
     _kv_want(name, t, torch.bfloat16, (t.shape[0], heads, dim))
     if not t.is_cuda:
         raise ValueError("tensors must live on a CUDA device")
-    if t.is_contiguous():
-        return heads * dim
     row, head, last = t.stride()
     if last != 1 or (heads > 1 and head != dim):
         raise ValueError(f"{name}: the heads of a row must lie one behind the other")
@@ -420,40 +447,69 @@ def _kv_ptr(t):
     return t.data_ptr()
 
 
+def _kv_dense(name, t, dtype, shape):
+    """Pointer of a dense device tensor, checked."""
+    p = _kv_at(t, dtype, shape)
+    if p is None:
+        _kv_want(name, t, dtype, shape)
+        return _kv_ptr(t)
+    return p
+
+
+def _kv_score(d, t):
+    return _kv_dense("score", t, _F32, (d.num_blocks, d.kv_heads, d.block_tokens))
+
+
+def _kv_checked(d, starts, lens, table, codes, scales, *rows):
+    """What _kv_batch_at and _kv_cache_at give, where one of them found something amiss: says what (types and shapes first,
+    those of the `rows`, (name, tensor, heads), among them)."""
+    batch, max_blocks = _kv_batch(starts, lens, table)
+    _kv_cache_want(d, codes, scales)
+    for name, t, heads in rows:
+        _kv_rows(name, t, heads, d.head_dim)
+    return (batch, max_blocks, _kv_ptr(starts), _kv_ptr(lens), _kv_ptr(table)), (_kv_ptr(codes), _kv_ptr(scales))
+
+
 def _kv_stream(stream, t):
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(t.get_device())
+    return stream.cuda_stream if stream is not None else _current_stream(t.get_device())
 
 
 def qalora_kv_append(d: KvDesc, max_new: int, starts, lens, table, k, v, codes, scales, score=None, dev_status=None,
                      stream=None):
     """Stores the new tokens' keys and values (rows k, v bf16 [m, kv_heads, head_dim]) in the cache."""
-    batch, max_blocks = _kv_batch(starts, lens, table)
-    _kv_cache_want(d, codes, scales, score)
-    k_stride = _kv_rows("k", k, d.kv_heads, d.head_dim)
-    v_stride = _kv_rows("v", v, d.kv_heads, d.head_dim)
-    if v.shape[0] != k.shape[0]:
+    at, pool = _kv_batch_at(starts, lens, table), _kv_cache_at(d, codes, scales)
+    if at is None or pool is None:
+        at, pool = _kv_checked(d, starts, lens, table, codes, scales, ("k", k, d.kv_heads), ("v", v, d.kv_heads))
+    heads, dim = d.kv_heads, d.head_dim
+    k_stride, v_stride = _kv_rows("k", k, heads, dim), _kv_rows("v", v, heads, dim)
+    m = k.shape[0]
+    if v.shape[0] != m:
         raise ValueError("k and v have different numbers of rows")
-    _check("qalora_kv_append", load().qalora_kv_append(byref(d), batch, k.shape[0], max_new, _kv_ptr(starts), _kv_ptr(lens), _kv_ptr(table),
-                                                       max_blocks, k.data_ptr(), k_stride, v.data_ptr(), v_stride, _kv_ptr(codes), _kv_ptr(scales),
-                                                       _kv_ptr(score), _kv_ptr(dev_status), _kv_stream(stream, codes)))
+    batch, max_blocks, p_starts, p_lens, p_table = at
+    _check("qalora_kv_append", load().qalora_kv_append(
+        byref(d), batch, m, max_new, p_starts, p_lens, p_table, max_blocks, k.data_ptr(), k_stride, v.data_ptr(), v_stride, pool[0], pool[1],
+        _kv_score(d, score) if score is not None else None, _kv_ptr(dev_status), _kv_stream(stream, codes)))
 
 
 def qalora_kv_read(d: KvDesc, max_new: int, starts, first, table, codes, scales, k, v, stream=None):
     """Reads tokens back: row i of sequence b is its token first[b] + i, into k, v [m, kv_heads, head_dim] (float32 or
     bfloat16; one of the two may be None)."""
-    batch, max_blocks = _kv_batch(starts, first, table)
-    _kv_cache_want(d, codes, scales)
     out = k if k is not None else v
     if out is None:
         raise ValueError("k and v are both None")
-    if out.dtype not in (torch.float32, torch.bfloat16):
+    dtype = out.dtype
+    if dtype is not _F32 and dtype is not _BF16:
         raise ValueError("k and v must be float32 or bfloat16")
-    for name, t in (("k", k), ("v", v)):
-        if t is not None:
-            _kv_want(name, t, out.dtype, (out.shape[0], d.kv_heads, d.head_dim))
-    _check("qalora_kv_read", load().qalora_kv_read(byref(d), batch, out.shape[0], max_new, _kv_ptr(starts), _kv_ptr(first), _kv_ptr(table),
-                                                   max_blocks, _kv_ptr(codes), _kv_ptr(scales), _kv_ptr(k), _kv_ptr(v),
-                                                   1 if out.dtype == torch.bfloat16 else 0, _kv_stream(stream, codes)))
+    at, pool = _kv_batch_at(starts, first, table), _kv_cache_at(d, codes, scales)
+    if at is None or pool is None:
+        at, pool = _kv_checked(d, starts, first, table, codes, scales)
+    m = out.shape[0]
+    shape = (m, d.kv_heads, d.head_dim)
+    p_k, p_v = (None if t is None else _kv_dense(name, t, dtype, shape) for name, t in (("k", k), ("v", v)))
+    batch, max_blocks, p_starts, p_first, p_table = at
+    _check("qalora_kv_read", load().qalora_kv_read(
+        byref(d), batch, m, max_new, p_starts, p_first, p_table, max_blocks, pool[0], pool[1], p_k, p_v, 1 if dtype is _BF16 else 0,
+        _kv_stream(stream, codes)))
 
 
 def qalora_kv_attention_workspace_bytes(d: KvDesc, batch: int, m: int, max_new: int, max_len: int, with_score: bool) -> int:
@@ -474,34 +530,35 @@ def qalora_kv_attention(d: KvDesc, max_new: int, max_len: int, starts, lens, tab
                         lse=None, score_in=None, score_out=None, workspace=None, stream=None):
     """out bf16 [m, heads, head_dim] = attention of the new tokens (rows q) over their sequences in the cache; lse float32
     [m, heads]; score_out = score_in + the attention weight that each cached token gathered."""
-    batch, max_blocks = _kv_batch(starts, lens, table)
-    _kv_cache_want(d, codes, scales)
-    q_stride = _kv_rows("q", q, d.heads, d.head_dim)
+    at, pool = _kv_batch_at(starts, lens, table), _kv_cache_at(d, codes, scales)
+    if at is None or pool is None:
+        at, pool = _kv_checked(d, starts, lens, table, codes, scales, ("q", q, d.heads))
+    heads, dim = d.heads, d.head_dim
+    q_stride = _kv_rows("q", q, heads, dim)
     m = q.shape[0]
-    _kv_want("out", out, torch.bfloat16, (m, d.heads, d.head_dim))
-    if lse is not None:
-        _kv_want("lse", lse, torch.float32, (m, d.heads))
-    for t in (score_in, score_out):
-        if t is not None:
-            _kv_want("score", t, torch.float32, (d.num_blocks, d.kv_heads, d.block_tokens))
+    p_out = _kv_dense("out", out, _BF16, (m, heads, dim))
+    p_lse = _kv_dense("lse", lse, _F32, (m, heads)) if lse is not None else None
+    p_in = _kv_score(d, score_in) if score_in is not None else None
+    p_score = _kv_score(d, score_out) if score_out is not None else None
+    batch, max_blocks, p_starts, p_lens, p_table = at
     _check("qalora_kv_attention", load().qalora_kv_attention(
-        byref(d), batch, m, max_new, max_len, _kv_ptr(starts), _kv_ptr(lens), _kv_ptr(table), max_blocks, q.data_ptr(), q_stride, _kv_ptr(codes),
-        _kv_ptr(scales), softmax_scale, _kv_ptr(out), _kv_ptr(lse), _kv_ptr(score_in), _kv_ptr(score_out), _kv_ptr(workspace),
-        workspace.numel() * workspace.element_size() if workspace is not None else 0, _kv_stream(stream, codes)))
+        byref(d), batch, m, max_new, max_len, p_starts, p_lens, p_table, max_blocks, q.data_ptr(), q_stride, pool[0], pool[1], softmax_scale,
+        p_out, p_lse, p_in, p_score, _kv_ptr(workspace), workspace.nbytes if workspace is not None else 0, _kv_stream(stream, codes)))
 
 
 def qalora_kv_evict(d: KvDesc, max_len: int, budget: int, recent: int, lens, table, codes, scales, score, dst_table, dst_lens, kept,
                     stream=None):
     """Copies at most `budget` tokens of each sequence and kv head (the last `recent` and those of largest score) to the
     blocks of dst_table; dst_lens int32 [batch] and kept int32 [batch, kv_heads, budget] say how many and which."""
-    batch, max_blocks = _kv_batch(None, lens, table)
-    _kv_cache_want(d, codes, scales, score)
-    _kv_want("dst_table", dst_table, torch.int32, (batch, dst_table.shape[-1]))
-    _kv_want("dst_lens", dst_lens, torch.int32, (batch,))
-    _kv_want("kept", kept, torch.int32, (batch, d.kv_heads, budget))
+    at, pool = _kv_batch_at(None, lens, table), _kv_cache_at(d, codes, scales)
+    if at is None or pool is None:
+        at, pool = _kv_checked(d, None, lens, table, codes, scales)
+    batch, max_blocks, _, p_lens, p_table = at
+    dst_max = dst_table.shape[-1]
     _check("qalora_kv_evict", load().qalora_kv_evict(
-        byref(d), batch, max_len, budget, recent, _kv_ptr(lens), _kv_ptr(table), max_blocks, _kv_ptr(codes), _kv_ptr(scales), _kv_ptr(score),
-        _kv_ptr(dst_table), dst_table.shape[1], _kv_ptr(dst_lens), _kv_ptr(kept), _kv_stream(stream, codes)))
+        byref(d), batch, max_len, budget, recent, p_lens, p_table, max_blocks, pool[0], pool[1], _kv_score(d, score),
+        _kv_dense("dst_table", dst_table, _I32, (batch, dst_max)), dst_max, _kv_dense("dst_lens", dst_lens, _I32, (batch,)),
+        _kv_dense("kept", kept, _I32, (batch, d.kv_heads, budget)), _kv_stream(stream, codes)))
 
 
 def qalora_kernel_launches() -> int:
