@@ -33,7 +33,8 @@ int check_batch(int32_t batch, int64_t m, int32_t max_new, int32_t max_blocks) {
 
 KvBatch make_batch(const KvShape& sh, const int32_t* starts, const int32_t* lens, const int32_t* table, int32_t batch,
                    int32_t max_blocks, int64_t m, int32_t max_new, int64_t max_len) {
-  const int64_t capacity = (int64_t)max_blocks * sh.block, most = capacity < 0x7fffff00 ? capacity : 0x7fffff00;
+  // (the kernels' positions, a step of a loop behind the last one included, stay below 2^31)
+  const int64_t capacity = (int64_t)max_blocks * sh.block, most = capacity < 0x7fff0000 ? capacity : 0x7fff0000;
   KvBatch b{};
   b.starts = starts; b.lens = lens; b.table = table;
   b.batch = batch; b.max_blocks = max_blocks;

@@ -28,8 +28,9 @@ kv_append_kernel(KvShape sh, KvBatch kb, const __nv_bfloat16* __restrict__ k, lo
   const KvSeq s = kv_seq(kb, b);
   if (s.n == 0) return;
   const int lo = s.first > 0 ? s.first : 0;
-  const int jb = (lo >> sh.log_block) + j, base = jb * sh.block;
-  if (base >= s.len) return;
+  const int jb = (lo >> sh.log_block) + j;
+  if (jb > (s.len - 1) >> sh.log_block) return;        // (compared as blocks: a position behind the last one may pass 2^31)
+  const int base = jb * sh.block;
   const int s0 = lo > base ? lo - base : 0;                                       // slots s0 .. s1 - 1 are new
   const int s1 = s.len - base < sh.block ? s.len - base : sh.block;
   const int raw = kb.table[(size_t)b * kb.max_blocks + jb];
@@ -139,10 +140,11 @@ kv_read_kernel(KvShape sh, KvBatch kb, const int8_t* __restrict__ codes, const f
   const int b = blockIdx.y, h = blockIdx.x % sh.kv_heads, j = blockIdx.x / sh.kv_heads;
   const int r0 = kb.starts[b], r1 = kb.starts[b + 1], first = kb.lens[b];         // (lens: position of the first token read)
   if (r0 < 0 || r1 < r0 || r1 > kb.m || r1 - r0 > kb.max_new) return;
-  const long long stop = (long long)first + (r1 - r0), room = (long long)kb.max_blocks * sh.block;
-  const int lo = first > 0 ? first : 0, hi = (int)(stop < room ? stop : room);    // positions read: lo .. hi - 1
-  const int jb = (lo >> sh.log_block) + j, base = jb * sh.block;
-  if (base >= hi) return;
+  const long long stop = (long long)first + (r1 - r0);
+  const int lo = first > 0 ? first : 0, hi = (int)(stop < kb.max_len ? stop : kb.max_len);   // positions read: lo .. hi - 1
+  const int jb = (lo >> sh.log_block) + j;
+  if (lo >= hi || jb > (hi - 1) >> sh.log_block) return;   // (first may be any number: jb * block may pass 2^31)
+  const int base = jb * sh.block;
   const int s0 = lo > base ? lo - base : 0, s1 = hi - base < sh.block ? hi - base : sh.block;
   const int which = threadIdx.x / T, t = threadIdx.x % T, chunk = t % CHUNKS, row = t / CHUNKS;
   void* out = which == 0 ? k : v;

@@ -861,7 +861,7 @@ KvPromptScratch kv_prompt_scratch(const KvShape& sh, int batch, int64_t m, int m
   // beyond its own, its rows go through memory in float32, and it has two tiles at least.  (Two pieces of up to
   // 700 tokens, 32 heads on 8 of 64, against 12345 cached ones, weights gathered: 404 us uncut, 349 cut; a prompt of 1000
   // tokens with 8 heads of 128: 31 and 23.)
-  const long long blocks = sh.kv_heads * ((long long)m * sh.group / (2 * PT_ROWS) + batch), tiles = (max_len + PT_TOK - 1) / PT_TOK;
+  const long long blocks = sh.kv_heads * ((long long)m * sh.group / (2 * PT_ROWS) + batch), tiles = ((long long)max_len + PT_TOK - 1) / PT_TOK;
   const long long sms = device_sm_count(), most = tiles / 2 < 2 * sms ? tiles / 2 : 2 * sms;
   long long splits = 1, least = 0;
   for (long long n = 1; n <= most || n == 1; ++n) {
