@@ -60,20 +60,27 @@ int launch_kv_evict(const KvShape& sh, const KvBatch& b, int budget, int recent,
 // Launches a kernel of the cache so that its blocks may be set up while the kernel before it in the stream ends
 // (programmatic dependent launch); kv_begin() is the first thing such a kernel does that touches memory.
 template <class... P, class... A>
-inline int kv_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args) {
+inline int kv_launch_clusters(void (*kernel)(P...), dim3 grid, int cluster, int threads, size_t smem, cudaStream_t st, A... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) return QALORA_ERR_CUDA;
   count_launch();
   return QALORA_OK;
+}
+template <class... P, class... A>
+inline int kv_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args) {
+  return kv_launch_clusters(kernel, grid, 1, threads, smem, st, args...);
 }
 // Waits for the kernel before, and only then lets the one after be set up: it can never run beside one before this.
 __device__ __forceinline__ void kv_begin() {

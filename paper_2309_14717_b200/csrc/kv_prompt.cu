@@ -1,8 +1,12 @@
 // Attention of many new tokens over the 8-bit key/value cache (a prompt, or the next piece of one) on
 // the 5th-generation tensor cores, and the weights that its cached tokens gather.
 #define QALORA_TU 14
+#include <cooperative_groups.h>
+
 #include "kv.cuh"
 #include "kv_ptx.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace qalora {
 
@@ -13,6 +17,7 @@ constexpr int PT_THREADS = 256 + PT_CONV * 32 + 128;   // 2 x 128 softmax, conve
 constexpr int PT_ISSUE = 8 + PT_CONV;          // first issuing warp
 constexpr int PT_TOK = 128, PT_ROWS = 128;    // a tile: tokens x rows (new tokens x heads of a group)
 constexpr int PT_HALF = 64;                   // tokens of a step: half a tile
+constexpr int PS_MAX_CLUSTER = 8;             // thread blocks that share a token tile's row tiles
 constexpr int PT_RING = 8;                    // tiles whose blocks and scales are kept
 constexpr int PT_RING_FLOATS = 48;            // ks[8], log2 of vs / ref [8], ref / vs [8], {ref_before / ref, ref, all there}, blocks of
                                               // keys [8] at 32 and of values [8] at 40
@@ -622,8 +627,8 @@ struct PsSmem {
   static constexpr int OFF_K = 0, OFF_Q = TILE;
   static constexpr int OFF_ROWS = OFF_Q + STAGES * TILE;         // [NROWS][2][128]: read after the tile itself is free
   static constexpr int NROWS = 4;
-  static constexpr int OFF_SUM = OFF_ROWS + NROWS * 128 * 8;     // [128] sums of the second half
-  static constexpr int OFF_BARS = OFF_SUM + 512;
+  static constexpr int OFF_SUM = OFF_ROWS + NROWS * 128 * 8;     // [2][128] sums of the second half; of the block
+  static constexpr int OFF_BARS = OFF_SUM + 1024;
   static constexpr int NBARS = 1 + 2 * STAGES + 2 * 2;
   static constexpr int OFF_SLOT = OFF_BARS + NBARS * 8 + 8;
   static constexpr int TOTAL = OFF_SLOT + 16 + 1024;
@@ -648,14 +653,16 @@ __device__ __forceinline__ float2 exp2_fma(float2 y) {
 
 // The weights that 128 tokens of one kv head gather: S^T = K Q^T with the tokens as the rows of the product, so
 // that a thread owns a token and adds up exp2(S * factor - lse) over the rows without any exchange.
-// The row tiles come as the images that kv_prompt_kernel left.  Two groups of 128 threads, each with its accumulator,
-// take the row tiles in turn, and two blocks share a multiprocessor, so that one's tile of keys is fetched and its products
-// run while the other's exponentials do.  Those bound it: two pieces of up to 700 tokens, 32 heads of 64, against up to 12345
-// cached ones 180 us with one block of four accumulators, 138 with two blocks (the exponential unit busy for 71 % of the
-// time), 128 with a quarter of the exponentials on the FMA pipe (an eighth 133, three eighths 135, half 145).
+// The row tiles come as the images that kv_prompt_kernel left; where there are few token tiles, a cluster of blocks
+// shares a tile's row tiles and adds its sums, in the order of the blocks, through distributed shared memory.  Two
+// groups of 128 threads, each with its accumulator, take the row tiles in turn, and two blocks share a multiprocessor,
+// so that one's tile of keys is fetched and its products run while the other's exponentials do.  Those bound it: two
+// pieces of up to 700 tokens, 32 heads of 64, against up to 12345 cached ones 180 us with one block of four
+// accumulators, 138 with two blocks (the exponential unit busy for 71 % of the time), 128 with a quarter of the
+// exponentials on the FMA pipe (an eighth 133, three eighths 135, half 145).
 template <int D>
 __global__ void __launch_bounds__(320, 2)
-kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, int* dbg) {
+kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int* dbg) {
   using S = PsSmem<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -670,12 +677,15 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, in
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   kv_begin();
   const KvShape& sh = a.sh;
-  const int b = blockIdx.y, h = blockIdx.x % sh.kv_heads, j = blockIdx.x / sh.kv_heads, t0 = j * PT_TOK;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), unit = blockIdx.x / C;
+  const int b = blockIdx.y, h = unit % sh.kv_heads, j = unit / sh.kv_heads, t0 = j * PT_TOK;
   const KvSeq s = kv_seq(a.kb, b);
-  if (s.n == 0 || t0 >= s.len) return;
+  if (s.n == 0 || t0 >= s.len) return;                           // (the same for the whole cluster)
   const int rows = s.n * sh.group, row_tiles = (rows + PT_ROWS - 1) / PT_ROWS;
-  const int rt0 = t0 > s.first ? (int)(((long long)(t0 - s.first) * sh.group) / PT_ROWS) : 0;   // the first that sees a token of the tile
-  const int count = row_tiles - rt0;
+  const int seen = t0 > s.first ? (int)(((long long)(t0 - s.first) * sh.group) / PT_ROWS) : 0;   // the first that sees a token of the tile
+  const int share = (row_tiles - seen + C - 1) / C, rt0 = seen + rank * share;                   // this block's row tiles
+  const int count = rt0 >= row_tiles ? 0 : (rt0 + share < row_tiles ? share : row_tiles - rt0);
   const long long slot0 = (long long)h * a.slots + first_slot(sh, s, b) + rt0;
 
   if (threadIdx.x == 0) {
@@ -694,6 +704,9 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, in
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  float* sums = reinterpret_cast<float*>(smem + S::OFF_SUM);
+  int id = -1;                                                   // block of the thread's token
+  float before = 0.f;                                            // what the token had gathered
 
   if (warp < 8) {
     const int half = warp >> 2, quarter = warp & 3, token = quarter * 32 + lane;
@@ -705,9 +718,9 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, in
         const int row = p * Map::ROWS + map.row0, t = t0 + row;
         uint4 c = make_uint4(0, 0, 0, 0);
         if (t < s.len) {
-          const int id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t >> sh.log_block);
-          if (id >= 0)
-            c = *reinterpret_cast<const uint4*>(a.at.codes + ((((long long)id * 2) * sh.kv_heads + h) * sh.block + (t & (sh.block - 1))) * D + map.piece * 16);
+          const int from = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t >> sh.log_block);
+          if (from >= 0)
+            c = *reinterpret_cast<const uint4*>(a.at.codes + ((((long long)from * 2) * sh.kv_heads + h) * sh.block + (t & (sh.block - 1))) * D + map.piece * 16);
         }
         store_codes(smem + S::OFF_K, row, map.piece, c);
       }
@@ -716,8 +729,10 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, in
       if (lane == 0) ptx::mbar_arrive(k_full);
     }
     const int t = t0 + token;
-    const int id = t < s.len ? kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t >> sh.log_block) : -1;
+    if (t < s.len) id = kv_block(a.kb.table, a.kb.max_blocks, sh.num_blocks, b, t >> sh.log_block);
     const float ks = id >= 0 ? a.at.scales[((long long)id * 2) * sh.kv_heads + h] : 0.f;
+    const long long own = ((long long)id * sh.kv_heads + h) * sh.block + (t & (sh.block - 1));
+    if (half == 0 && rank == 0 && id >= 0 && a.at.score_in != nullptr) before = a.at.score_in[own];
     // the first row of this tile's first row tile that sees the token (rows before it are masked)
     const long long sees = t > s.first ? (long long)(t - s.first) * sh.group - (long long)rt0 * PT_ROWS : 0;
     const float2 kk = make_float2(fmaxf(ks, kTiny), fmaxf(ks, kTiny));
@@ -762,14 +777,9 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, in
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(s_empty(half));
     }
-    float* other = reinterpret_cast<float*>(smem + S::OFF_SUM);
-    if (half == 1) other[token] = sum;
+    if (half == 1) sums[token] = sum;
     ptx::named_barrier(1, 256);
-    if (half == 0 && id >= 0) {
-      const long long at = ((long long)id * sh.kv_heads + h) * sh.block + (t & (sh.block - 1));
-      if (QALORA_CHECK(dbg, at, (long long)sh.num_blocks * sh.kv_heads * sh.block))
-        a.at.score_out[at] = (a.at.score_in != nullptr ? a.at.score_in[at] : 0.f) + (sum + other[token]);
-    }
+    if (half == 0) sums[128 + token] = sum + sums[token];
   } else if (warp == 8) {
     if (lane == 0) {
       constexpr uint32_t IDESC = kvp::idesc_f16(128, 128, false, false);
@@ -807,12 +817,20 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int token_tiles, in
     __syncwarp();
   }
   ptx::tc_fence_before();
-  __syncthreads();
+  if (C == 1) __syncthreads(); else cluster.sync();
+  if (threadIdx.x < 128 && rank == 0 && id >= 0) {
+    float sum = 0.f;
+    for (int r = 0; r < C; ++r) sum += cluster.map_shared_rank(sums, r)[128 + threadIdx.x];
+    const long long at = ((long long)id * sh.kv_heads + h) * sh.block + ((t0 + threadIdx.x) & (sh.block - 1));
+    if (QALORA_CHECK(dbg, at, (long long)sh.num_blocks * sh.kv_heads * sh.block))
+      a.at.score_out[at] = before + sum;
+  }
   if (threadIdx.x == 0 && *flag != 0) *a.status = 1;
   if (warp == 8) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem, 256);
   }
+  if (C > 1) cluster.sync();                                     // (a block's sums are read by its cluster until here)
 }
 
 template <int D>
@@ -845,9 +863,16 @@ int prompt(const PromptArgs& a, cudaStream_t st) {
     });
     if (ok != QALORA_OK) return ok;
     const int tiles = (a.kb.max_len + PT_TOK - 1) / PT_TOK;
-    if ((long long)tiles * sh.kv_heads > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
-    return kv_launch(kv_prompt_score_kernel<D>, dim3((unsigned)(tiles * sh.kv_heads), (unsigned)a.kb.batch), 320, (size_t)PsSmem<D>::TOTAL, st, a,
-                     tiles, debug_words());
+    const long long units = (long long)tiles * sh.kv_heads, row_tiles = (rows_max + PT_ROWS - 1) / PT_ROWS;
+    // Thread blocks per token tile, a cluster that shares its row tiles: while they all run at once, and each has two row
+    // tiles at least.  (Both kernels, one and up to eight blocks: 2500 tokens of a sequence of 6000, 8 heads on one of 128,
+    // 231 us and 144; a prompt of 1000 tokens, 16 heads on 2, 90 and 45; 700 tokens, 32 heads on 8, 50 and 39; 60 new
+    // ones of 3000, 8 heads on one of 64, 26.8 and 26.1.)
+    int C = 1;
+    while (C < PS_MAX_CLUSTER && units * a.kb.batch * C * 2 <= 2ll * device_sm_count() && row_tiles >= 4 * C) C *= 2;
+    if (units * C > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
+    return kv_launch_clusters(kv_prompt_score_kernel<D>, dim3((unsigned)(units * C), (unsigned)a.kb.batch), C, 320,
+                              (size_t)PsSmem<D>::TOTAL, st, a, debug_words());
   }
   return QALORA_OK;
 }

@@ -72,3 +72,17 @@ def test_few_rows_whole_or_in_even_shares(lens, new, heads, kv_heads, dim, block
     q = bf16(rng.standard_normal((sum(new), heads, dim)))
     out, lse, got, _ = attend(c, q, new, dim ** -0.5, scores)
     check(c, q, new, dim ** -0.5, out, lse, got, c.score)
+
+
+@pytest.mark.parametrize("lens,new,heads,kv_heads,dim,block", [
+    ([1500], [700], 8, 1, 64, 128), ([1300, 300, 9], [600, 20, 9], 8, 1, 128, 32), ([700], [700], 16, 2, 128, 64),
+    ([515, 0, 130], [515, 3, 130], 12, 3, 64, 16), ([2100], [260], 5, 1, 128, 16),
+])
+def test_gathered_weights_of_prompts_with_few_heads(lens, new, heads, kv_heads, dim, block):
+    """(clusters of 8, 4 and 2 thread blocks share the rows of a token tile, some of them without a row tile)"""
+    rng = np.random.default_rng(sum(lens) + heads)
+    c = Cache(rng, lens, heads, kv_heads, dim, block)
+    q = bf16(rng.standard_normal((sum(new), heads, dim)))
+    out, lse, got, _ = attend(c, q, new, dim ** -0.5, True)
+    check(c, q, new, dim ** -0.5, out, lse, got, c.score)
+    assert torch.equal(attend(c, q, new, dim ** -0.5, True)[2], got)
