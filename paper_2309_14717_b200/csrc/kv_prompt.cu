@@ -369,10 +369,20 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       ask_rest(step + 1);
       return true;
     };
-    ok = ask(0);
-    ask_rest(0);
+    if ((pair * 2 + i) * PT_ROWS + quarter * 32 < rows) {
+      ok = ask(0);
+      ask_rest(0);
 #pragma unroll 1
-    for (int step = 0; step < n_steps && ok; ++step) ok = work(step);
+      for (int step = 0; step < n_steps && ok; ++step) ok = work(step);
+    } else {
+      // none of the warp's rows is there: whatever its part of P holds reaches only its own rows of O, which nobody reads
+      // (four drafted tokens of 31 sequences of up to 23 159 tokens, 16 heads on 2 of 64, weights gathered: 324 us -> 300)
+#pragma unroll 1
+      for (int step = 0; step < n_steps && ok; ++step) {
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(s_full(i, step), (step >> 1) & 1, flag));
+        if (ok && lane == 0) ptx::mbar_arrive(p_full(i, step));
+      }
+    }
     if (some && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(o_done(i, n_steps - 1), ((n_steps - 1) >> 1) & 1, flag));
     ptx::tc_fence_after();
     const float m = w.m, l = w.l, ref = w.ref;
@@ -660,7 +670,8 @@ __device__ __forceinline__ float2 exp2_fma(float2 y) {
 // pieces of up to 700 tokens, 32 heads of 64, against up to 12345 cached ones 180 us with one block of four
 // accumulators, 138 with two blocks (the exponential unit busy for 71 % of the time), 128 with a quarter of the
 // exponentials on the FMA pipe (an eighth 133, three eighths 135, half 145).
-template <int D>
+// COLS: groups of 32 rows of a row tile that may be there (one where a sequence has 32 rows at most).
+template <int D, int COLS>
 __global__ void __launch_bounds__(320, 2)
 kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int* dbg) {
   using S = PsSmem<D>;
@@ -747,7 +758,7 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int* dbg) {
       const bool edge = __any_sync(0xffffffffu, skip > 0);
       float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < COLS; ++q) {
         float v[32];
         ptx::tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + 128 * half + 32 * q, reinterpret_cast<uint32_t*>(v));
         ptx::tmem_wait_ld();
@@ -859,7 +870,8 @@ int prompt(const PromptArgs& a, cudaStream_t st) {
   }
   if (a.at.score_out != nullptr && a.kb.max_len > 0) {
     ok = once_score.run([] {
-      return cudaFuncSetAttribute(kv_prompt_score_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PsSmem<D>::TOTAL);
+      const cudaError_t e = cudaFuncSetAttribute(kv_prompt_score_kernel<D, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, PsSmem<D>::TOTAL);
+      return e != cudaSuccess ? e : cudaFuncSetAttribute(kv_prompt_score_kernel<D, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, PsSmem<D>::TOTAL);
     });
     if (ok != QALORA_OK) return ok;
     const int tiles = (a.kb.max_len + PT_TOK - 1) / PT_TOK;
@@ -871,7 +883,9 @@ int prompt(const PromptArgs& a, cudaStream_t st) {
     int C = 1;
     while (C < PS_MAX_CLUSTER && units * a.kb.batch * C * 2 <= 2ll * device_sm_count() && row_tiles >= 4 * C) C *= 2;
     if (units * C > 0x7fffffffll) return QALORA_ERR_UNSUPPORTED_SHAPE;
-    return kv_launch_clusters(kv_prompt_score_kernel<D>, dim3((unsigned)(units * C), (unsigned)a.kb.batch), C, 320,
+    // (a few drafted tokens of a large group of heads: four of 31 sequences of up to 23 159 tokens, 16 heads on 2 of 64, both
+    // kernels 300 us with all four groups of rows, 284 with one)
+    return kv_launch_clusters(rows_max <= 32 ? kv_prompt_score_kernel<D, 1> : kv_prompt_score_kernel<D, 4>, dim3((unsigned)(units * C), (unsigned)a.kb.batch), C, 320,
                               (size_t)PsSmem<D>::TOTAL, st, a, debug_words());
   }
   return QALORA_OK;
