@@ -397,8 +397,11 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       if (QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) a.part_ml[at] = make_float2(m, l);
     }
     const float inv = partial ? ref : (l == 0.f ? 0.f : ref / l);
-    // through the warp's quarter of its tile of Q, which the products are done with, CHUNKS pieces of 16 bytes of a row at a
-    // time in an order that keeps both sides free of bank conflicts
+    // through a quarter of the tile of Q, CHUNKS pieces of 16 bytes of a row at a time in an order that keeps both sides
+    // free of bank conflicts.  With 128 channels that quarter holds rows of Q that other warps of the row tile fetched.
+    // o_done says that the products are done with them; where there is no product, in a part of the tokens that the row tile does
+    // not see, the four warps meet instead, so that nobody's rows are still on their way.
+    if (!some) { if (i == 0) ptx::named_barrier(1, 128); else ptx::named_barrier(2, 128); }
     constexpr int CHUNKS = D / 8;
     uint8_t* stage = smem + S::OFF_Q + i * S::TILE + quarter * (S::TILE / 4);
     auto place = [&](int of, int c) { return stage + of * (16 * CHUNKS) + ((c ^ (of & 7)) << 4); };
