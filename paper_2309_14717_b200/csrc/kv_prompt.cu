@@ -163,8 +163,11 @@ __device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[PT_H
 //   softmax threads   one per row: S from tensor memory, P back over its columns.
 // S of the next step is there while a step's softmax runs: a row tile's softmax never waits for its products.  (Steps of
 // 128 tokens, for whose S there is one place only, left softmax and products of a row tile to alternate: 189 us for a
-// 4096-token prompt of 32 heads of 128, against 185.)  P V of a step is issued before S of the next but one by the same
-// thread, so that S may overwrite P.
+// 4096-token prompt of 32 heads of 128, against 185.)  S of the next step but one
+// lies where P of a step was, so it waits for the arrival that tells that P V of the step is done: tcgen05 products of
+// one thread are ordered among themselves only where accumulator and shape are the same, and these two differ in
+// both.  (Relying on the order of issue: 179.2 us for that prompt against 179.9 with the wait; two pieces of up to 700 tokens,
+// 32 heads of 64, with the weights gathered 356.0 against 359.6.)
 // What bounds it: the softmax warps.  A step takes about 2200 cycles, of which the exponential unit is busy for 1024 (64 x 128
 // exponentials of either row tile at 16 a cycle), the tensor core for 1024 to 1280 (S with 64 columns reads Q again for
 // every half tile) and the four issue slots for about 1150; the two softmax warps of a scheduler run in step, so that the
@@ -491,6 +494,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
         const int it = step >> 1, st = it & 1;
         if ((step & 1) == 0 && !wait(k_full(st), (it >> 1) & 1)) return false;
         if (step < n_steps) {
+          if (step >= 2 && !wait(o_done(i, step), ((step >> 1) - 1) & 1)) return false;      // P V of the step two before
           ptx::tc_fence_after();
           const uint64_t k_desc = ptx::smem_desc(sbase + S::OFF_K + st * S::TILE, 16, 1024) + (uint64_t)((step & 1) * 512);
 #pragma unroll

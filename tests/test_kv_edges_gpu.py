@@ -52,3 +52,16 @@ def test_parts_of_a_prompt_that_a_row_tile_does_not_see(heads, kv_heads, dim, n)
         # (a row of NaN changes when the other rows of its warp move to a new maximum: their last bits, within the bounds)
         out[at], lse[at] = want[at], want_lse[at]
         check(c, q, [n], 0.1, out, lse)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,n,cached", [(2, 2, 128, 400, 3000), (4, 2, 64, 300, 4000)])
+def test_long_prompts_repeat_their_bits(heads, kv_heads, dim, n, cached):
+    """Many steps of scores that follow weights in the same place of tensor memory."""
+    rng = np.random.default_rng(cached)
+    c = Cache(rng, [cached + n, cached], heads, kv_heads, dim, 64)
+    q = bf16(rng.standard_normal((2 * n, heads, dim)))
+    want, want_lse, _, _ = attend(c, q, [n, n], 0.1)
+    check(c, q, [n, n], 0.1, want, want_lse)
+    for _ in range(10):
+        out, lse, _, _ = attend(c, q, [n, n], 0.1)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
