@@ -342,7 +342,9 @@ int qalora_forward_static(const qalora_desc* desc, int64_t m, const void* x, con
  *                                      to sequence b: its n newest tokens, at positions
  *                                      lens[b] - n ... lens[b] - 1
  * and by three HOST bounds: `m` rows in all (<= QALORA_MAX_ROWS), `max_new` rows of one
- * sequence, `max_len` tokens of one sequence.  A row whose position is negative (fewer tokens
+ * sequence, `max_len` tokens of one sequence.  Each may be larger than what a call has: rows
+ * from starts[batch] to m belong to nobody and stay as they are (bounds that are near what
+ * there is divide the work better).  A row whose position is negative (fewer tokens
  * than rows) is not there: it is not stored, it attends to nothing, its output is 0 and its
  * lse -infinity.  Entries that break a bound (a length above max_len or max_blocks *
  * block_tokens, starts that fall or leave 0 .. m, a block outside the pool) never cause an

@@ -606,7 +606,7 @@ int attend(const AttnArgs& a, cudaStream_t st) {
 
 struct AttnLayout {
   size_t status, plan, parts, lse2, logits, pr_ml, pr_o, pr_q, pr_rows, total;
-  int few;               // new rows per sequence up to which the kernels of this file take it
+  int few, many_lo;      // new rows per sequence up to which the kernels of this file take it, from which the prompt kernel does
   bool any_few, any_many;
   KvPromptScratch prompt;
 };
@@ -642,9 +642,12 @@ AttnLayout attention_layout(const KvShape& sh, int batch, int64_t m, int max_new
   const int most_few = kFewRows / sh.group;
   w.few = max_new < most_few ? max_new : most_few;
   w.any_many = max_new > w.few;
-  // (with every sequence at its bound but one, that one has m - (batch - 1) * max_new rows: when even
-  // those are many, no sequence has few)
-  w.any_few = w.few > 0 && m - (int64_t)(batch - 1) * max_new <= w.few;
+  // Which kernels run.  m bounds the rows, so nothing follows from it about a sequence's own; the rule only guesses.  If
+  // the rows were exactly m, a sequence with few of them would need the others to be near their bound: where even
+  // that leaves many, this looks like prompts alone, and the prompt kernel takes every sequence (many_lo), a short one
+  // in a tile of 128 rows.
+  w.any_few = w.few > 0 && (!w.any_many || m - (int64_t)(batch - 1) * max_new <= w.few);
+  w.many_lo = w.any_few ? w.few + 1 : 1;
   const int rows = 8 * column_tiles(sh, w.few);
   const size_t few_rows = w.any_few ? (size_t)batch * w.few * sh.heads : 0;
   w.status = take(256);
@@ -712,7 +715,7 @@ int launch_kv_attention(const KvShape& sh, const KvBatch& b, const KvAttention& 
   int r = L.any_few ? launch_few(sh, b, at, L, base, max_len, st) : QALORA_OK;
   if (r != QALORA_OK || !L.any_many) return r;
   KvBatch many = b;
-  many.n_lo = L.few + 1;
+  many.n_lo = L.many_lo;
   return launch_kv_prompt(sh, many, at, L.prompt, reinterpret_cast<float2*>(base + L.pr_ml), reinterpret_cast<float*>(base + L.pr_o),
                           reinterpret_cast<uint8_t*>(base + L.pr_q), reinterpret_cast<float*>(base + L.pr_rows),
                           reinterpret_cast<int*>(base + L.status), st);

@@ -4,7 +4,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_kv_cache_gpu import Cache, attend, bf16, check
+from paper_2309_14717_b200 import binding as Q
+from test_kv_cache_gpu import Cache, attend, bf16, check, dev, starts_of
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +66,91 @@ def test_long_prompts_repeat_their_bits(heads, kv_heads, dim, n, cached):
     for _ in range(10):
         out, lse, _, _ = attend(c, q, [n, n], 0.1)
         assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+# --------------------------------------------------------------------- m as a bound of the rows
+def attend_bounded(c, q, new, m, max_new, max_len, scale, scores, starts=None):
+    """As attend(), with `m` rows of q, out and lse of which the sequences have the first sum(new); the others hold NaN
+    queries and must stay as they are."""
+    used = sum(new)
+    rows = torch.full((m, c.d.heads, c.d.head_dim), NAN, dtype=torch.bfloat16, device="cuda")
+    rows[:used] = dev(q).bfloat16()
+    codes, scales, score = c.up()
+    out = torch.full((m, c.d.heads, c.d.head_dim), 9.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((m, c.d.heads), 9.0, device="cuda")
+    got = torch.full_like(score, -7.0) if scores else None
+    ws = Q.alloc_kv_workspace(c.d, len(new), m, max_new, max_len, scores)
+    ws.fill_(0xFF)
+    Q.qalora_kv_attention(c.d, max_new, max_len, dev(starts_of(new) if starts is None else starts), dev(c.lens), dev(c.table), rows, codes,
+                          scales, scale, out, lse, score if scores else None, got, ws)
+    torch.cuda.synchronize()
+    assert Q.workspace_status(ws) == 0
+    assert (out[used:] == 9).all() and (lse[used:] == 9).all()
+    return out[:used], lse[:used], got
+
+
+@pytest.mark.parametrize("scores", [False, True])
+@pytest.mark.parametrize("lens,new,heads,kv_heads,dim,m,max_new", [
+    ([70, 3, 200, 129] * 6, [1] * 24, 4, 4, 128, 32, 1), ([70, 3, 200, 129] * 6, [1] * 24, 4, 4, 128, 25, 1),       # a padded batch of tokens
+    ([90], [1], 8, 2, 64, 2, 1), ([90], [3], 8, 2, 64, 100, 100), ([90], [3], 8, 2, 128, 4, 4),                     # one sequence
+    ([50, 60, 70, 80], [1, 2, 3, 4], 4, 1, 128, 256, 64), ([50, 60, 70, 80], [1, 0, 3, 0], 4, 4, 64, 256, 64),      # far below the bounds
+    ([150, 90], [100, 5], 4, 4, 128, 200, 100), ([150, 90, 33], [5, 90, 1], 4, 2, 64, 300, 100),                    # prompts and tokens
+    ([40, 77, 9], [4, 4, 4], 2, 2, 128, 64, 4), ([40, 77, 9], [17, 2, 1], 2, 2, 128, 64, 17), ([0, 5], [2, 1], 2, 1, 64, 40, 20),
+])
+def test_rows_below_their_bounds(lens, new, heads, kv_heads, dim, m, max_new, scores):
+    rng = np.random.default_rng(m + max_new)
+    c = Cache(rng, lens, heads, kv_heads, dim, 32)
+    q = bf16(rng.standard_normal((sum(new), heads, dim)))
+    out, lse, got = attend_bounded(c, q, new, m, max_new, max(lens), 0.1, scores)
+    check(c, q, new, 0.1, out, lse, got, c.score)
+
+
+@pytest.mark.parametrize("scores", [False, True])
+def test_a_sequence_that_breaks_its_bounds_leaves_its_neighbours(scores):
+    """starts that fall make one sequence's rows unspecified; short and long neighbours are answered all the same."""
+    rng = np.random.default_rng(5)
+    heads, kv_heads, dim, new = 4, 2, 128, [3, 0, 40]
+    c = Cache(rng, [60, 50, 90], heads, kv_heads, dim, 32)
+    q = bf16(rng.standard_normal((sum(new), heads, dim)))
+    out, lse, got = attend_bounded(c, q, new, 43, 40, 90, 0.1, scores, np.array([0, 3, 3, 43], np.int32))
+    check(c, q, new, 0.1, out, lse, got, c.score)
+    c.lens = np.array([60, 50, 90, 70], np.int32)              # the third has rows 50 .. 3: none
+    c.table = np.concatenate([c.table, c.table[1:2]])
+    new = [3, 47, 0, 0]
+    q = bf16(rng.standard_normal((50, heads, dim)))
+    starts = np.array([0, 3, 50, 3, 3], np.int32)
+    out, lse, got = attend_bounded(c, q, new, 100, 60, 90, 0.1, scores, starts)
+    c.lens, c.table = c.lens[:2], c.table[:2]
+    check(c, q, new[:2], 0.1, out, lse, got, c.score)
+
+
+def test_captured_attention_replays_with_other_rows():
+    """One graph for any rows within its bounds: starts and lens change between replays."""
+    rng = np.random.default_rng(6)
+    heads, kv_heads, dim, m, max_new, max_len = 4, 2, 128, 96, 64, 300
+    c = Cache(rng, [300, 300, 300, 300], heads, kv_heads, dim, 32)
+    (codes, scales, score), table = c.up(), dev(c.table)
+    q = torch.zeros((m, heads, dim), dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.zeros((m, heads, dim), dtype=torch.bfloat16, device="cuda"), torch.zeros((m, heads), device="cuda")
+    starts, lens = torch.zeros(5, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    got = torch.zeros_like(score)
+    ws = Q.alloc_kv_workspace(c.d, 4, m, max_new, max_len, True)
+
+    def step():
+        Q.qalora_kv_attention(c.d, max_new, max_len, starts, lens, table, q, codes, scales, 0.1, out, lse, score, got, ws)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for new, length in ([[1, 1, 1, 1], [300, 20, 1, 77]], [[64, 1, 9, 0], [64, 300, 150, 3]], [[0, 0, 30, 2], [10, 0, 30, 5]], [[17, 16, 33, 8], [200] * 4]):
+        c.lens = np.array(length, np.int32)
+        rows = bf16(rng.standard_normal((sum(new), heads, dim)))
+        q.fill_(NAN), out.fill_(9), lse.fill_(9), got.fill_(-7)
+        q[:sum(new)] = dev(rows).bfloat16()
+        starts.copy_(dev(starts_of(new))), lens.copy_(dev(c.lens))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (out[sum(new):] == 9).all()
+        check(c, rows, new, 0.1, out[:sum(new)], lse[:sum(new)], got, c.score)

@@ -1,0 +1,20 @@
+"""Host-side rules of the key/value cache calls that need no GPU."""
+import pytest
+
+from paper_2309_14717_b200 import binding as Q
+from paper_2309_14717_b200 import build as _build
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    _build.build()
+
+
+@pytest.mark.parametrize("scores", [False, True])
+@pytest.mark.parametrize("batch,max_new,group", [(24, 1, 1), (24, 4, 4), (1, 16, 1), (3, 2, 8), (40, 1, 16)])
+def test_scratch_of_few_rows_does_not_vanish_when_m_is_a_bound(batch, max_new, group, scores):
+    """m bounds the rows: where no sequence has many, the kernel of few rows runs whatever m says."""
+    d = Q.kv_desc(32, 32 // group, 128, 64, 4096)
+    exact = Q.qalora_kv_attention_workspace_bytes(d, batch, batch * max_new, max_new, 2048, scores)
+    for m in (batch * max_new + 1, batch * max_new + max_new, 2 * batch * max_new + 16, 4096):
+        assert Q.qalora_kv_attention_workspace_bytes(d, batch, m, max_new, 2048, scores) >= exact
