@@ -399,7 +399,8 @@ int qalora_kv_read(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t
  *                  of softmax(S[i, :])_t
  * in the layout of `score`; score_in may be NULL (zeros) and may be score_out.  Sums and
  * softmax statistics are float32, products are exact (8-bit codes and bf16 in fp16 operands);
- * a row's weights are rounded to fp16, relative to its largest, before they meet the values.
+ * a row's weights times the value scales of their blocks are rounded to fp16, relative to the
+ * row's largest such product, before they meet the codes.
  * softmax_scale must be positive and finite.  No atomics: results are reproducible bit for bit
  * for given bounds and device.  `workspace`: qalora_kv_attention_workspace_bytes() bytes for
  * the same batch, m, max_new and max_len, content undefined; its first int32 becomes the

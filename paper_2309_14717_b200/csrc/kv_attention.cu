@@ -18,8 +18,9 @@ constexpr int JOIN_TOKENS = 512;                  // whose gathered weights a bl
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoMax = -1e30f;                  // running maximum of a row that has met no token
 constexpr float kGrow = 6.f;                      // a row is rescaled when its maximum has grown by 2^6 or more
-constexpr float kLift = 8.f;                      // weights are kept times 2^8: at most 2^14 in fp16, and 2^-22 of the largest
-                                                  // weight still is an ordinary fp16 number
+constexpr float kLift = 8.f;                      // weighted value scales are kept times 2^8: below 2^15 in fp16, and 2^-22 of the
+                                                  // largest still is an ordinary fp16 number
+constexpr float kNoScale = -1000.f;               // exponent of a value scale of 0
 
 struct AttnArgs {
   KvShape sh;
@@ -70,18 +71,40 @@ struct AtSmem {
   static constexpr int BLOCKS = NT == 1 ? 3 : 2;                // thread blocks per multiprocessor
   static constexpr int MERGE = AT_WARPS * ROWS * D * 4;
   static constexpr int OFF_MERGE = STAGES * 2 * TILE;
-  static constexpr int OFF_SCALES = OFF_MERGE + MERGE;                        // [STAGES][2][SUBS]
-  static constexpr int OFF_ML = OFF_SCALES + STAGES * 2 * SUBS * 4;           // [AT_WARPS][ROWS][2]
-  static constexpr int OFF_BARS = OFF_ML + AT_WARPS * ROWS * 2 * 4;
+  static constexpr int OFF_SCALES = OFF_MERGE + MERGE;                        // [STAGES][3][SUBS]
+  static constexpr int OFF_ML = OFF_SCALES + STAGES * 3 * SUBS * 4;           // [AT_WARPS][ROWS]
+  static constexpr int OFF_BARS = OFF_ML + AT_WARPS * ROWS * 16;
   static constexpr int OFF_FLAG = OFF_BARS + STAGES * 2 * 8;
   static constexpr int OFF_SEQS = OFF_FLAG + 16;                              // [batch] KvSeq, then the plan
   static int total(int batch) { return OFF_SEQS + batch * (int)sizeof(KvSeq) + (batch + 2) * 4 + 1024; }   // (the window starts on a 1 KiB boundary)
 };
 
 // Partial result `slot` = 2 * block + (0: the rows' units began in an earlier block, 1: they began here):
-// [ROWS] of {maximum, sum}, then [ROWS][D] sums of weighted values relative to that maximum.
+// [ROWS] of {maximum, sum, maximum of weighted value scales, -}, then [ROWS][D] sums of weighted values relative to the latter.
 template <int D, int ROWS>
-__host__ __device__ constexpr long long part_floats() { return (long long)ROWS * (D + 2); }
+__host__ __device__ constexpr long long part_floats() { return (long long)ROWS * (D + 4); }
+
+// A value scale as v.x * 2^v.y, v.x in 1 .. 2.
+__device__ __forceinline__ float2 split_scale(float s) {
+  const bool tiny = s < 0x1p-126f;
+  const uint32_t u = __float_as_uint(tiny ? s * 0x1p64f : s);
+  if (!(s > 0.f && s < INFINITY)) return make_float2(s, s == 0.f ? kNoScale : 0.f);
+  return make_float2(__uint_as_float((u & 0x007fffffu) | 0x3f800000u), (float)((int)(u >> 23) - (tiny ? 127 + 64 : 127)));
+}
+
+// x brought from weighted value scales relative to 2^top to values: times 2^(top - mx) / l, the power in two halves, since with
+// scales near either end of float32 it would leave the range of one.
+struct RowScale {
+  float by, again;
+  __device__ __forceinline__ RowScale(float top, float mx, float l) {
+    const float half = exp2f(0.5f * (top - kLift - mx));
+    by = l == 0.f ? 0.f : __fdiv_rn(half, l);
+    again = l == 0.f ? 0.f : half;
+  }
+  __device__ __forceinline__ float4 operator()(float4 x) const {
+    return make_float4(x.x * by * again, x.y * by * again, x.z * by * again, x.w * by * again);
+  }
+};
 
 // D: head width; NT: tiles of 8 rows (new tokens x heads of a group); SUB: 16-token steps per warp and unit.
 // Both products have the tokens or channels as the 16 rows of m16n8k16 and the few query rows as its 8 columns:
@@ -94,6 +117,12 @@ __host__ __device__ constexpr long long part_floats() { return (long long)ROWS *
 // Codes turn into fp16 exactly (1024 + 128 + c by byte permutation, minus 1152), the query is fp16 after a
 // power-of-two scaling per row (bf16 has fewer bits), so the scores are sums of exact products in float32.
 // Every warp keeps maximum, sum and output of its own tokens; the warps meet only at the end of a row tile.
+// Value scales go into the weights, as the channels' sums run over blocks of different scales, and the weights into fp16: a
+// scale is split into 2^e and a factor of 1 .. 2, and the weights of the values are relative to the row's largest score + e,
+// those of the softmax's sum to its largest score.  So both keep their bits wherever the scales lie in float32, for
+// a second exponential.  (Against weights relative to the score alone, times the scale relative to the largest one: 32
+// conversations of up to 4096 tokens 121.4 us and 122.0, two documents of up to 100 003 tokens with eight heads to a key
+// head and gathered weights 78.5 and 77.8, four new tokens of 16 of up to 4000, 32 heads on 8, 43.1 and 45.2.)
 template <int D, int NT, int SUB>
 __global__ void __launch_bounds__(AT_THREADS, AtSmem<D, NT, SUB>::BLOCKS)
 kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnArgs a, int* dbg) {
@@ -104,7 +133,7 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t sbase = ptx::smem_u32(smem);
   float* scale_ring = reinterpret_cast<float*>(smem + S::OFF_SCALES);
-  float* ml = reinterpret_cast<float*>(smem + S::OFF_ML);
+  float4* ml = reinterpret_cast<float4*>(smem + S::OFF_ML);
   float* merge = reinterpret_cast<float*>(smem + S::OFF_MERGE);
   volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_FLAG);
   KvSeq* seqs = reinterpret_cast<KvSeq*>(smem + S::OFF_SEQS);
@@ -195,7 +224,13 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           ptx::tma_load_2d(at, &map, 0, cur.k_row, full(st));
           ptx::tma_load_2d(at + S::TILE, &map, 0, cur.v_row, full(st));
         }
-        if (mine) { scale_ring[st * 2 * SUBS + sub] = cur.ks; scale_ring[st * 2 * SUBS + SUBS + sub] = cur.vs; }
+        if (mine) {
+          const float2 v = split_scale(cur.vs);
+          float* ring = scale_ring + st * 3 * SUBS + sub;
+          ring[0] = cur.ks;
+          ring[SUBS] = v.x;
+          ring[2 * SUBS] = v.y;
+        }
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive_expect_tx(full(st), (uint32_t)(boxes * 2 * box * D));
         __syncwarp();
@@ -208,7 +243,7 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     uint32_t qf[NT][KSTEPS][2];
     float q_scale[NT][2];                              // softmax_scale * log2(e) / (the row's power of two)
     int limit[NT][2];                                  // last token the row sees, -1: none
-    float mrow[NT][2], lrow[NT][2], o[NT][KSTEPS][4], ref = 0.f, inv_ref = 0.f;
+    float mrow[NT][2], vrow[NT][2], lrow[NT][2], o[NT][KSTEPS][4];       // running maxima of score and of score + e; sum; output
     float* logit_row[NT][2];
     UnitPlace p{};
     KvSeq s{};
@@ -219,7 +254,6 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         p = find_unit<TOK>(prefix, seqs, a.kb.batch, u);
         s = seqs[p.b];
         rows = s.n * sh.group;
-        ref = inv_ref = 0.f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           // this lane's part of row g8 of the tile, as the B operand
@@ -252,7 +286,7 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
             const int own = nt * 8 + q4 * 2 + c, io = own / sh.group;
             q_scale[nt][c] = __shfl_sync(0xffffffffu, back, (q4 * 2 + c) * 4);
             limit[nt][c] = own < rows ? s.first + io : -1;
-            mrow[nt][c] = kNoMax;
+            mrow[nt][c] = vrow[nt][c] = kNoMax;
             lrow[nt][c] = 0.f;
             logit_row[nt][c] = a.logits != nullptr && own < rows
                                    ? a.logits + ((long long)((a.batch0 + p.b) * a.kb.n_hi + io) * sh.heads + p.h * sh.group + own % sh.group) *
@@ -272,11 +306,13 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       const uint32_t k_base = sbase + st * 2 * S::TILE, v_base = k_base + S::TILE;
       const int sub0 = warp * SUB, t0 = p.tile * TOK + sub0 * 16;        // this warp's SUB * 16 tokens of the unit
       if (t0 < s.len && ok) {
-        float ks[SUB], vs[SUB], sc[SUB][NT][4];
+        float ks[SUB], vs[SUB], ve[SUB], sc[SUB][NT][4];
 #pragma unroll
         for (int g = 0; g < SUB; ++g) {                // (a group behind the sequence's end has scales of 0 and is masked)
-          ks[g] = scale_ring[st * 2 * SUBS + sub0 + g];
-          vs[g] = scale_ring[st * 2 * SUBS + SUBS + sub0 + g];
+          const float* ring = scale_ring + st * 3 * SUBS + sub0 + g;
+          ks[g] = ring[0];
+          vs[g] = ring[SUBS];
+          ve[g] = ring[2 * SUBS];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -302,9 +338,6 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         // scaled scores in powers of two, masked
         const bool edge = t0 + SUB * 16 - 1 > s.first || rows < ROWS;    // (the first row sees the least)
         bool grow = false;
-        float v_top = vs[0];
-#pragma unroll
-        for (int g = 1; g < SUB; ++g) v_top = fmaxf(v_top, vs[g]);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -320,29 +353,36 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
                 if (t > limit[nt][c]) x0 = -INFINITY;
                 if (t + 8 > limit[nt][c]) x1 = -INFINITY;
               }
-              grow |= fmaxf(x0, x1) > mrow[nt][c] + kGrow;
+              const float top = fmaxf(x0, x1);
+              grow |= top > mrow[nt][c] + kGrow || top + ve[g] > vrow[nt][c] + kGrow;
               if (logit_row[nt][c] != nullptr && QALORA_CHECK(dbg, t + 8, a.logit_stride)) {
                 logit_row[nt][c][t] = x0;
                 logit_row[nt][c][t + 8] = x1;
               }
             }
-        if (__any_sync(0xffffffffu, grow) || v_top > ref) {
-          // rare: bring the rows to their new maximum, and the outputs to the new largest value scale
-          const float ref_new = fmaxf(v_top, ref), ref_ratio = ref_new > 0.f ? ref / ref_new : 0.f;
+        if (__any_sync(0xffffffffu, grow)) {
+          // rare: bring the rows to their new maxima
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             float by[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              float mx = mrow[nt][c];
+              float mx = mrow[nt][c], vx = vrow[nt][c];
 #pragma unroll
-              for (int g = 0; g < SUB; ++g) mx = fmaxf(mx, fmaxf(sc[g][nt][c], sc[g][nt][2 + c]));
+              for (int g = 0; g < SUB; ++g) {
+                const float top = fmaxf(sc[g][nt][c], sc[g][nt][2 + c]);
+                mx = fmaxf(mx, top);
+                vx = fmaxf(vx, top + ve[g]);
+              }
 #pragma unroll
-              for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-              by[c] = exp2f(mrow[nt][c] - mx);
+              for (int w = 4; w < 32; w <<= 1) {
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+                vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, w));
+              }
+              lrow[nt][c] *= exp2f(mrow[nt][c] - mx);
+              by[c] = exp2f(vrow[nt][c] - vx);
               mrow[nt][c] = mx;
-              lrow[nt][c] *= by[c];
-              by[c] *= ref_ratio;
+              vrow[nt][c] = vx;
             }
 #pragma unroll
             for (int k = 0; k < KSTEPS; ++k) {
@@ -350,24 +390,21 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
               o[nt][k][2] *= by[0]; o[nt][k][3] *= by[1];
             }
           }
-          ref = ref_new;
-          inv_ref = ref > 0.f ? 1.f / ref : 0.f;
         }
         uint32_t pf[SUB][NT][2];                       // P^T as the B operand: tokens 0-7 and 8-15 of a group
 #pragma unroll
-        for (int g = 0; g < SUB; ++g) {
-          const float v_rel = vs[g] * inv_ref;
+        for (int g = 0; g < SUB; ++g)
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
+            const float* x = sc[g][nt];
+            lrow[nt][0] += kvp::exp2_fast(x[0] - mrow[nt][0]) + kvp::exp2_fast(x[2] - mrow[nt][0]);
+            lrow[nt][1] += kvp::exp2_fast(x[1] - mrow[nt][1]) + kvp::exp2_fast(x[3] - mrow[nt][1]);
             float e[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) e[c] = kvp::exp2_fast(sc[g][nt][c] - (mrow[nt][c & 1] - kLift));
-            lrow[nt][0] += e[0] + e[2];
-            lrow[nt][1] += e[1] + e[3];
-            pf[g][nt][0] = kvp::movmatrix(kvp::pack_half2(e[0] * v_rel, e[1] * v_rel));
-            pf[g][nt][1] = kvp::movmatrix(kvp::pack_half2(e[2] * v_rel, e[3] * v_rel));
+            for (int c = 0; c < 4; ++c) e[c] = kvp::exp2_fast(x[c] + (ve[g] + (kLift - vrow[nt][c & 1]))) * vs[g];
+            pf[g][nt][0] = kvp::movmatrix(kvp::pack_half2(e[0], e[1]));
+            pf[g][nt][1] = kvp::movmatrix(kvp::pack_half2(e[2], e[3]));
           }
-        }
 #pragma unroll
         for (int g = 0; g < SUB; ++g)
 #pragma unroll
@@ -401,39 +438,40 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
             const int r = nt * 8 + q4 * 2 + c;
-            if (g8 == 0) { ml[(warp * ROWS + r) * 2] = mrow[nt][c]; ml[(warp * ROWS + r) * 2 + 1] = l; }
+            if (g8 == 0) ml[warp * ROWS + r] = make_float4(mrow[nt][c], l, vrow[nt][c], 0.f);
             if (r < rows) {
 #pragma unroll
               for (int k = 0; k < KSTEPS; ++k)
-                *reinterpret_cast<float2*>(merge + (warp * ROWS + r) * D + k * 16 + g8 * 2) = make_float2(o[nt][k][c] * ref, o[nt][k][2 + c] * ref);
+                *reinterpret_cast<float2*>(merge + (warp * ROWS + r) * D + k * 16 + g8 * 2) = make_float2(o[nt][k][c], o[nt][k][2 + c]);
             }
           }
         ptx::named_barrier(1, AT_WARPS * 32);
         for (int i = tid; i < rows * (D / 4); i += AT_WARPS * 32) {
           const int r = i / (D / 4), d = (i % (D / 4)) * 4;
-          float mx = kNoMax, l = 0.f;
+          float mx = kNoMax, vx = kNoMax, l = 0.f;
 #pragma unroll
-          for (int w = 0; w < AT_WARPS; ++w) mx = fmaxf(mx, ml[(w * ROWS + r) * 2]);
+          for (int w = 0; w < AT_WARPS; ++w) { mx = fmaxf(mx, ml[w * ROWS + r].x); vx = fmaxf(vx, ml[w * ROWS + r].z); }
           float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
           for (int w = 0; w < AT_WARPS; ++w) {
-            const float by = exp2f(ml[(w * ROWS + r) * 2] - mx);
+            const float4 of = ml[w * ROWS + r];
+            const float by = exp2f(of.z - vx);
             const float4 y = *reinterpret_cast<const float4*>(merge + (w * ROWS + r) * D + d);
-            l = fmaf(by, ml[(w * ROWS + r) * 2 + 1], l);
+            l = fmaf(exp2f(of.x - mx), of.y, l);
             x.x = fmaf(by, y.x, x.x); x.y = fmaf(by, y.y, x.y); x.z = fmaf(by, y.z, x.z); x.w = fmaf(by, y.w, x.w);
           }
           if (whole) {
             const int i_new = r / sh.group, head = p.h * sh.group + r % sh.group;
             const long long at = (long long)(s.row0 + i_new) * sh.heads + head;
             if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) continue;
-            kvp::store_row4(a.at.out + at * D + d, x, l);
+            kvp::store_row4(a.at.out + at * D + d, RowScale(vx, mx, l)(x));
             if (d == 0) {
               const long long own = (long long)((a.batch0 + p.b) * a.kb.n_hi + i_new) * sh.heads + head;
-              kvp::store_lse(a.at.lse, at, a.lse2, own, mx, l, kLift);
+              kvp::store_lse(a.at.lse, at, a.lse2, own, mx, l, 0.f);
             }
           } else if (QALORA_CHECK(dbg, slot, 2 * a.units_grid)) {
-            *reinterpret_cast<float4*>(part + 2 * ROWS + r * D + d) = x;
-            if (d == 0) *reinterpret_cast<float2*>(part + 2 * r) = make_float2(mx, l);
+            *reinterpret_cast<float4*>(part + 4 * ROWS + r * D + d) = x;
+            if (d == 0) *reinterpret_cast<float4*>(part + 4 * r) = make_float4(mx, l, vx, 0.f);
           }
         }
         ptx::named_barrier(1, AT_WARPS * 32);
@@ -466,34 +504,36 @@ kv_join_kernel(const __grid_constant__ AttnArgs a, int row_blocks, int* dbg) {
   const uint32_t f = a.plan[b] + (uint32_t)h * tiles, c0 = f / per_block, c1 = (f + tiles - 1) / per_block;
   if (scores ? t0 >= s.len : c0 == c1) return;                  // (c0 == c1: one block had all of it)
   auto part_of = [&](uint32_t c) { return a.parts + (2ll * c + (f < c * per_block ? 0 : 1)) * part_floats<D, ROWS>(); };
-  // maximum and sum of row r over the parts, by one warp
-  auto stats = [&](int r, float& mx, float& l) {
-    mx = kNoMax;
+  // maxima and sum of row r over the parts, by one warp
+  auto stats = [&](int r, float& mx, float& l, float& vx) {
+    mx = vx = kNoMax;
     l = 0.f;
     for (uint32_t c = c0 + lane; c <= c1; c += 32) {
-      const float2 v = *reinterpret_cast<const float2*>(part_of(c) + 2 * r);
+      const float4 v = *reinterpret_cast<const float4*>(part_of(c) + 4 * r);
       const float top = fmaxf(mx, v.x);
       l = l * exp2f(mx - top) + v.y * exp2f(v.x - top);
       mx = top;
+      vx = fmaxf(vx, v.z);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       const float m2 = __shfl_xor_sync(0xffffffffu, mx, o), l2 = __shfl_xor_sync(0xffffffffu, l, o), top = fmaxf(mx, m2);
       l = l * exp2f(mx - top) + l2 * exp2f(m2 - top);
       mx = top;
+      vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, o));
     }
   };
   if (!scores) {
     constexpr int LANES = D / 4, SHARES = 128 / LANES;          // lanes of a row's output; shares of its parts
-    float mx, l;
-    stats(row, mx, l);
+    float mx, l, vx;
+    stats(row, mx, l, vx);
     const int who = tid / LANES, d = (tid % LANES) * 4;
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
     for (uint32_t c = c0 + who; c <= c1; c += SHARES) {
       const float* part = part_of(c);
-      const float by = exp2f(part[2 * row] - mx);
-      const float4 v = *reinterpret_cast<const float4*>(part + 2 * ROWS + row * D + d);
+      const float by = exp2f(part[4 * row + 2] - vx);
+      const float4 v = *reinterpret_cast<const float4*>(part + 4 * ROWS + row * D + d);
       y.x = fmaf(v.x, by, y.x); y.y = fmaf(v.y, by, y.y); y.z = fmaf(v.z, by, y.z); y.w = fmaf(v.w, by, y.w);
     }
     share[warp][lane] = y;
@@ -507,8 +547,8 @@ kv_join_kernel(const __grid_constant__ AttnArgs a, int row_blocks, int* dbg) {
     }
     const long long at = (long long)(s.row0 + row / sh.group) * sh.heads + h * sh.group + row % sh.group;
     if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) return;
-    kvp::store_row4(a.at.out + at * D + d, y, l);
-    if (d == 0) kvp::store_lse(a.at.lse, at, nullptr, 0, mx, l, kLift);
+    kvp::store_row4(a.at.out + at * D + d, RowScale(vx, mx, l)(y));
+    if (d == 0) kvp::store_lse(a.at.lse, at, nullptr, 0, mx, l, 0.f);
     return;
   }
   // Four tokens per thread; the scores of the first four rows are asked for before the rows' sums, whose parts take two
@@ -536,9 +576,9 @@ kv_join_kernel(const __grid_constant__ AttnArgs a, int row_blocks, int* dbg) {
   }
   if (c0 != c1) {
     for (int r = warp; r < rows; r += 4) {
-      float mx, l;
-      stats(r, mx, l);
-      if (lane == 0) row_lse[r] = l > 0.f ? mx - kLift + log2f(l) : INFINITY;
+      float mx, l, vx;
+      stats(r, mx, l, vx);
+      if (lane == 0) row_lse[r] = l > 0.f ? mx + log2f(l) : INFINITY;
     }
   } else if (tid < rows) {
     row_lse[tid] = a.lse2[(long long)((a.batch0 + b) * a.kb.n_hi + tid / sh.group) * sh.heads + h * sh.group + tid % sh.group];
@@ -652,7 +692,7 @@ AttnLayout attention_layout(const KvShape& sh, int batch, int64_t m, int max_new
   const size_t few_rows = w.any_few ? (size_t)batch * w.few * sh.heads : 0;
   w.status = take(256);
   w.plan = take((size_t)((batch < AT_MAX_BATCH ? batch : AT_MAX_BATCH) + 2) * 4);
-  w.parts = take(w.any_few ? (size_t)device_sm_count() * 3 * 2 * rows * (sh.dim + 2) * 4 : 0);   // (two for each of up to three blocks)
+  w.parts = take(w.any_few ? (size_t)device_sm_count() * 3 * 2 * rows * (sh.dim + 4) * 4 : 0);   // (two for each of up to three blocks)
   w.lse2 = take(with_score ? few_rows * 4 : 0);
   w.logits = take(with_score ? few_rows * round_up((size_t)max_len, 128) * 4 : 0);
   if (w.any_many) w.prompt = kv_prompt_scratch(sh, batch, m, max_len, with_score);

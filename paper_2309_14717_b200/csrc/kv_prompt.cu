@@ -631,7 +631,8 @@ kv_prompt_join_kernel(const __grid_constant__ PromptArgs a, int row_blocks, int*
     m = top;
   }
   const long long at = (long long)(s.row0 + r / sh.group) * sh.heads + h * sh.group + r % sh.group;
-  kvp::store_row4(a.at.out + at * D + d, x, l);
+  const float by = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
+  kvp::store_row4(a.at.out + at * D + d, make_float4(x.x * by, x.y * by, x.z * by, x.w * by));
   if (d == 0) {
     kvp::store_lse(a.at.lse, at, nullptr, 0, m, l, kLift);
     if (a.rows != nullptr) a.rows[(prow / PT_ROWS * 2 + 1) * PT_ROWS + prow % PT_ROWS] = l != 0.f ? kLift - m - log2f(l) : -INFINITY;

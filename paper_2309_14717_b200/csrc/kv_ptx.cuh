@@ -72,10 +72,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
-// out = x / l in bf16, zeros for a row that saw no token
-__device__ __forceinline__ void store_row4(__nv_bfloat16* out, float4 x, float l) {
-  const float by = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
-  const __nv_bfloat162 a = __floats2bfloat162_rn(x.x * by, x.y * by), b = __floats2bfloat162_rn(x.z * by, x.w * by);
+__device__ __forceinline__ void store_row4(__nv_bfloat16* out, float4 x) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(x.z, x.w);
   uint2 w;
   w.x = *reinterpret_cast<const uint32_t*>(&a);
   w.y = *reinterpret_cast<const uint32_t*>(&b);

@@ -154,3 +154,94 @@ def test_captured_attention_replays_with_other_rows():
         torch.cuda.synchronize()
         assert (out[sum(new):] == 9).all()
         check(c, rows, new, 0.1, out[:sum(new)], lse[:sum(new)], got, c.score)
+
+
+# ------------------------------------------------------------------ value scales anywhere in float32
+def check_values(c, q, new, scale, out, lse):
+    """Bounds that follow the values a row weights: 2^-8 |out| (bf16), 2^-10 + 2^-16 + 2 d of sum weight |value| (weights in fp16;
+    an exponent of up to 150 added to a score in float32; d as in test_kv_cache_gpu.py), 2^-26 of the largest weight * value scale for
+    each token (a weighted scale is at least 2^8 for the largest, and fp16 numbers are 2^-24 apart at the least; codes go to 127),
+    and 2^-133 (the least bf16 number)."""
+    T, group, row = c.codes.shape[3], c.d.heads // c.d.kv_heads, 0
+    o, l = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for b, n in enumerate(new):
+        for i in range(n):
+            t = np.arange(int(c.lens[b]) - n + i + 1)
+            blk = c.table[b][t // T]
+            for h in range(c.d.heads):
+                kv = h // group
+                key, val = (c.codes[blk, w, kv, t % T].astype(np.float64) * c.scales[blk, w, kv].astype(np.float64)[:, None] for w in (0, 1))
+                s = scale * (key @ q[row, h])
+                d = 2.0 ** -18 * (1 + scale * (np.abs(key) @ np.abs(q[row, h])).max())
+                w = np.exp(s - s.max())
+                total = w.sum()
+                w /= total
+                want, spread = w @ val, w @ np.abs(val)
+                tol = (2.0 ** -8 * np.abs(want) + (2.0 ** -10 + 2.0 ** -16 + 2 * d) * spread
+                       + len(t) * 2.0 ** -26 * (w * c.scales[blk, 1, kv]).max() + 2.0 ** -133)
+                assert np.isfinite(o[row, h]).all()
+                assert (np.abs(o[row, h] - want) <= tol).all(), (b, i, h, (np.abs(o[row, h] - want) / tol).max())
+                norm = s.max() + np.log(total)
+                assert abs(l[row, h] - norm) <= d + 2.0 ** -22 * abs(norm)
+            row += 1
+
+
+ROWS_OF = {"few": ([150, 40, 97], [1, 4, 3], 4, 2)}
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("form", ["few"])
+@pytest.mark.parametrize("values", ["subnormal", "subnormal and zero", "tiny, then ordinary", "ordinary, then tiny", "largest", "both ends", "zero"])
+def test_value_scales_at_the_ends_of_float32(values, form, dim):
+    lens, new, heads, kv_heads = ROWS_OF[form]
+    rng = np.random.default_rng(dim + len(values))
+    c = Cache(rng, lens, heads, kv_heads, dim, 16)
+    v = c.scales[:, 1]                                          # [blocks][kv_heads], by place in the sequence below
+    place = np.zeros(c.blocks, int)
+    for row in c.table:
+        place[row] = np.arange(len(row))
+    even = (place % 2 == 0)[:, None]
+    v[:] = {"subnormal": 1e-41 * v, "subnormal and zero": np.where(even, 3e-39 * v, 0), "tiny, then ordinary": np.where(place[:, None] < 2, 1e-40, v),
+            "ordinary, then tiny": np.where(place[:, None] < 2, v, 1e-37), "largest": 2.6e36 / v.max() * v,
+            "both ends": np.where(even, 2.6e36, 1e-44), "zero": 0 * v}[values].astype(np.float32)
+    q = bf16(rng.standard_normal((sum(new), heads, dim)))
+    out, lse, _, _ = attend(c, q, new, 0.05)
+    check_values(c, q, new, 0.05, out, lse)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("form", ["few"])
+@pytest.mark.parametrize("power", [-20, -25, -30, -38])
+def test_weight_on_values_far_below_the_largest(power, form, dim):
+    """Rows that attend sharply to blocks whose value scale is 2^power of the others': before, between and behind them."""
+    lens, new, heads, kv_heads = ROWS_OF[form]
+    rng = np.random.default_rng(dim - power)
+    c = Cache(rng, lens, heads, kv_heads, dim, 16)
+    for row in c.table:
+        c.scales[row[::2], 1] *= np.float32(2.0 ** power)
+        c.scales[row[1::2], 0] *= np.float32(0.01)              # their keys are short ...
+        c.codes[row[::2], 0, :, :, 0] = 100                     # ... and the others' agree with the queries
+    q = bf16(rng.standard_normal((sum(new), heads, dim)))
+    q[..., 0] = 64.0
+    out, lse, _, _ = attend(c, q, new, 1.0)
+    check_values(c, q, new, 1.0, out, lse)
+
+
+@pytest.mark.parametrize("n", [1, 3])
+def test_attention_over_what_append_stores_at_the_extremes(n):
+    """Zeros, subnormals and the largest numbers as values, stored by append and read by attention in one sequence."""
+    rng = np.random.default_rng(9)
+    heads, kv_heads, dim, length = 4, 2, 64, 90
+    c = Cache(rng, [length], heads, kv_heads, dim, 16)
+    codes, scales, score = c.up()
+    v = torch.randn((length, kv_heads, dim), generator=torch.Generator().manual_seed(3))
+    v[:16], v[16:32], v[32:48], v[48:64] = v[:16] * 1e-39, 0, v[32:48].sign() * 3.3e38, v[48:64] * 1e-36
+    k = torch.randn((length, kv_heads, dim), generator=torch.Generator().manual_seed(4))
+    Q.qalora_kv_append(c.d, length, dev(starts_of([length])), dev(c.lens), dev(c.table), k.bfloat16().cuda(), v.bfloat16().cuda(), codes, scales)
+    torch.cuda.synchronize()
+    c.codes, c.scales = codes.cpu().numpy(), scales.cpu().numpy()
+    for length in (10, 30, 45, 60, 90):
+        c.lens = np.array([length], np.int32)
+        q = bf16(rng.standard_normal((n, heads, dim)))
+        out, lse, _, _ = attend(c, q, [n], 0.125)
+        check_values(c, q, [n], 0.125, out, lse)
