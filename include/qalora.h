@@ -400,7 +400,9 @@ int qalora_kv_read(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t
  * in the layout of `score`; score_in may be NULL (zeros) and may be score_out.  Sums and
  * softmax statistics are float32, products are exact (8-bit codes and bf16 in fp16 operands);
  * a row's weights times the value scales of their blocks are rounded to fp16, relative to the
- * row's largest such product, before they meet the codes.
+ * row's largest such product, before they meet the codes; where a sequence has many new rows
+ * (more than 16 / (heads / kv_heads)), values of blocks whose scale is below 2^-80 of the
+ * largest value scale met so far count as zeros.
  * softmax_scale must be positive and finite.  No atomics: results are reproducible bit for bit
  * for given bounds and device.  `workspace`: qalora_kv_attention_workspace_bytes() bytes for
  * the same batch, m, max_new and max_len, content undefined; its first int32 becomes the

@@ -25,7 +25,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoMax = -1e30f;
 constexpr float kGrow = 6.f, kLift = 8.f;     // as in the few-row kernel: weights at most 2^14 in fp16
 constexpr float kTiny = 1e-37f;               // stands for a smaller factor of a score (|score| < 2^30): keeps 0 * -inf away
-constexpr float kLeastValueScale = 9.094947e-13f;   // 2^-40 of the largest one met so far: below it a block's values count as 0
+constexpr float kLeastExponent = -80.f, kLeastValueScale = 0x1p-80f;   // of the largest one met so far: below it a block's values count as 0
+constexpr float kMostSum = 64.f;              // a change of reference lets a row's sum grow to 2^64, and the weights after it by 2^80 each
 
 struct PromptArgs {
   KvShape sh;
@@ -101,20 +102,19 @@ __device__ __forceinline__ void convert_tile(const uint8_t* staged, uint8_t* til
 // A softmax thread's row.
 struct SoftmaxRow {
   float factor;            // softmax_scale * log2(e) / (the row's power of two)
-  float m, l;              // running maximum of score + log2 of the relative value scale, in powers of two; sum
+  float m, l;              // running maximum of score + log2 of the relative value scale, in powers of two; sum of 2^(score - m)
   float ref;               // value scale that the outputs are relative to
 };
 
-// A step's scores in a thread's registers: the columns (tokens) beyond `seen` masked, and whether the row's maximum has grown
-// by 2^kGrow or more (rare; and always on the first step).  c, off: the factor of a score and log2 of the value scale,
-// of 16 tokens each.  Returns the row's maximum, the running one included.
-__device__ __forceinline__ float softmax_top(const SoftmaxRow& w, float (&x)[PT_HALF], const float4 c, const float4 off, bool edge, int seen) {
+// A step's scores in a thread's registers: the columns (tokens) beyond `seen` masked.  c, off: the factor of a score and log2 of the value scale,
+// of 16 tokens each.  Returns the step's maximum.
+__device__ __forceinline__ float softmax_top(float (&x)[PT_HALF], const float4 c, const float4 off, bool edge, int seen) {
   if (edge) {
 #pragma unroll
     for (int t = 0; t < PT_HALF; ++t) if (t > seen) x[t] = -INFINITY;
   }
   const float cs[4] = {c.x, c.y, c.z, c.w}, os[4] = {off.x, off.y, off.z, off.w};
-  float top = w.m;
+  float top = -INFINITY;
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     const float* v = x + 16 * g;
@@ -342,10 +342,14 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       w.ref = refs.y;
       const int t0 = (2 * first + step) * PT_HALF;
       ptx::tmem_wait_ld();
-      const float top = softmax_top(w, x, c, off, t0 + PT_HALF - 1 > limit_lo, limit - t0);
-      if (__any_sync(0xffffffffu, top > w.m + kGrow) || ref_ratio != 1.f) {
-        // rare: the maximum and the outputs are brought up to date
-        const float by = exp2f(w.m - top), scale = by * ref_ratio;
+      const float most = softmax_top(x, c, off, t0 + PT_HALF - 1 > limit_lo, limit - t0);
+      if (__any_sync(0xffffffffu, most > w.m + kGrow) || ref_ratio != 1.f) {
+        // Rare: the maximum and the outputs are brought up to date.  With a larger reference the logarithms of all relative
+        // scales fall, and the maximum with them; else the weights of values like the earlier ones would sink into fp16's
+        // subnormals.  The sum, which no scale enters, grows in turn, so that the fall is limited.
+        float fall = 0.f;
+        if (ref_ratio != 1.f) fall = fmaxf(fmaxf(log2f(ref_ratio), kLeastExponent), fminf(log2f(w.l) - kMostSum, 0.f));
+        const float top = fmaxf(w.m + fall, most), by = exp2f(w.m - top), scale = by * ref_ratio;
         w.m = top;
         w.l *= by;
         if (step > 0) {
@@ -399,7 +403,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       const long long at = (long long)split * a.slots * sh.kv_heads * PT_ROWS + prow;
       if (QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) a.part_ml[at] = make_float2(m, l);
     }
-    const float inv = partial ? ref : (l == 0.f ? 0.f : ref / l);
+    const float by = l == 0.f ? 0.f : __fdiv_rn(1.f, l);         // (not ref / l: the reference may be the least number there is)
     // through a quarter of the tile of Q, CHUNKS pieces of 16 bytes of a row at a time in an order that keeps both sides
     // free of bank conflicts.  With 128 channels that quarter holds rows of Q that other warps of the row tile fetched.
     // o_done says that the products are done with them; where there is no product, in a part of the tokens that the row tile does
@@ -422,7 +426,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
         }
         float f[16];
 #pragma unroll
-        for (int t = 0; t < 16; ++t) f[t] = !some || !ok || l == 0.f ? 0.f : __uint_as_float(o[t]) * inv;
+        for (int t = 0; t < 16; ++t) f[t] = !some || !ok || l == 0.f ? 0.f : __uint_as_float(o[t]) * by * ref;
         if (partial) {
 #pragma unroll
           for (int t = 0; t < 4; ++t) *reinterpret_cast<float4*>(place(lane, (c >> 2) + t)) = make_float4(f[4 * t], f[4 * t + 1], f[4 * t + 2], f[4 * t + 3]);
@@ -569,8 +573,9 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
         float* rg = ring + (it % PT_RING) * PT_RING_FLOATS;
         if (lane < 8) {
           rg[lane] = ks;
-          rg[8 + lane] = log2f(least);
-          rg[16 + lane] = 1.f / least;
+          const float off = log2f(least);
+          rg[8 + lane] = off;
+          rg[16 + lane] = exp2f(-off);             // (of the rounded logarithm: its error leaves the softmax's sum alone)
           reinterpret_cast<int*>(rg)[32 + lane] = cur.id;
           reinterpret_cast<int*>(rg)[40 + lane] = v_id;
         }
@@ -624,15 +629,19 @@ kv_prompt_join_kernel(const __grid_constant__ PromptArgs a, int row_blocks, int*
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int p = 0; p < a.splits; ++p) {
     const float2 v = a.part_ml[p * plane + prow];
-    const float4 y = *reinterpret_cast<const float4*>(a.part_o + (p * plane + prow) * D + d);
-    const float top = fmaxf(m, v.x), b0 = exp2f(m - top), b1 = exp2f(v.x - top);
-    l = l * b0 + v.y * b1;
-    x.x = x.x * b0 + y.x * b1; x.y = x.y * b0 + y.y * b1; x.z = x.z * b0 + y.z * b1; x.w = x.w * b0 + y.w * b1;
+    const float top = fmaxf(m, v.x);
+    l = l * exp2f(m - top) + v.y * exp2f(v.x - top);
     m = top;
   }
-  const long long at = (long long)(s.row0 + r / sh.group) * sh.heads + h * sh.group + r % sh.group;
   const float by = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
-  kvp::store_row4(a.at.out + at * D + d, make_float4(x.x * by, x.y * by, x.z * by, x.w * by));
+  for (int p = 0; p < a.splits; ++p) {                            // (each part's output is its own weighted mean)
+    const float2 v = a.part_ml[p * plane + prow];
+    const float4 y = *reinterpret_cast<const float4*>(a.part_o + (p * plane + prow) * D + d);
+    const float share = v.y * exp2f(v.x - m) * by;
+    x.x = fmaf(y.x, share, x.x); x.y = fmaf(y.y, share, x.y); x.z = fmaf(y.z, share, x.z); x.w = fmaf(y.w, share, x.w);
+  }
+  const long long at = (long long)(s.row0 + r / sh.group) * sh.heads + h * sh.group + r % sh.group;
+  kvp::store_row4(a.at.out + at * D + d, x);
   if (d == 0) {
     kvp::store_lse(a.at.lse, at, nullptr, 0, m, l, kLift);
     if (a.rows != nullptr) a.rows[(prow / PT_ROWS * 2 + 1) * PT_ROWS + prow % PT_ROWS] = l != 0.f ? kLift - m - log2f(l) : -INFINITY;
