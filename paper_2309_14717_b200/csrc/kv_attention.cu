@@ -578,7 +578,7 @@ kv_join_kernel(const __grid_constant__ AttnArgs a, int row_blocks, int* dbg) {
     for (int r = warp; r < rows; r += 4) {
       float mx, l, vx;
       stats(r, mx, l, vx);
-      if (lane == 0) row_lse[r] = l > 0.f ? mx + log2f(l) : INFINITY;
+      if (lane == 0) row_lse[r] = l == 0.f ? INFINITY : mx + log2f(l);
     }
   } else if (tid < rows) {
     row_lse[tid] = a.lse2[(long long)((a.batch0 + b) * a.kb.n_hi + tid / sh.group) * sh.heads + h * sh.group + tid % sh.group];
@@ -587,6 +587,11 @@ kv_join_kernel(const __grid_constant__ AttnArgs a, int row_blocks, int* dbg) {
   if (id < 0) return;
   float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](const float4 v, float n) {
+    if (n != n) {                                               // a row of NaN spoils the tokens it sees (the others' scores are -infinity)
+      w.x += v.x == -INFINITY ? 0.f : n; w.y += v.y == -INFINITY ? 0.f : n;
+      w.z += v.z == -INFINITY ? 0.f : n; w.w += v.w == -INFINITY ? 0.f : n;
+      return;
+    }
     w.x += kvp::exp2_fast(v.x - n); w.y += kvp::exp2_fast(v.y - n);
     w.z += kvp::exp2_fast(v.z - n); w.w += kvp::exp2_fast(v.w - n);
   };

@@ -155,6 +155,14 @@ __device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[PT_H
   }
 }
 
+// What a row whose sum is NaN leaves for the gathered weights: a query of NaN, which spoils the weights of the tokens it sees, and
+// (in `rows`) minus infinity, as NaN there would reach the masked tokens too.
+template <int D>
+__device__ __forceinline__ void spoil_row(uint8_t* q_image, long long slot, int row) {
+  *reinterpret_cast<uint16_t*>(q_image + slot * PtSmem<D>::TILE + row * 128 + ((row & 7) << 4)) = 0x7fff;
+}
+__device__ __forceinline__ float minus_log2_sum(float m, float l) { return l > 0.f ? kLift - m - log2f(l) : -INFINITY; }
+
 // Two tiles of 128 rows of one kv head against a range of its sequence's tokens, in tiles of 128 and steps of 64:
 //   look-up warp      blocks and scales of a tile, bulk copies of its codes;
 //   conversion warps  codes of a tile -> fp16 keys (K-major) and values (MN-major) in shared memory;
@@ -397,7 +405,8 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
     const long long prow = slot * PT_ROWS + row;
     if (a.rows != nullptr && tile_there && split == 0 && QALORA_CHECK(dbg, slot, a.slots * sh.kv_heads)) {
       a.rows[slot * 2 * PT_ROWS + row] = fmaxf(factor, kTiny);
-      a.rows[slot * 2 * PT_ROWS + PT_ROWS + row] = !partial && there && l != 0.f ? kLift - m - log2f(l) : -INFINITY;
+      a.rows[slot * 2 * PT_ROWS + PT_ROWS + row] = !partial && there ? minus_log2_sum(m, l) : -INFINITY;
+      if (!partial && there && l != l) spoil_row<D>(a.q_image, slot, row);
     }
     if (partial && tile_there) {
       const long long at = (long long)split * a.slots * sh.kv_heads * PT_ROWS + prow;
@@ -644,7 +653,10 @@ kv_prompt_join_kernel(const __grid_constant__ PromptArgs a, int row_blocks, int*
   kvp::store_row4(a.at.out + at * D + d, x);
   if (d == 0) {
     kvp::store_lse(a.at.lse, at, nullptr, 0, m, l, kLift);
-    if (a.rows != nullptr) a.rows[(prow / PT_ROWS * 2 + 1) * PT_ROWS + prow % PT_ROWS] = l != 0.f ? kLift - m - log2f(l) : -INFINITY;
+    if (a.rows != nullptr) {
+      a.rows[(prow / PT_ROWS * 2 + 1) * PT_ROWS + prow % PT_ROWS] = minus_log2_sum(m, l);
+      if (l != l) spoil_row<D>(a.q_image, prow / PT_ROWS, (int)(prow % PT_ROWS));
+    }
   }
 }
 
@@ -662,10 +674,11 @@ struct PsSmem {
 };
 
 // 2^y of two values on the FMA pipe: y = n + r with |r| <= 1/2 by adding 1.5 * 2^23, 2^r by its minimax polynomial
-// of degree 4 (relative error 2.7e-6, 2^-18.5), n added to the exponent.  y <= 126; below -125 the result is 2^-125.
+// of degree 4 (relative error 2.7e-6, 2^-18.5), times 2^n.  y <= 126; a y of -126.5 or less gives 0 (its 2^n has no bits
+// left), NaN gives NaN.
 __device__ __forceinline__ float2 exp2_fma(float2 y) {
-  y.x = fmaxf(y.x, -125.f);
-  y.y = fmaxf(y.y, -125.f);
+  y.x = kvp::max_nan(y.x, -127.f);
+  y.y = kvp::max_nan(y.y, -127.f);
   const float2 n = ptx::fadd2(y, make_float2(12582912.f, 12582912.f));
   const float2 r = ptx::ffma2(ptx::fadd2(n, make_float2(-12582912.f, -12582912.f)), make_float2(-1.f, -1.f), y);
   float2 p = make_float2(0.0095701022f, 0.0095701022f);
@@ -673,9 +686,8 @@ __device__ __forceinline__ float2 exp2_fma(float2 y) {
   p = ptx::ffma2(p, r, make_float2(0.24024744f, 0.24024744f));
   p = ptx::ffma2(p, r, make_float2(0.69312179f, 0.69312179f));
   p = ptx::ffma2(p, r, make_float2(0.99999928f, 0.99999928f));
-  p.x = __uint_as_float(__float_as_uint(p.x) + (__float_as_uint(n.x) << 23));
-  p.y = __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(n.y) << 23));
-  return p;
+  return ptx::fmul2(p, make_float2(__uint_as_float((__float_as_uint(n.x) << 23) + 0x3f800000u),
+                                   __uint_as_float((__float_as_uint(n.y) << 23) + 0x3f800000u)));
 }
 
 // The weights that 128 tokens of one kv head gather: S^T = K Q^T with the tokens as the rows of the product, so

@@ -66,6 +66,12 @@ __device__ __forceinline__ float exp2_fast(float x) {           // relative erro
   return y;
 }
 
+__device__ __forceinline__ float max_nan(float a, float b) {    // NaN where one of them is
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import kv_oracle as K
 from paper_2309_14717_b200 import binding as Q
 from test_kv_cache_gpu import Cache, attend, bf16, check, dev, starts_of
 
@@ -255,3 +256,49 @@ def test_attention_over_what_append_stores_at_the_extremes(n):
         q = bf16(rng.standard_normal((n, heads, dim)))
         out, lse, _, _ = attend(c, q, [n], 0.125)
         check_values(c, q, [n], 0.125, out, lse)
+
+
+# ------------------------------------------------------------------------ NaN, and weights of zero
+@pytest.mark.parametrize("lens,new,heads,kv_heads,dim,bad", [
+    ([200], [200], 4, 2, 128, range(0, 200, 29)), ([200], [200], 4, 2, 128, [7]), ([200], [200], 2, 2, 64, [6]), ([200], [200], 2, 2, 64, [5]),
+    ([500, 300], [90, 120], 2, 1, 128, [13, 150]), ([90], [20], 4, 1, 64, [3]),                                     # tiles of rows
+    ([1100], [100], 2, 2, 128, [31, 70]),                                                                            # cut into parts
+    ([200, 64, 30], [3, 2, 4], 4, 2, 128, [1, 3, 7]), ([900], [8], 2, 2, 64, [4]), ([40] * 3, [5] * 3, 3, 3, 128, [0, 9, 14]),   # few rows
+])
+def test_a_query_of_nan_spoils_the_weights_of_what_it_sees(lens, new, heads, kv_heads, dim, bad):
+    rng = np.random.default_rng(sum(lens) + dim)
+    c = Cache(rng, lens, heads, kv_heads, dim, 32)
+    q = bf16(rng.standard_normal((sum(new), heads, dim)))
+    for i in bad:
+        q[i, i % heads, i % dim] = NAN
+    with np.errstate(invalid="ignore"):
+        r = K.attention(c.codes, c.scales, starts_of(new), c.lens, c.table, q, 0.1, c.score, True)
+    assert np.isnan(r["score"]).any() and np.isfinite(r["score"]).any()
+    out, lse, got, _ = attend(c, q, new, 0.1, True)
+    got, mine = got.double().cpu().numpy(), np.zeros(c.score.shape, bool)
+    for b, n in enumerate(c.lens):
+        t = np.arange(int(n))
+        mine[c.table[b][t // 32], :, t % 32] = True
+    assert (np.isnan(got) == (np.isnan(r["score"]) & mine)).all()
+    fine = mine & ~np.isnan(got)
+    d = 2.0 ** -18 * (1 + np.nanmax(r["reach"]))
+    assert (np.abs(got - r["score"])[fine] <= (d * (r["score"] - c.score) + 2.0 ** -22 * r["score"] + 1e-30)[fine]).all()
+    assert (np.isnan(lse.cpu().numpy()) == np.isnan(r["lse"])).all()
+    assert (np.isnan(out.float().cpu().numpy()) == np.isnan(r["out"])).all()
+
+
+@pytest.mark.parametrize("lens,new,dim", [([260], [260], 128), ([500], [70], 64), ([1100], [40], 128), ([300, 90], [4, 9], 64)])
+def test_tokens_without_weight_gather_nothing(lens, new, dim):
+    """Sharp scores: a token whose weights are all below 2^-150 keeps its score, and with none before it has exactly 0."""
+    rng = np.random.default_rng(dim)
+    c = Cache(rng, lens, 2, 2, dim, 16)
+    for row in c.table:
+        c.codes[row[::3], 0, :, :, 0] = -127
+    q = bf16(rng.standard_normal((sum(new), 2, dim)))
+    q[..., 0] = 400.0
+    r = K.attention(c.codes, c.scales, starts_of(new), c.lens, c.table, q, 1.0, None, True)
+    none = (r["score"] > 0) & (r["score"] < 2.0 ** -150)
+    assert none.sum() > 50
+    for score_in in (False, True):
+        _, _, got, before = attend(c, q, new, 1.0, True, score_in=score_in)
+        assert torch.equal(got[dev(none)], before[dev(none)] if score_in else torch.zeros_like(got[dev(none)]))
