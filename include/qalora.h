@@ -398,7 +398,8 @@ int qalora_kv_read(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t
  *   score_out[t] = score_in[t] + sum over the sequence's new rows i and the heads of the group
  *                  of softmax(S[i, :])_t
  * in the layout of `score`; score_in may be NULL (zeros) and may be score_out.  Sums and
- * softmax statistics are float32, products are exact (8-bit codes and bf16 in fp16 operands);
+ * softmax statistics are float32, exponentials have a relative error of 2^-22, products are
+ * exact (8-bit codes and bf16 in fp16 operands);
  * a row's weights times the value scales of their blocks are rounded to fp16, relative to the
  * row's largest such product, before they meet the codes; where a sequence has many new rows
  * (more than 16 / (heads / kv_heads)), values of blocks whose scale is below 2^-80 of the

@@ -674,18 +674,20 @@ struct PsSmem {
 };
 
 // 2^y of two values on the FMA pipe: y = n + r with |r| <= 1/2 by adding 1.5 * 2^23, 2^r by its minimax polynomial
-// of degree 4 (relative error 2.7e-6, 2^-18.5), times 2^n.  y <= 126; a y of -126.5 or less gives 0 (its 2^n has no bits
+// of degree 5 (Remez exchange on the relative error: 7.5e-8, 2.2e-7 = 2^-22.1 with the roundings of its evaluation, as the
+// exponential unit's), times 2^n.  y <= 126; a y of -126.5 or less gives 0 (its 2^n has no bits
 // left), NaN gives NaN.
 __device__ __forceinline__ float2 exp2_fma(float2 y) {
   y.x = kvp::max_nan(y.x, -127.f);
   y.y = kvp::max_nan(y.y, -127.f);
   const float2 n = ptx::fadd2(y, make_float2(12582912.f, 12582912.f));
   const float2 r = ptx::ffma2(ptx::fadd2(n, make_float2(-12582912.f, -12582912.f)), make_float2(-1.f, -1.f), y);
-  float2 p = make_float2(0.0095701022f, 0.0095701022f);
-  p = ptx::ffma2(p, r, make_float2(0.055917859f, 0.055917859f));
-  p = ptx::ffma2(p, r, make_float2(0.24024744f, 0.24024744f));
-  p = ptx::ffma2(p, r, make_float2(0.69312179f, 0.69312179f));
-  p = ptx::ffma2(p, r, make_float2(0.99999928f, 0.99999928f));
+  float2 p = make_float2(0.00132764725f, 0.00132764725f);
+  p = ptx::ffma2(p, r, make_float2(0.00967554096f, 0.00967554096f));
+  p = ptx::ffma2(p, r, make_float2(0.0555071309f, 0.0555071309f));
+  p = ptx::ffma2(p, r, make_float2(0.240221202f, 0.240221202f));
+  p = ptx::ffma2(p, r, make_float2(0.693146944f, 0.693146944f));
+  p = ptx::ffma2(p, r, make_float2(1.00000012f, 1.00000012f));
   return ptx::fmul2(p, make_float2(__uint_as_float((__float_as_uint(n.x) << 23) + 0x3f800000u),
                                    __uint_as_float((__float_as_uint(n.y) << 23) + 0x3f800000u)));
 }

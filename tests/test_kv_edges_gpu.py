@@ -302,3 +302,28 @@ def test_tokens_without_weight_gather_nothing(lens, new, dim):
     for score_in in (False, True):
         _, _, got, before = attend(c, q, new, 1.0, True, score_in=score_in)
         assert torch.equal(got[dev(none)], before[dev(none)] if score_in else torch.zeros_like(got[dev(none)]))
+
+
+@pytest.mark.parametrize("places", [(6, 7), (0, 1, 2, 3, 4, 5)])
+def test_exponentials_of_gathered_weights(places):
+    """Rows at `places` of eight weight the tokens mildly, the others only token 0: a token gathers the exponentials of the former,
+    which with many rows are polynomials on the FMA pipe for places 6 and 7 and the exponential unit's for the others.  How the
+    weights of the tokens relate to each other knows nothing of the rows' sums.  Its bound, twice (a token and the mean):
+    ln 2 * (4 * 2^-24 for a score within +-1 after four roundings + 2^-21 for score minus logarithm, within 8 .. 16) + 2^-22
+    (either exponential) + 2^-24 for each row that is added."""
+    dim, n, cached = 64, 24, 256
+    c = Cache(np.random.default_rng(1), [n + cached], 1, 1, dim, 16)
+    c.codes[:, 0] = 0
+    rng = np.random.default_rng(2)
+    for t in range(n + cached):
+        c.codes[c.table[0, t // 16], 0, 0, t % 16, 0] = rng.integers(-127, 128)
+    c.codes[c.table[0, 0], 0, 0, 0, 1] = 127
+    c.scales[:, 0] = np.float32(1 / 127)
+    mild = [i for i in range(n) if i % 8 in places]
+    q = np.zeros((n, 1, dim))
+    q[:, 0, 1], q[mild, 0, 1], q[mild, 0, 0] = 200.0, 0.0, 0.6875
+    r = K.attention(c.codes, c.scales, starts_of([n]), c.lens, c.table, q, 1.0, None, True)
+    _, _, got, _ = attend(c, q, [n], 1.0, True, score_in=False)
+    t = np.arange(1, cached)
+    ratio = got.double().cpu().numpy()[c.table[0][t // 16], 0, t % 16] / r["score"][c.table[0][t // 16], 0, t % 16]
+    assert np.abs(ratio / ratio.mean() - 1).max() <= 2 * (np.log(2) * (2.0 ** -22 + 2.0 ** -21) + 2.0 ** -22 + len(mild) * 2.0 ** -24)
