@@ -16,7 +16,7 @@ constexpr int AT_THREADS = (AT_WARPS + 1) * 32;
 constexpr int AT_MAX_BATCH = 512;                 // sequences of one launch (their rows, lengths and units lie in shared memory)
 constexpr int JOIN_TOKENS = 512;                  // whose gathered weights a block of the second kernel adds up
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNoMax = -1e30f;                  // running maximum of a row that has met no token
+constexpr float kNoMax = -3.40282347e38f;         // running maximum of a row that has met no token
 constexpr float kGrow = 6.f;                      // a row is rescaled when its maximum has grown by 2^6 or more
 constexpr float kLift = 8.f;                      // weighted value scales are kept times 2^8: below 2^15 in fp16, and 2^-22 of the
                                                   // largest still is an ordinary fp16 number
@@ -80,7 +80,7 @@ struct AtSmem {
 };
 
 // Partial result `slot` = 2 * block + (0: the rows' units began in an earlier block, 1: they began here):
-// [ROWS] of {maximum, sum, maximum of weighted value scales, -}, then [ROWS][D] sums of weighted values relative to the latter.
+// [ROWS] of {maximum, sum, maximum of weighted value scales relative to it, -}, then [ROWS][D] sums of weighted values relative to the latter.
 template <int D, int ROWS>
 __host__ __device__ constexpr long long part_floats() { return (long long)ROWS * (D + 4); }
 
@@ -92,12 +92,12 @@ __device__ __forceinline__ float2 split_scale(float s) {
   return make_float2(__uint_as_float((u & 0x007fffffu) | 0x3f800000u), (float)((int)(u >> 23) - (tiny ? 127 + 64 : 127)));
 }
 
-// x brought from weighted value scales relative to 2^top to values: times 2^(top - mx) / l, the power in two halves, since with
-// scales near either end of float32 it would leave the range of one.
+// x brought from weighted value scales relative to 2^v to values: times 2^v / l, the power in two halves, since with scales
+// near either end of float32 it would leave the range of one.
 struct RowScale {
   float by, again;
-  __device__ __forceinline__ RowScale(float top, float mx, float l) {
-    const float half = exp2f(0.5f * (top - kLift - mx));
+  __device__ __forceinline__ RowScale(float v, float l) {
+    const float half = exp2f(0.5f * (v - kLift));
     by = l == 0.f ? 0.f : __fdiv_rn(half, l);
     again = l == 0.f ? 0.f : half;
   }
@@ -118,8 +118,9 @@ struct RowScale {
 // power-of-two scaling per row (bf16 has fewer bits), so the scores are sums of exact products in float32.
 // Every warp keeps maximum, sum and output of its own tokens; the warps meet only at the end of a row tile.
 // Value scales go into the weights, as the channels' sums run over blocks of different scales, and the weights into fp16: a
-// scale is split into 2^e and a factor of 1 .. 2, and the weights of the values are relative to the row's largest score + e,
-// those of the softmax's sum to its largest score.  So both keep their bits wherever the scales lie in float32, for
+// scale is split into 2^e and a factor of 1 .. 2, and the weights of the values are relative to the row's largest score + e
+// (held as a difference from the largest score, which would swallow e where scores are large), those of the softmax's sum
+// to its largest score.  So both keep their bits wherever the scales lie in float32, for
 // a second exponential.  (Against weights relative to the score alone, times the scale relative to the largest one: 32
 // conversations of up to 4096 tokens 121.4 us and 122.0, two documents of up to 100 003 tokens with eight heads to a key
 // head and gathered weights 78.5 and 77.8, four new tokens of 16 of up to 4000, 32 heads on 8, 43.1 and 45.2.)
@@ -243,7 +244,7 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     uint32_t qf[NT][KSTEPS][2];
     float q_scale[NT][2];                              // softmax_scale * log2(e) / (the row's power of two)
     int limit[NT][2];                                  // last token the row sees, -1: none
-    float mrow[NT][2], vrow[NT][2], lrow[NT][2], o[NT][KSTEPS][4];       // running maxima of score and of score + e; sum; output
+    float mrow[NT][2], vrow[NT][2], lrow[NT][2], o[NT][KSTEPS][4];       // running maxima of score, and of score - that one + e; sum; output
     float* logit_row[NT][2];
     UnitPlace p{};
     KvSeq s{};
@@ -353,8 +354,8 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
                 if (t > limit[nt][c]) x0 = -INFINITY;
                 if (t + 8 > limit[nt][c]) x1 = -INFINITY;
               }
-              const float top = fmaxf(x0, x1);
-              grow |= top > mrow[nt][c] + kGrow || top + ve[g] > vrow[nt][c] + kGrow;
+              const float over = fmaxf(x0, x1) - mrow[nt][c];
+              grow |= over > kGrow || over + ve[g] > vrow[nt][c] + kGrow;
               if (logit_row[nt][c] != nullptr && QALORA_CHECK(dbg, t + 8, a.logit_stride)) {
                 logit_row[nt][c][t] = x0;
                 logit_row[nt][c][t + 8] = x1;
@@ -367,20 +368,19 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
             float by[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              float mx = mrow[nt][c], vx = vrow[nt][c];
+              float mx = mrow[nt][c];
 #pragma unroll
-              for (int g = 0; g < SUB; ++g) {
-                const float top = fmaxf(sc[g][nt][c], sc[g][nt][2 + c]);
-                mx = fmaxf(mx, top);
-                vx = fmaxf(vx, top + ve[g]);
-              }
+              for (int g = 0; g < SUB; ++g) mx = fmaxf(mx, fmaxf(sc[g][nt][c], sc[g][nt][2 + c]));
 #pragma unroll
-              for (int w = 4; w < 32; w <<= 1) {
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-                vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, w));
-              }
+              for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+              const float before = vrow[nt][c] + (mrow[nt][c] - mx);        // in terms of the new maximum
+              float vx = before;
+#pragma unroll
+              for (int g = 0; g < SUB; ++g) vx = fmaxf(vx, fmaxf(sc[g][nt][c], sc[g][nt][2 + c]) - mx + ve[g]);
+#pragma unroll
+              for (int w = 4; w < 32; w <<= 1) vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, w));
               lrow[nt][c] *= exp2f(mrow[nt][c] - mx);
-              by[c] = exp2f(vrow[nt][c] - vx);
+              by[c] = exp2f(before - vx);
               mrow[nt][c] = mx;
               vrow[nt][c] = vx;
             }
@@ -396,10 +396,11 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         for (int g = 0; g < SUB; ++g)
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            const float* x = sc[g][nt];
-            lrow[nt][0] += kvp::exp2_fast(x[0] - mrow[nt][0]) + kvp::exp2_fast(x[2] - mrow[nt][0]);
-            lrow[nt][1] += kvp::exp2_fast(x[1] - mrow[nt][1]) + kvp::exp2_fast(x[3] - mrow[nt][1]);
-            float e[4];
+            float x[4], e[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] = sc[g][nt][c] - mrow[nt][c & 1];
+            lrow[nt][0] += kvp::exp2_fast(x[0]) + kvp::exp2_fast(x[2]);
+            lrow[nt][1] += kvp::exp2_fast(x[1]) + kvp::exp2_fast(x[3]);
 #pragma unroll
             for (int c = 0; c < 4; ++c) e[c] = kvp::exp2_fast(x[c] + (ve[g] + (kLift - vrow[nt][c & 1]))) * vs[g];
             pf[g][nt][0] = kvp::movmatrix(kvp::pack_half2(e[0], e[1]));
@@ -450,12 +451,14 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           const int r = i / (D / 4), d = (i % (D / 4)) * 4;
           float mx = kNoMax, vx = kNoMax, l = 0.f;
 #pragma unroll
-          for (int w = 0; w < AT_WARPS; ++w) { mx = fmaxf(mx, ml[w * ROWS + r].x); vx = fmaxf(vx, ml[w * ROWS + r].z); }
+          for (int w = 0; w < AT_WARPS; ++w) mx = fmaxf(mx, ml[w * ROWS + r].x);
+#pragma unroll
+          for (int w = 0; w < AT_WARPS; ++w) vx = fmaxf(vx, ml[w * ROWS + r].z + (ml[w * ROWS + r].x - mx));
           float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
           for (int w = 0; w < AT_WARPS; ++w) {
             const float4 of = ml[w * ROWS + r];
-            const float by = exp2f(of.z - vx);
+            const float by = exp2f(of.z + (of.x - mx) - vx);
             const float4 y = *reinterpret_cast<const float4*>(merge + (w * ROWS + r) * D + d);
             l = fmaf(exp2f(of.x - mx), of.y, l);
             x.x = fmaf(by, y.x, x.x); x.y = fmaf(by, y.y, x.y); x.z = fmaf(by, y.z, x.z); x.w = fmaf(by, y.w, x.w);
@@ -464,7 +467,7 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
             const int i_new = r / sh.group, head = p.h * sh.group + r % sh.group;
             const long long at = (long long)(s.row0 + i_new) * sh.heads + head;
             if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) continue;
-            kvp::store_row4(a.at.out + at * D + d, RowScale(vx, mx, l)(x));
+            kvp::store_row4(a.at.out + at * D + d, RowScale(vx, l)(x));
             if (d == 0) {
               const long long own = (long long)((a.batch0 + p.b) * a.kb.n_hi + i_new) * sh.heads + head;
               kvp::store_lse(a.at.lse, at, a.lse2, own, mx, l, 0.f);
@@ -512,15 +515,15 @@ kv_join_kernel(const __grid_constant__ AttnArgs a, int row_blocks, int* dbg) {
       const float4 v = *reinterpret_cast<const float4*>(part_of(c) + 4 * r);
       const float top = fmaxf(mx, v.x);
       l = l * exp2f(mx - top) + v.y * exp2f(v.x - top);
+      vx = fmaxf(vx + (mx - top), v.z + (v.x - top));
       mx = top;
-      vx = fmaxf(vx, v.z);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       const float m2 = __shfl_xor_sync(0xffffffffu, mx, o), l2 = __shfl_xor_sync(0xffffffffu, l, o), top = fmaxf(mx, m2);
       l = l * exp2f(mx - top) + l2 * exp2f(m2 - top);
+      vx = fmaxf(vx + (mx - top), __shfl_xor_sync(0xffffffffu, vx, o) + (m2 - top));
       mx = top;
-      vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, o));
     }
   };
   if (!scores) {
@@ -532,7 +535,7 @@ kv_join_kernel(const __grid_constant__ AttnArgs a, int row_blocks, int* dbg) {
 #pragma unroll 8
     for (uint32_t c = c0 + who; c <= c1; c += SHARES) {
       const float* part = part_of(c);
-      const float by = exp2f(part[4 * row + 2] - vx);
+      const float by = exp2f(part[4 * row + 2] + (part[4 * row] - mx) - vx);
       const float4 v = *reinterpret_cast<const float4*>(part + 4 * ROWS + row * D + d);
       y.x = fmaf(v.x, by, y.x); y.y = fmaf(v.y, by, y.y); y.z = fmaf(v.z, by, y.z); y.w = fmaf(v.w, by, y.w);
     }
@@ -547,7 +550,7 @@ kv_join_kernel(const __grid_constant__ AttnArgs a, int row_blocks, int* dbg) {
     }
     const long long at = (long long)(s.row0 + row / sh.group) * sh.heads + h * sh.group + row % sh.group;
     if (!QALORA_CHECK(dbg, at, (long long)a.kb.m * sh.heads)) return;
-    kvp::store_row4(a.at.out + at * D + d, RowScale(vx, mx, l)(y));
+    kvp::store_row4(a.at.out + at * D + d, RowScale(vx, l)(y));
     if (d == 0) kvp::store_lse(a.at.lse, at, nullptr, 0, mx, l, 0.f);
     return;
   }

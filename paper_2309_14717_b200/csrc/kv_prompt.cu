@@ -22,7 +22,7 @@ constexpr int PT_RING = 8;                    // tiles whose blocks and scales a
 constexpr int PT_RING_FLOATS = 48;            // ks[8], log2 of vs / ref [8], ref / vs [8], {ref_before / ref, ref, all there}, blocks of
                                               // keys [8] at 32 and of values [8] at 40
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNoMax = -1e30f;
+constexpr float kNoMax = -3.40282347e38f;
 constexpr float kGrow = 6.f, kLift = 8.f;     // as in the few-row kernel: weights at most 2^14 in fp16
 constexpr float kTiny = 1e-37f;               // stands for a smaller factor of a score (|score| < 2^30): keeps 0 * -inf away
 constexpr float kLeastExponent = -80.f, kLeastValueScale = 0x1p-80f;   // of the largest one met so far: below it a block's values count as 0

@@ -327,3 +327,35 @@ def test_exponentials_of_gathered_weights(places):
     t = np.arange(1, cached)
     ratio = got.double().cpu().numpy()[c.table[0][t // 16], 0, t % 16] / r["score"][c.table[0][t // 16], 0, t % 16]
     assert np.abs(ratio / ratio.mean() - 1).max() <= 2 * (np.log(2) * (2.0 ** -22 + 2.0 ** -21) + 2.0 ** -22 + len(mild) * 2.0 ** -24)
+
+
+# ------------------------------------------------------------------------- scores of any magnitude
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("heads,dim,new,power", [(1, 64, 1, 110), (2, 128, 3, 110), (1, 64, 50, 12), (2, 128, 50, 12)])
+def test_scores_far_beyond_any_weight(heads, dim, new, power, sign):
+    """Scores of +-2^power * 64 .. 123: every row weights one token alone (no two have the same score), the first row its only
+    one.  With few rows any float32 score will do, with many up to 2^20.  What a row gives its token is 1 but for its score's
+    rounding, 2^-22 of it after four operations; with few rows maximum and score are the same number."""
+    rng = np.random.default_rng(dim + new)
+    for length in (new, 55):
+        c = Cache(rng, [length], heads, heads, dim, 16)
+        key = rng.permutation(60)[:length] + 64
+        c.codes[:, 0] = 0
+        for t in range(length):
+            c.codes[c.table[0, t // 16], 0, :, t % 16, 0] = key[t]
+        c.scales[:, 0] = np.float32(2.0 ** (power // 2))
+        q = np.zeros((new, heads, dim))
+        q[..., 0] = sign * 2.0 ** (power - power // 2)
+        out, lse, got, _ = attend(c, q, [new], 1.0, True, score_in=False)
+        gathered = np.zeros((length, heads))
+        for i in range(new):
+            t = int(np.argmax(sign * key[:length - new + i + 1]))
+            blk = c.table[0, t // 16]
+            want = torch.as_tensor(c.codes[blk, 1, :, t % 16].astype(np.float64) * c.scales[blk, 1].astype(np.float64)[:, None])
+            assert (out[i].double().cpu() - want).abs().max() <= 2.0 ** -8 * want.abs().max()
+            norm = sign * 2.0 ** power * float(key[t])
+            assert (np.abs(lse[i].double().cpu().numpy() - norm) <= 2.0 ** -22 * abs(norm)).all()
+            gathered[t] += 1
+        t = np.arange(length)
+        off = 0 if new * heads <= 16 else np.expm1(2.0 ** -22 * 2.0 ** power * 127)
+        assert (np.abs(got.cpu().numpy()[c.table[0][t // 16], :, t % 16] - gathered) <= off * gathered).all()
