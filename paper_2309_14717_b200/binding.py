@@ -471,7 +471,9 @@ def _kv_checked(d, starts, lens, table, codes, scales, *rows):
 
 
 def _kv_stream(stream, t):
-    return stream.cuda_stream if stream is not None else _current_stream(t.get_device())
+    if stream is not None:
+        return stream.cuda_stream
+    return _current_stream(t.get_device()) if _current_stream is not None else torch.cuda.current_stream(t.device).cuda_stream
 
 
 def qalora_kv_append(d: KvDesc, max_new: int, starts, lens, table, k, v, codes, scales, score=None, dev_status=None,

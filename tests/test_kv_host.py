@@ -1,5 +1,8 @@
 """Host-side rules of the key/value cache calls that need no GPU."""
+import types
+
 import pytest
+import torch
 
 from paper_2309_14717_b200 import binding as Q
 from paper_2309_14717_b200 import build as _build
@@ -18,3 +21,14 @@ def test_scratch_of_few_rows_does_not_vanish_when_m_is_a_bound(batch, max_new, g
     exact = Q.qalora_kv_attention_workspace_bytes(d, batch, batch * max_new, max_new, 2048, scores)
     for m in (batch * max_new + 1, batch * max_new + max_new, 2 * batch * max_new + 16, 4096):
         assert Q.qalora_kv_attention_workspace_bytes(d, batch, m, max_new, 2048, scores) >= exact
+
+
+def test_stream_without_the_raw_handle(monkeypatch):
+    """A torch that does not offer the raw handle of its current stream: the stream object's is taken."""
+    t = torch.zeros(1)
+    monkeypatch.setattr(Q, "_current_stream", None)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=77, device=device))
+    assert Q._kv_stream(None, t) == 77
+    assert Q._kv_stream(types.SimpleNamespace(cuda_stream=5), t) == 5
+    monkeypatch.setattr(Q, "_current_stream", lambda device: 9)
+    assert Q._kv_stream(None, t) == 9
