@@ -99,7 +99,7 @@ class Block:
         self.kv = Q.kv_desc(cfg.heads, cfg.kv_heads, cfg.head_dim, cfg.block_tokens, cfg.pool_blocks)
         self.codes, self.scales, self.score = Q.alloc_kv_cache(self.kv)
 
-    def forward(self, x, position, max_new, max_len, starts, lens, table):
+    def forward(self, x, position, max_new, max_len, starts, lens, table, work):
         cfg, m = self.cfg, x.shape[0]
         h = normalise(x)
         y = {name: torch.empty(m, self.layers[name].width, dtype=torch.bfloat16, device=x.device) for name in "qkv"}
@@ -111,7 +111,6 @@ class Block:
         Q.qalora_kv_append(self.kv, max_new, starts, lens, table, k, y["v"].view(m, cfg.kv_heads, cfg.head_dim), self.codes,
                            self.scales, self.score)
         attended = torch.empty(m, cfg.heads, cfg.head_dim, dtype=torch.bfloat16, device=x.device)
-        work = Q.alloc_kv_workspace(self.kv, lens.shape[0], m, max_new, max_len, True)
         Q.qalora_kv_attention(self.kv, max_new, max_len, starts, lens, table, q, self.codes, self.scales, cfg.head_dim ** -0.5,
                               attended, score_in=self.score, score_out=self.score, workspace=work)
         out, o = torch.empty_like(x), self.layers["o"]
@@ -149,7 +148,9 @@ class Server:
             self.lens[b] += n
             self.held[b] += self._take(self.lens[b] - len(self.held[b]) * self.cfg.block_tokens)
         as_int = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
-        args = (max(new), max(self.lens), as_int(starts), as_int(self.lens), self._table(self.held))
+        # (one scratch for the step: the blocks' attention calls follow each other)
+        work = Q.alloc_kv_workspace(self.blocks[0].kv, len(new), x.shape[0], max(new), max(self.lens), True)
+        args = (max(new), max(self.lens), as_int(starts), as_int(self.lens), self._table(self.held), work)
         for block in self.blocks:
             x = block.forward(x, as_int(position), *args)
         return x

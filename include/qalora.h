@@ -409,7 +409,9 @@ int qalora_kv_read(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t
  * softmax_scale must be positive and finite.  No atomics: results are reproducible bit for bit
  * for given bounds and device.  `workspace`: qalora_kv_attention_workspace_bytes() bytes for
  * the same batch, m, max_new and max_len, content undefined; its first int32 becomes the
- * status word described at qalora_workspace_bytes. */
+ * status word described at qalora_workspace_bytes.  With score_out it holds the scores of
+ * sequences with few new rows, 4 * batch * heads * max_len * the least of max_new and
+ * 16 / (heads / kv_heads) bytes. */
 int qalora_kv_attention_workspace_bytes(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t max_new,
                                         int32_t max_len, int with_score, size_t* bytes);
 int qalora_kv_attention(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t max_new, int32_t max_len,

@@ -523,9 +523,12 @@ def qalora_kv_attention_workspace_bytes(d: KvDesc, batch: int, m: int, max_new: 
 
 def alloc_kv_workspace(d: KvDesc, batch: int, m: int, max_new: int, max_len: int, with_score: bool = False,
                        device="cuda") -> torch.Tensor:
-    """Scratch of qalora_kv_attention_workspace_bytes() bytes; workspace_status() reads its status word."""
-    return torch.zeros(max(qalora_kv_attention_workspace_bytes(d, batch, m, max_new, max_len, with_score), 16),
-                       dtype=torch.uint8, device=device)
+    """Scratch of qalora_kv_attention_workspace_bytes() bytes; workspace_status() reads its status word, the only part that
+    is cleared.  One will do for all layers of a model: their calls follow each other on a stream."""
+    scratch = torch.empty(max(qalora_kv_attention_workspace_bytes(d, batch, m, max_new, max_len, with_score), 16),
+                          dtype=torch.uint8, device=device)
+    scratch[:4].zero_()
+    return scratch
 
 
 def qalora_kv_attention(d: KvDesc, max_new: int, max_len: int, starts, lens, table, q, codes, scales, softmax_scale: float, out,

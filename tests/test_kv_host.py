@@ -32,3 +32,15 @@ def test_stream_without_the_raw_handle(monkeypatch):
     assert Q._kv_stream(types.SimpleNamespace(cuda_stream=5), t) == 5
     monkeypatch.setattr(Q, "_current_stream", lambda device: 9)
     assert Q._kv_stream(None, t) == 9
+
+
+def test_scratch_is_allocated_not_cleared(monkeypatch):
+    """Its content may be undefined: only the status word is set."""
+    def dirty(*shape, **kw):
+        return torch.full(shape if isinstance(shape[0], int) else shape[0], 0xAB, **kw)
+
+    monkeypatch.setattr(torch, "empty", dirty)
+    d = Q.kv_desc(8, 2, 128, 64, 100)
+    ws = Q.alloc_kv_workspace(d, 3, 6, 2, 1000, True, device="cpu")
+    assert ws.numel() == Q.qalora_kv_attention_workspace_bytes(d, 3, 6, 2, 1000, True)
+    assert Q.workspace_status(ws) == 0 and (ws[256:] == 0xAB).all()
