@@ -377,7 +377,8 @@ int qalora_kv_cache_bytes(const qalora_kv_desc* desc, size_t* code_bytes, size_t
  *   dev_status : as in qalora_quantize, bit 0 is OR-ed in when x is not finite: infinities
  *                become +-127, NaNs 0, and neither enters a scale.  May be NULL.
  * A sequence of the batch may have no new rows.  No block may appear twice among those that
- * the new tokens enter. */
+ * the new tokens enter (full blocks of a common beginning may be shared by sequences; one that
+ * is still being filled changes for all that name it). */
 int qalora_kv_append(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t max_new,
                      const int32_t* starts, const int32_t* lens, const int32_t* table, int32_t max_blocks,
                      const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -397,7 +398,10 @@ int qalora_kv_read(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t
  * and, when score_out is not NULL, for every token t of a sequence that has new rows,
  *   score_out[t] = score_in[t] + sum over the sequence's new rows i and the heads of the group
  *                  of softmax(S[i, :])_t
- * in the layout of `score`; score_in may be NULL (zeros) and may be score_out.  Sums and
+ * in the layout of `score`; score_in may be NULL (zeros) and may be score_out.  Sequences may
+ * share blocks, but not with score_out: no block may then belong to two sequences that have
+ * new rows, as each writes its own sum to the block's entries and one of them is lost (call
+ * once for each of them, score_out being the next call's score_in, to add them up).  Sums and
  * softmax statistics are float32, exponentials have a relative error of 2^-22, products are
  * exact (8-bit codes and bf16 in fp16 operands);
  * a row's weights times the value scales of their blocks are rounded to fp16, relative to the
@@ -425,8 +429,8 @@ int qalora_kv_attention(const qalora_kv_desc* desc, int32_t batch, int64_t m, in
  * largest score (ties go to the earlier token; NaN counts as the largest), in their order, are
  * copied to the blocks that dst_table names, with their scores.  Sequences of at most `budget`
  * tokens are copied whole.  Scales are made anew from the copied values as by qalora_kv_append
- * into empty blocks.  The destination blocks must not be among the sources; the caller frees
- * the sources afterwards.
+ * into empty blocks.  Sources may be shared; the destination blocks must not be among them, nor
+ * appear twice.  The caller frees the sources afterwards.
  *   dst_lens out int32 [batch];  kept out int32 [batch][kv_heads][budget]: the source position
  *   of each copied token, -1 beyond dst_lens. */
 int qalora_kv_evict(const qalora_kv_desc* desc, int32_t batch, int32_t max_len, int32_t budget, int32_t recent,

@@ -534,7 +534,8 @@ def alloc_kv_workspace(d: KvDesc, batch: int, m: int, max_new: int, max_len: int
 def qalora_kv_attention(d: KvDesc, max_new: int, max_len: int, starts, lens, table, q, codes, scales, softmax_scale: float, out,
                         lse=None, score_in=None, score_out=None, workspace=None, stream=None):
     """out bf16 [m, heads, head_dim] = attention of the new tokens (rows q) over their sequences in the cache; lse float32
-    [m, heads]; score_out = score_in + the attention weight that each cached token gathered."""
+    [m, heads]; score_out = score_in + the attention weight that each cached token gathered (no block may then belong to
+    two sequences with new rows)."""
     at, pool = _kv_batch_at(starts, lens, table), _kv_cache_at(d, codes, scales)
     if at is None or pool is None:
         at, pool = _kv_checked(d, starts, lens, table, codes, scales, ("q", q, d.heads))

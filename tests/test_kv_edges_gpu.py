@@ -359,3 +359,34 @@ def test_scores_far_beyond_any_weight(heads, dim, new, power, sign):
         t = np.arange(length)
         off = 0 if new * heads <= 16 else np.expm1(2.0 ** -22 * 2.0 ** power * 127)
         assert (np.abs(got.cpu().numpy()[c.table[0][t // 16], :, t % 16] - gathered) <= off * gathered).all()
+
+
+# ------------------------------------------------------------------------------ shared beginnings
+@pytest.mark.parametrize("new", [[1, 1, 1], [3, 0, 2], [60, 40, 33], [60, 1, 2]])
+def test_sequences_that_share_their_beginning(new):
+    """Blocks of a common beginning, named by every sequence's table: the same numbers as with copies of them; with gathered
+    weights one call for each sequence, whose sums add up in the shared blocks."""
+    rng = np.random.default_rng(sum(new))
+    lens, heads, kv_heads, dim, block, common = [150, 200, 131], 4, 2, 128, 32, 3
+    c = Cache(rng, lens, heads, kv_heads, dim, block)
+    for row in c.table[1:]:
+        for j in range(common):
+            c.codes[row[j]], c.scales[row[j]], c.score[row[j]] = (x[c.table[0, j]] for x in (c.codes, c.scales, c.score))
+    q = bf16(rng.standard_normal((sum(new), heads, dim)))
+    want, want_lse, _, _ = attend(c, q, new, 0.1)
+    c.table[1:, :common] = c.table[0, :common]
+    out, lse, _, _ = attend(c, q, new, 0.1)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    check(c, q, new, 0.1, out, lse)
+    codes, scales, score = c.up()
+    starts = starts_of(new)
+    for b in range(3):
+        if new[b]:
+            rows = dev(q[starts[b]:starts[b + 1]]).bfloat16()
+            ws = Q.alloc_kv_workspace(c.d, 1, new[b], new[b], lens[b], True)
+            Q.qalora_kv_attention(c.d, new[b], lens[b], dev(starts_of([new[b]])), dev(c.lens[b:b + 1]), dev(c.table[b:b + 1]), rows, codes,
+                                  scales, 0.1, torch.empty_like(rows), None, score, score, ws)
+    torch.cuda.synchronize()
+    r = K.attention(c.codes, c.scales, starts, c.lens, c.table, q, 0.1, c.score, True)
+    d = 2.0 ** -18 * (1 + r["reach"].max())
+    assert (np.abs(score.double().cpu().numpy() - r["score"]) <= d * (r["score"] - c.score) + 3 * 2.0 ** -22 * r["score"] + 1e-30).all()
