@@ -390,3 +390,25 @@ def test_sequences_that_share_their_beginning(new):
     r = K.attention(c.codes, c.scales, starts, c.lens, c.table, q, 0.1, c.score, True)
     d = 2.0 ** -18 * (1 + r["reach"].max())
     assert (np.abs(score.double().cpu().numpy() - r["score"]) <= d * (r["score"] - c.score) + 3 * 2.0 ** -22 * r["score"] + 1e-30).all()
+
+
+# ------------------------------------------------------------------------------ bounds-check build
+def test_edges_entries_and_sizes_pass_the_bounds_check_build():
+    """The tests here, those of entries that lead outside and those of the division of work, once more in a child process that
+    loads the build with index checks and workspace guards."""
+    import os
+    import subprocess
+    import sys
+    if os.environ.get("QALORA_LIBRARY") == "debug":
+        pytest.skip("already inside the bounds-check run")
+    from paper_2309_14717_b200 import build as B
+    B.build(debug=True)
+    env = dict(os.environ, QALORA_LIBRARY="debug")
+    env.pop("QALORA_PARITY_MARGINS", None)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    p = subprocess.run([sys.executable, "-m", "pytest", "-m", "gpu", "-x", "-q", "-p", "no:cacheprovider", "tests/test_kv_edges_gpu.py",
+                        "tests/test_kv_entries_gpu.py", "tests/test_kv_sizes_gpu.py"], cwd=root, env=env, capture_output=True, text=True,
+                       timeout=1500)
+    tail = "\n".join((p.stdout + p.stderr).splitlines()[-40:])
+    assert p.returncode == 0, tail
+    assert " passed" in p.stdout and "bounds-check build" in p.stdout, tail
