@@ -238,6 +238,8 @@ kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       }
       cur = next;
     }
+    // nothing is on its way to shared memory when the block ends, also where a wait ran out (the limit holds here too)
+    for (uint32_t i = it < (uint32_t)STAGES ? 0 : it - STAGES; i < it; ++i) ptx::mbar_wait(full(i % STAGES), (i / STAGES) & 1, flag);
   } else {
     // ---- consumers
     const int g8 = lane >> 2, q4 = lane & 3;          // token (or channel pair) within 8, quad lane: rows 2 q4 and 2 q4 + 1

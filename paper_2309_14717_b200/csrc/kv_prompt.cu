@@ -55,7 +55,7 @@ struct PtSmem {
   static constexpr int OFF_STAGED = 6 * TILE;                 // keys, values
   static constexpr int OFF_RING = OFF_STAGED + 2 * STAGED;
   static constexpr int OFF_BARS = OFF_RING + PT_RING * PT_RING_FLOATS * 4;
-  static constexpr int NBARS = 1 + 4 * 2 + 6 * 2 + PT_RING + 4;
+  static constexpr int NBARS = 1 + 4 * 2 + 6 * 2 + PT_RING + 4 + 2;
   static constexpr int OFF_SLOT = OFF_BARS + NBARS * 8 + 8;
   static constexpr int TOTAL = OFF_SLOT + 16 + 1024;
 };
@@ -206,6 +206,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
   auto r_used = [&](int x) { return bars + 168 + 8 * x; };              // the codes of a tile have been converted
   auto c_full = [&](int w) { return bars + 168 + 8 * (PT_RING + w); };  // codes of keys (0) or values (1) are staged
   auto c_empty = [&](int w) { return bars + 168 + 8 * (PT_RING + 2 + w); };
+  auto given_up = [&](int i) { return bars + 168 + 8 * (PT_RING + 4 + i); };    // products issued before a wait ran out are done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::OFF_SLOT);
   volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_SLOT + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -245,7 +246,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       for (int y = 0; y < 2; ++y) { ptx::mbar_init(s_full(x, y), 1); ptx::mbar_init(p_full(x, y), 4); ptx::mbar_init(o_done(x, y), 1); }
     }
     for (int x = 0; x < PT_RING; ++x) ptx::mbar_init(r_used(x), PT_CONV);
-    for (int x = 0; x < 2; ++x) { ptx::mbar_init(c_full(x), 1); ptx::mbar_init(c_empty(x), PT_CONV); }
+    for (int x = 0; x < 2; ++x) { ptx::mbar_init(c_full(x), 1); ptx::mbar_init(c_empty(x), PT_CONV); ptx::mbar_init(given_up(x), 1); }
     ptx::fence_mbar_init();
   }
   if (warp == PT_ISSUE) {
@@ -544,6 +545,10 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
         __syncwarp();
         if (step + 2 < 2 * count) ok = scores(step + 2);
       }
+      if (!ok) {                                                 // (the limit of a wait holds here too)
+        kvp::mma_commit(leader, given_up(i));
+        wait(given_up(i), 0);
+      }
     } else if (i == 2) {
       // ------------------------------------------------------------------------- look-ups ----
       // lane l < 8: block and scales of tokens 16 l ... of a tile, each step of the chain table -> scales asked for one
@@ -561,6 +566,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       Look next = look(entry(0));
       int after = entry(1);
       float ref = 0.f;
+      int sent[2] = {0, 0};                                      // tiles of keys, of values
       for (int it = 0; it < count; ++it) {
         const Look cur = next;
         next = look(after);
@@ -606,9 +612,13 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
           if (copies)
             ptx::bulk_load(sbase + S::OFF_STAGED + w * S::STAGED + lane * 16 * D,
                            a.at.codes + (((long long)id * 2 + w) * sh.kv_heads + h) * sh.block * D, (uint32_t)(sh.block * D), c_full(w));
+          ++sent[w];
         }
         if (!ok) break;
       }
+      // nothing is on its way to shared memory when the block ends, also where a wait ran out
+#pragma unroll
+      for (int w = 0; w < 2; ++w) if (sent[w] > 0) ptx::mbar_wait(c_full(w), (sent[w] - 1) & 1, flag);
     }
     __syncwarp();
   }
@@ -668,7 +678,7 @@ struct PsSmem {
   static constexpr int NROWS = 4;
   static constexpr int OFF_SUM = OFF_ROWS + NROWS * 128 * 8;     // [2][128] sums of the second half; of the block
   static constexpr int OFF_BARS = OFF_SUM + 1024;
-  static constexpr int NBARS = 1 + 2 * STAGES + 2 * 2;
+  static constexpr int NBARS = 1 + 2 * STAGES + 2 * 2 + 1;
   static constexpr int OFF_SLOT = OFF_BARS + NBARS * 8 + 8;
   static constexpr int TOTAL = OFF_SLOT + 16 + 1024;
 };
@@ -714,6 +724,7 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int* dbg) {
   auto q_empty = [&](int x) { return bars + 8 + 8 * (S::STAGES + x); };
   auto s_full = [&](int x) { return bars + 8 + 8 * (2 * S::STAGES + x); };
   auto s_empty = [&](int x) { return bars + 8 + 8 * (2 * S::STAGES + 2 + x); };
+  const uint32_t given_up = bars + 8 + 8 * (2 * S::STAGES + 4);                 // as in kv_prompt_kernel
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::OFF_SLOT);
   volatile int* flag = reinterpret_cast<volatile int*>(smem + S::OFF_SLOT + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -735,6 +746,7 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int* dbg) {
     ptx::mbar_init(k_full, 8);
     for (int x = 0; x < S::STAGES; ++x) { ptx::mbar_init(q_full(x), 1); ptx::mbar_init(q_empty(x), 1); }
     for (int x = 0; x < 2; ++x) { ptx::mbar_init(s_full(x), 1); ptx::mbar_init(s_empty(x), 4); }
+    ptx::mbar_init(given_up, 1);
     ptx::fence_mbar_init();
   }
   if (warp == 8) {
@@ -841,11 +853,16 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int* dbg) {
         ptx::mma_commit(s_full(buf));
         ptx::mma_commit(q_empty(st));
       }
+      if (!ok) {
+        ptx::mma_commit(given_up);
+        ptx::mbar_wait(given_up, 0, flag);
+      }
     }
     __syncwarp();
   } else {
     if (lane == 0) {
-      for (int it = 0; it < count; ++it) {
+      int it = 0;
+      for (; it < count; ++it) {
         const int st = it % S::STAGES;
         if (it >= S::STAGES && !ptx::mbar_wait(q_empty(st), ((it / S::STAGES) - 1) & 1, flag)) break;
         // (the rows' entry was last read for the tile four before, whose accumulator has since been handed back: the
@@ -855,6 +872,7 @@ kv_prompt_score_kernel(const __grid_constant__ PromptArgs a, int* dbg) {
         ptx::bulk_load(sbase + S::OFF_Q + st * S::TILE, a.q_image + (slot0 + it) * S::TILE, S::TILE, q_full(st));
         ptx::bulk_load(sbase + S::OFF_ROWS + (it % S::NROWS) * 1024, a.rows + (slot0 + it) * 2 * PT_ROWS, 1024, q_full(st));
       }
+      for (int i = it < S::STAGES ? 0 : it - S::STAGES; i < it; ++i) ptx::mbar_wait(q_full(i % S::STAGES), (i / S::STAGES) & 1, flag);
     }
     __syncwarp();
   }
