@@ -430,7 +430,8 @@ int qalora_kv_attention(const qalora_kv_desc* desc, int32_t batch, int64_t m, in
  * copied to the blocks that dst_table names, with their scores.  Sequences of at most `budget`
  * tokens are copied whole.  Scales are made anew from the copied values as by qalora_kv_append
  * into empty blocks.  Sources may be shared; the destination blocks must not be among them, nor
- * appear twice.  The caller frees the sources afterwards.
+ * appear twice, and dst_max_blocks must hold the least of budget, max_len and the tokens that
+ * max_blocks hold.  The caller frees the sources afterwards.
  *   dst_lens out int32 [batch];  kept out int32 [batch][kv_heads][budget]: the source position
  *   of each copied token, -1 beyond dst_lens. */
 int qalora_kv_evict(const qalora_kv_desc* desc, int32_t batch, int32_t max_len, int32_t budget, int32_t recent,

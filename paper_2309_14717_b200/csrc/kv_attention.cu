@@ -113,7 +113,8 @@ struct RowScale {
 //   O^T = V^T P^T the transposing ldmatrix, whose 16-bit elements are pairs of channels, gives the even and the odd
 //                 channels as rows 0-7 and 8-15 of A; P^T is S^T's result through movmatrix.
 // (With the query rows as the 16 rows of the product, most of them padding, the same work took twice the products and
-// 450 instead of 250 instructions per 16 tokens: 32 conversations of up to 4096 tokens 181 us, against 115: 5.2 TB/s.)
+// 450 instead of 250 instructions per 16 tokens: 32 conversations of up to 4096 tokens 181 us, against 115 to 122 from GPU
+// to GPU: 5.0 to 5.3 TB/s.)
 // Codes turn into fp16 exactly (1024 + 128 + c by byte permutation, minus 1152), the query is fp16 after a
 // power-of-two scaling per row (bf16 has fewer bits), so the scores are sums of exact products in float32.
 // Every warp keeps maximum, sum and output of its own tokens; the warps meet only at the end of a row tile.
@@ -122,8 +123,9 @@ struct RowScale {
 // (held as a difference from the largest score, which would swallow e where scores are large), those of the softmax's sum
 // to its largest score.  So both keep their bits wherever the scales lie in float32, for
 // a second exponential.  (Against weights relative to the score alone, times the scale relative to the largest one: 32
-// conversations of up to 4096 tokens 121.4 us and 122.0, two documents of up to 100 003 tokens with eight heads to a key
-// head and gathered weights 78.5 and 77.8, four new tokens of 16 of up to 4000, 32 heads on 8, 43.1 and 45.2.)
+// conversations of up to 4096 tokens 121.9 us and 121.4, two documents of up to 100 003 tokens with eight heads to a key
+// head and gathered weights 78.5 and 77.3, four new tokens of 16 sequences, 32 heads on 8: of up to 4000 tokens with
+// heads of 128 43.8 and 45.3, of 6000 with heads of 64 33.0 and 31.8.)
 template <int D, int NT, int SUB>
 __global__ void __launch_bounds__(AT_THREADS, AtSmem<D, NT, SUB>::BLOCKS)
 kv_attend_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnArgs a, int* dbg) {

@@ -710,7 +710,8 @@ __device__ __forceinline__ float2 exp2_fma(float2 y) {
 // so that one's tile of keys is fetched and its products run while the other's exponentials do.  Those bound it: two
 // pieces of up to 700 tokens, 32 heads of 64, against up to 12345 cached ones 180 us with one block of four
 // accumulators, 138 with two blocks (the exponential unit busy for 71 % of the time), 128 with a quarter of the
-// exponentials on the FMA pipe (an eighth 133, three eighths 135, half 145).
+// exponentials on the FMA pipe (an eighth 133, three eighths 135, half 145).  The unit is then busy for 56 % of the time and
+// the issue slots for 52 %, so that neither is a limit by itself.
 // COLS: groups of 32 rows of a row tile that may be there (one where a sequence has 32 rows at most).
 template <int D, int COLS>
 __global__ void __launch_bounds__(320, 2)
