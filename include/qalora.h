@@ -407,9 +407,9 @@ int qalora_kv_read(const qalora_kv_desc* desc, int32_t batch, int64_t m, int32_t
  * a row's weights times the value scales of their blocks are rounded to fp16, relative to the
  * row's largest such product, before they meet the codes; where a sequence has many new rows
  * (more than 16 / (heads / kv_heads)), values of blocks whose scale is below 2^-80 of the
- * largest value scale met so far count as zeros, and scores may be up to 2^20 in magnitude
- * (from there on a weight's exponent has no bits left behind the point, and from 2^27 on rows
- * may come out as NaN).
+ * largest value scale met so far count as zeros, and a row whose largest score is beyond 2^24
+ * in magnitude adds nothing to score_out.  (A score's rounding, 2^-24 of it or more, shows in
+ * its weight.)
  * softmax_scale must be positive and finite.  No atomics: results are reproducible bit for bit
  * for given bounds and device.  `workspace`: qalora_kv_attention_workspace_bytes() bytes for
  * the same batch, m, max_new and max_len, content undefined; its first int32 becomes the

@@ -19,8 +19,10 @@ constexpr int PT_TOK = 128, PT_ROWS = 128;    // a tile: tokens x rows (new toke
 constexpr int PT_HALF = 64;                   // tokens of a step: half a tile
 constexpr int PS_MAX_CLUSTER = 8;             // thread blocks that share a token tile's row tiles
 constexpr int PT_RING = 8;                    // tiles whose blocks and scales are kept
-constexpr int PT_RING_FLOATS = 48;            // ks[8], log2 of vs / ref [8], ref / vs [8], {ref_before / ref, ref, all there}, blocks of
-                                              // keys [8] at 32 and of values [8] at 40
+constexpr int PT_RING_FLOATS = 48;            // ks[8], log2 of vs / ref [8], ref / vs [8], {ref_before / ref, ref, all there, largest ks},
+                                              // blocks of keys [8] at 32 and of values [8] at 40
+constexpr float kLargeFactor = 0x1p-9f;       // of S, which allows scores beyond 2^20 (|S| <= 2^29)
+constexpr float kMostGathered = 0x1p24f;      // largest score with which a row takes part in the gathered weights
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoMax = -3.40282347e38f;
 constexpr float kGrow = 6.f, kLift = 8.f;     // as in the few-row kernel: weights at most 2^14 in fp16
@@ -129,11 +131,12 @@ __device__ __forceinline__ float softmax_top(float (&x)[PT_HALF], const float4 c
   return top;
 }
 
-// The step's weights to P, over its own columns of S; inv: the inverse of the relative value scale.
+// The step's weights to P, over its own columns of S; inv: the inverse of the relative value scale; m: what the scores are
+// relative to.
 template <int q>
-__device__ __forceinline__ void softmax_exp(SoftmaxRow& w, const float (&x)[PT_HALF], const float4 c, const float4 off, const float4 inv, uint32_t t_s) {
+__device__ __forceinline__ void softmax_exp(SoftmaxRow& w, float m, const float (&x)[PT_HALF], const float4 c, const float4 off, const float4 inv, uint32_t t_s) {
   const float cs[4] = {c.x, c.y, c.z, c.w}, os[4] = {off.x, off.y, off.z, off.w}, is[4] = {inv.x, inv.y, inv.z, inv.w};
-  const float base = kLift - w.m;
+  const float base = kLift - m;
   {
     uint32_t pk[16];
 #pragma unroll
@@ -161,7 +164,9 @@ template <int D>
 __device__ __forceinline__ void spoil_row(uint8_t* q_image, long long slot, int row) {
   *reinterpret_cast<uint16_t*>(q_image + slot * PtSmem<D>::TILE + row * 128 + ((row & 7) << 4)) = 0x7fff;
 }
-__device__ __forceinline__ float minus_log2_sum(float m, float l) { return l > 0.f ? kLift - m - log2f(l) : -INFINITY; }
+// (A score here and the row's logarithm are rounded apart: with scores beyond 2^24 their difference is no longer a weight's
+// exponent, and the row is left out.)
+__device__ __forceinline__ float minus_log2_sum(float m, float l) { return l > 0.f && fabsf(m) <= kMostGathered ? kLift - m - log2f(l) : -INFINITY; }
 
 // Two tiles of 128 rows of one kv head against a range of its sequence's tokens, in tiles of 128 and steps of 64:
 //   look-up warp      blocks and scales of a tile, bulk copies of its codes;
@@ -345,21 +350,23 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
       const uint32_t t_mine = t_s + PT_HALF * (step & 1);
       const float4* rg = reinterpret_cast<const float4*>(ring + ((step >> 1) % PT_RING) * PT_RING_FLOATS) + (step & 1);
       const float4 k = rg[0], off = rg[2], inv = rg[4];
-      const float4 c = make_float4(fmaxf(factor * k.x, kTiny), fmaxf(factor * k.y, kTiny), fmaxf(factor * k.z, kTiny), fmaxf(factor * k.w, kTiny));
-      const float2 refs = *reinterpret_cast<const float2*>(rg - (step & 1) + 6);      // {reference before the tile / in it, in it}
+      float4 c = make_float4(fmaxf(factor * k.x, kTiny), fmaxf(factor * k.y, kTiny), fmaxf(factor * k.z, kTiny), fmaxf(factor * k.w, kTiny));
+      const float4 refs = rg[6 - (step & 1)];                    // {reference before the tile / in it, in it, -, largest scale of keys}
+      const bool large = factor * refs.w > kLargeFactor;
       const float ref_ratio = (step & 1) == 0 ? refs.x : 1.f;
       w.ref = refs.y;
       const int t0 = (2 * first + step) * PT_HALF;
       ptx::tmem_wait_ld();
       const float most = softmax_top(x, c, off, t0 + PT_HALF - 1 > limit_lo, limit - t0);
-      if (__any_sync(0xffffffffu, most > w.m + kGrow) || ref_ratio != 1.f) {
+      float m = w.m;
+      if (__any_sync(0xffffffffu, most > m + kGrow || large) || ref_ratio != 1.f) {
         // Rare: the maximum and the outputs are brought up to date.  With a larger reference the logarithms of all relative
         // scales fall, and the maximum with them; else the weights of values like the earlier ones would sink into fp16's
         // subnormals.  The sum, which no scale enters, grows in turn, so that the fall is limited.
         float fall = 0.f;
         if (ref_ratio != 1.f) fall = fmaxf(fmaxf(log2f(ref_ratio), kLeastExponent), fminf(log2f(w.l) - kMostSum, 0.f));
         const float top = fmaxf(w.m + fall, most), by = exp2f(w.m - top), scale = by * ref_ratio;
-        w.m = top;
+        m = w.m = top;
         w.l *= by;
         if (step > 0) {
           if (!__all_sync(0xffffffffu, ptx::mbar_wait(o_done(i, step - 1), ((step - 1) >> 1) & 1, flag))) return false;
@@ -374,9 +381,20 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
             ptx::tmem_st16(t_o + 16 * q, o);
           }
         }
+        if (large) {
+          // The weights' exponents are a fused product minus a rounded maximum, which of scores beyond 2^27 may be any number.
+          // So the product is rounded too, and its difference from the maximum bounded.  (That such scores are looked for at all:
+          // 178.1 us and 179.2 for a 4096-token prompt of 32 heads of 128.)
+          const float cs[4] = {c.x, c.y, c.z, c.w}, os[4] = {off.x, off.y, off.z, off.w};
+#pragma unroll
+          for (int t = 0; t < PT_HALF; ++t)
+            x[t] = kvp::min_nan(__fadd_rn(__fmul_rn(x[t], cs[t >> 4]), -m), kGrow - os[t >> 4]);
+          c = make_float4(1.f, 1.f, 1.f, 1.f);
+          m = 0.f;
+        }
       }
-      softmax_exp<0>(w, x, c, off, inv, t_mine);
-      softmax_exp<1>(w, x, c, off, inv, t_mine);
+      softmax_exp<0>(w, m, x, c, off, inv, t_mine);
+      softmax_exp<1>(w, m, x, c, off, inv, t_mine);
       ptx::tmem_wait_st();
       ptx::tc_fence_before();
       __syncwarp();
@@ -573,9 +591,13 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
         after = entry(it + 2);
         // value scales relative to the largest one so far; blocks far below it (or of zeros) count as zeros
         const float ks = cur.id >= 0 ? cur.ks : 0.f, vs = cur.id >= 0 ? cur.vs : 0.f;
-        float top = vs;
+        float top = vs, k_top = ks;
 #pragma unroll
-        for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        for (int o = 4; o > 0; o >>= 1) {
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          k_top = fmaxf(k_top, __shfl_xor_sync(0xffffffffu, k_top, o));
+        }
+        k_top = __shfl_sync(0xffffffffu, k_top, 0);
         top = fmaxf(ref, __shfl_sync(0xffffffffu, top, 0));
         const float ratio = ref == top ? 1.f : ref / top;
         const float rel = top > 0.f ? vs / top : 0.f, least = fmaxf(rel, kLeastValueScale);
@@ -594,7 +616,7 @@ kv_prompt_kernel(const __grid_constant__ PromptArgs a, int pairs_max, int* dbg) 
           reinterpret_cast<int*>(rg)[32 + lane] = cur.id;
           reinterpret_cast<int*>(rg)[40 + lane] = v_id;
         }
-        if (lane == 8) { rg[24] = ratio; rg[25] = ref; reinterpret_cast<int*>(rg)[26] = all ? 1 : 0; }
+        if (lane == 8) { rg[24] = ratio; rg[25] = ref; reinterpret_cast<int*>(rg)[26] = all ? 1 : 0; rg[27] = k_top; }
         __syncwarp();
         // the codes of the blocks that are there, one copy each (a copy starts on a 16-byte boundary: blocks are multiples
         // of 1 KiB); lane 16-token group l stands for the block that begins with it

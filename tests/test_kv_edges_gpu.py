@@ -331,11 +331,12 @@ def test_exponentials_of_gathered_weights(places):
 
 # ------------------------------------------------------------------------- scores of any magnitude
 @pytest.mark.parametrize("sign", [-1, 1])
-@pytest.mark.parametrize("heads,dim,new,power", [(1, 64, 1, 110), (2, 128, 3, 110), (1, 64, 50, 12), (2, 128, 50, 12)])
+@pytest.mark.parametrize("heads,dim,new,power", [(1, 64, 1, 110), (2, 128, 3, 110), (1, 64, 50, 12), (2, 128, 50, 12), (1, 64, 50, 110),
+                                                 (2, 128, 50, 110), (1, 128, 50, 24)])
 def test_scores_far_beyond_any_weight(heads, dim, new, power, sign):
     """Scores of +-2^power * 64 .. 123: every row weights one token alone (no two have the same score), the first row its only
-    one.  With few rows any float32 score will do, with many up to 2^20.  What a row gives its token is 1 but for its score's
-    rounding, 2^-22 of it after four operations; with few rows maximum and score are the same number."""
+    one.  What a row gives its token is 1; with many rows but for its score's rounding, 2^-22 of it after four operations, and 0
+    with scores beyond 2^24."""
     rng = np.random.default_rng(dim + new)
     for length in (new, 55):
         c = Cache(rng, [length], heads, heads, dim, 16)
@@ -357,7 +358,9 @@ def test_scores_far_beyond_any_weight(heads, dim, new, power, sign):
             assert (np.abs(lse[i].double().cpu().numpy() - norm) <= 2.0 ** -22 * abs(norm)).all()
             gathered[t] += 1
         t = np.arange(length)
-        off = 0 if new * heads <= 16 else np.expm1(2.0 ** -22 * 2.0 ** power * 127)
+        if new * heads > 16 and power > 17:
+            gathered[:] = 0
+        off = 0 if new * heads <= 16 else np.expm1(2.0 ** -22 * 2.0 ** power * 127) if power < 17 else 0
         assert (np.abs(got.cpu().numpy()[c.table[0][t // 16], :, t % 16] - gathered) <= off * gathered).all()
 
 
